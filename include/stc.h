@@ -23,6 +23,9 @@
  *                        stc_decode_step_static: without a caller-provided workspace)
  *   recent tokens        stc_append_tail, stc_decode_attention_tail (uncompressed tail),
  *                        stc_flush_tail (tail tokens into the compressed cache, in place)
+ *   rotary positions     stc_rotary (a prompt's queries or keys, with its inverse),
+ *                        stc_rotary_append (a generated token: rotation, and its key and value
+ *                        into tails of different lengths), stc_rotary_turns (frequencies)
  *   per-query-head form  stc_select_pages_per_head, stc_decode_attention_per_head,
  *                        stc_union_pages + stc_decode_attention_union (shared K/V reads)
  *   helpers              stc_workspace_bytes, stc_bounds_bytes, stc_status_string, stc_version
@@ -98,6 +101,38 @@ enum {
    * token and layer (App. B.1); stc_router_logits with Hkv = 1 writes logits of that shape */
   STC_ROUTE_SHARED = 0x100
 };
+
+/* rotary positions: which two channels of the rotated part (channels 0 .. rot_dim-1 of a head)
+ * make a pair, pair j = 0 .. rot_dim/2 - 1 */
+enum {
+  STC_ROTARY_HALVES = 0,      /* channels j and j + rot_dim/2 */
+  STC_ROTARY_INTERLEAVED = 1, /* channels 2j and 2j + 1 */
+  /* flag, OR-ed into a layout (stc_rotary only): the transposed rotation, which takes positions
+   * away again and is the rotation's gradient */
+  STC_ROTARY_INVERSE = 0x100
+};
+
+/* rotary positions: frequencies beyond the context a model was trained on.  f_j = base^(-2j/rot_dim)
+ * radians per position, and */
+enum {
+  STC_ROTARY_SCALE_NONE = 0,       /* f_j */
+  STC_ROTARY_SCALE_LINEAR = 1,     /* f_j / factor: positions pressed together */
+  STC_ROTARY_SCALE_BASE = 2,       /* base * factor^(rot_dim/(rot_dim-2)) for base: the slowest pair
+                                      slows by factor, the fastest stays */
+  STC_ROTARY_SCALE_CHANNELS = 3,   /* f_j ((1-w) + w/factor); w rises from 0 to 1 between the pair
+                                      (rounded down) that makes `fast` rotations over original_len
+                                      and the one (rounded up) that makes `slow`, linearly in j */
+  STC_ROTARY_SCALE_WAVELENGTHS = 4 /* f_j (w + (1-w)/factor); w rises from 0 to 1 between `slow`
+                                      and `fast` rotations over original_len, linearly in them */
+};
+
+typedef struct stc_rotary_scaling {
+  int32_t kind;         /* STC_ROTARY_SCALE_* */
+  int32_t original_len; /* tokens; CHANNELS and WAVELENGTHS: >= 1 */
+  double base;          /* > 1 */
+  double factor;        /* > 0; not used by NONE */
+  double slow, fast;    /* rotations over original_len, 0 < slow < fast; CHANNELS, WAVELENGTHS */
+} stc_rotary_scaling_t;
 
 int stc_version(void);
 const char *stc_status_string(int status);
@@ -288,6 +323,63 @@ int stc_decode_step_tail(const stc_shape_t *shape, const void *q, const void *bo
  */
 int stc_append_tail(const stc_shape_t *shape, const void *k_new, const void *v_new, void *K_tail,
                     void *V_tail, int n_tail, int tail_cap, void *stream);
+
+/*
+ * Revolutions per position of the rot_dim/2 pairs, f_j / (2 pi), in 64 bits: what the calls below
+ * read as `turns`.
+ *   rot_dim  16, 32, .. 128
+ *   turns    [rot_dim/2] double, out, in HOST memory: the caller copies it to the device once
+ */
+int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t *scaling, double *turns);
+
+/*
+ * Rotary positions of a prompt's queries or keys (in front of stc_build_page_bounds: the cache holds
+ * keys with their positions).  Pair j of a head at position t turns by the angle
+ * a = 2 pi t turns[j]:
+ *   y0 = amplitude (x0 cos a - x1 sin a),  y1 = amplitude (x0 sin a + x1 cos a)
+ * (STC_ROTARY_INVERSE: -sin a for sin a); channels rot_dim .. D-1 are copied.  Angles are reduced to
+ * one revolution in 64 bits, the rest is float arithmetic with one rounding.
+ *   x, y      [B, H, N, D] bf16, in / out, with strides: x_stride and y_stride are HOST arrays of the
+ *             strides of b, h and n in elements, multiples of 8, >= 0; a head's D channels (64 or 128)
+ *             are contiguous.  So x may be a projection's output [B, N, H, D] and y a cache
+ *             [B, H, N_cap, D].  y may be x with the same strides; else the two must not overlap,
+ *             nor rows of y with each other.
+ *   rot_dim   16, 32, .. D;  layout  STC_ROTARY_HALVES or _INTERLEAVED, | STC_ROTARY_INVERSE
+ *   turns     [rot_dim/2] double, in
+ *   amplitude finite; 1 but for methods that raise the logits of long contexts
+ *   pos       [B, N] int32, in: the tokens' positions (any value), or NULL: token n of every
+ *             sequence stands at pos0 + n, which must not pass 2^31 - 1
+ * B <= 65535, N * H < 2^31.
+ */
+int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int32_t layout,
+               const double *turns, float amplitude, const int32_t *pos, int32_t pos0, const void *x,
+               const int64_t *x_stride, void *y, const int64_t *y_stride, void *stream);
+
+/*
+ * The generated token of every sequence, in one launch: its query and key get their rotary positions
+ * (arithmetic of stc_rotary), key and value are appended to the sequence's own uncompressed tail.
+ * Unlike stc_append_tail, sequences may have tails of different lengths, and the lengths lie on the
+ * device, so that a captured graph of the step can be replayed as they grow.
+ *   shape     B, Hq, Hkv, D are used (the rest must be valid)
+ *   q, k_new, v_new  [B, Hq, D], [B, Hkv, D], [B, Hkv, D] bf16, in; element b's heads are contiguous
+ *             and start q_stride (k_stride, v_stride) elements after element b-1's: multiples of 8,
+ *             >= 0 (slices of one fused projection's output)
+ *   q_out     [B, Hq, D] bf16, out; may be q where q_stride is Hq*D
+ *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16: row n_tail[b] of sequence b's streams is written
+ *   n_tail    [B] int32, in.  n_tail[b] < 0: b is padding, nothing of it is read or written.
+ *             n_tail[b] >= tail_cap: no room; nothing of b is written, *dev_status becomes 1
+ *   n_out     [B] int32, out, may be NULL or n_tail itself: n_tail[b] + 1 where a token was appended,
+ *             else n_tail[b]
+ *   rot_dim   0 (no rotation; turns may be NULL), 16, 32, .. D;  layout without STC_ROTARY_INVERSE
+ *   pos       [B] int32, in: the tokens' positions, or NULL: pos0 + n_tail[b], which must not pass
+ *             2^31 - 1 (with pos0 the tokens in front of the tail)
+ *   dev_status int32 on the device, out, may be NULL; the caller zeroes it
+ */
+int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride, const void *k_new,
+                      int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out,
+                      void *K_tail, void *V_tail, const int32_t *n_tail, int32_t *n_out,
+                      int tail_cap, int rot_dim, int layout, const double *turns, float amplitude,
+                      const int32_t *pos, int32_t pos0, int32_t *dev_status, void *stream);
 
 /*
  * Per-query-head page selection and attention: the other reading of Quest under grouped-query

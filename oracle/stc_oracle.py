@@ -435,3 +435,43 @@ def decode_attention_all(q_bits, K_bits, V_bits, mask, page_idx, G, P=16, K_tail
                 mask[b, h], page_idx[b, h], G, P,
                 None if K_tail is None else K_tail[b, h], None if V_tail is None else V_tail[b, h])
     return out
+
+
+def rotary_turns(rot_dim, base, kind="none", factor=1.0, original_len=0, slow=0.0, fast=0.0):
+    """Revolutions per position of the rot_dim/2 pairs (float64): base^(-2j/rot_dim) / (2 pi), and
+    its four ways to longer contexts (positions pressed together; a larger base; slowed by pair
+    index; slowed by rotations over the original length)."""
+    out = np.zeros(rot_dim // 2)
+    if kind == "base":
+        base = base * factor ** (rot_dim / (rot_dim - 2.0))
+    for j in range(rot_dim // 2):
+        f = base ** (-2.0 * j / rot_dim)
+        if kind == "linear":
+            f /= factor
+        elif kind == "channels":
+            # f_j L / (2 pi) = r  <=>  j = rot_dim log(L / (2 pi r)) / (2 log base)
+            at = [rot_dim * np.log(original_len / (2 * np.pi * r)) / (2 * np.log(base))
+                  for r in (fast, slow)]
+            lo, hi = max(np.floor(at[0]), 0.0), min(np.ceil(at[1]), rot_dim - 1.0)
+            w = min(max((j - lo) / max(hi - lo, 1e-3), 0.0), 1.0)
+            f = (1 - w) * f + w * f / factor
+        elif kind == "wavelengths":
+            w = min(max((original_len * f / (2 * np.pi) - slow) / (fast - slow), 0.0), 1.0)
+            f = w * f + (1 - w) * f / factor
+        out[j] = f / (2 * np.pi)
+    return out
+
+
+def rotary(x, pos, turns, rot_dim, interleaved, amplitude=1.0, inverse=False):
+    """x[..., D] float64, pos broadcasts to x's shape without D -> float64: pair j turned by
+    2 pi pos turns[j] (backwards if inverse) and scaled by amplitude; the channels behind rot_dim
+    unchanged."""
+    x = np.asarray(x, dtype=np.float64)
+    whole = np.asarray(pos, dtype=np.float64)[..., None] * np.asarray(turns, dtype=np.float64)
+    angle = 2 * np.pi * (whole - np.floor(whole)) * (-1.0 if inverse else 1.0)
+    first = np.arange(rot_dim // 2) * (2 if interleaved else 1)
+    second = first + (1 if interleaved else rot_dim // 2)
+    y = x.copy()
+    y[..., first] = amplitude * (x[..., first] * np.cos(angle) - x[..., second] * np.sin(angle))
+    y[..., second] = amplitude * (x[..., first] * np.sin(angle) + x[..., second] * np.cos(angle))
+    return y

@@ -22,6 +22,9 @@ STC_WS_ROUTE, STC_WS_SELECT, STC_WS_ATTENTION, STC_WS_ATTENTION_TAIL = 1, 2, 3, 
 STC_WS_SELECT_PER_HEAD, STC_WS_ATTENTION_PER_HEAD, STC_WS_STEP, STC_WS_STEP_TAIL = 5, 6, 7, 8
 STC_ROUTE_MASK, STC_ROUTE_TOPK, STC_ROUTE_GLOBAL = 0, 1, 2
 STC_ROUTE_SHARED = 0x100        # flag: one set of routing inputs per batch element
+STC_ROTARY_HALVES, STC_ROTARY_INTERLEAVED, STC_ROTARY_INVERSE = 0, 1, 0x100
+STC_ROTARY_SCALE_NONE, STC_ROTARY_SCALE_LINEAR, STC_ROTARY_SCALE_BASE = 0, 1, 2
+STC_ROTARY_SCALE_CHANNELS, STC_ROTARY_SCALE_WAVELENGTHS = 3, 4
 
 EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bounds_bytes",
            "stc_build_page_bounds",
@@ -29,7 +32,7 @@ EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bound
            "stc_select_pages_per_head", "stc_decode_attention_per_head", "stc_router_logits",
            "stc_union_pages", "stc_decode_attention_union", "stc_flush_tail",
            "stc_compact_tokens", "stc_decode_step", "stc_decode_step_tail",
-           "stc_decode_step_static"]
+           "stc_decode_step_static", "stc_rotary_turns", "stc_rotary", "stc_rotary_append"]
 
 
 class StcError(RuntimeError):
@@ -48,6 +51,12 @@ class stc_shape_t(ctypes.Structure):
 def make_shape(B, Hq, Hkv, D, N, G, v_cap_groups, P=16, N_cap=0):
     """N_cap: token capacity (stride) of K, mask, tok_off and bounds; 0 = exactly N."""
     return stc_shape_t(B, Hq, Hkv, D, N, P, G, N_cap, v_cap_groups)
+
+
+class stc_rotary_scaling_t(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("original_len", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("slow", ctypes.c_double), ("fast", ctypes.c_double)]
 
 
 _lib = None
@@ -112,6 +121,18 @@ def load_library():
     lib.stc_append_tail.argtypes = [shp, vp, vp, vp, vp, ctypes.c_int, ctypes.c_int, vp]
     lib.stc_router_logits.restype = ctypes.c_int
     lib.stc_router_logits.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.stc_rotary_turns.restype = ctypes.c_int
+    lib.stc_rotary_turns.argtypes = [i32, ctypes.POINTER(stc_rotary_scaling_t),
+                                     ctypes.POINTER(ctypes.c_double)]
+    strides = ctypes.POINTER(i64)
+    lib.stc_rotary.restype = ctypes.c_int
+    lib.stc_rotary.argtypes = [i32, i32, i32, i32, i32, i32, vp, f32, vp, i32, vp, strides, vp,
+                               strides, vp]
+    lib.stc_rotary_append.restype = ctypes.c_int
+    lib.stc_rotary_append.argtypes = [shp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp,
+                                      ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, f32, vp, i32, vp,
+                                      vp]
     lib.stc_compact_tokens.restype = ctypes.c_int
     lib.stc_compact_tokens.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     _lib = lib
@@ -264,6 +285,49 @@ def stc_compact_tokens(src, token_idx, dst, B, Hkv, N_src, n_keep, D, dev_status
                                                dev_status)
 
 
+def stc_rotary_turns(rot_dim, base=10000.0, kind=STC_ROTARY_SCALE_NONE, factor=1.0, original_len=0,
+                     slow=0.0, fast=0.0):
+    """Revolutions per position of the rot_dim/2 pairs: a float64 tensor in host memory, to be
+    copied to the device once."""
+    scaling = stc_rotary_scaling_t(kind, original_len, base, factor, slow, fast)
+    out = (ctypes.c_double * (max(rot_dim, 2) // 2))()
+    status = load_library().stc_rotary_turns(rot_dim, ctypes.byref(scaling), out)
+    if status != STC_OK:
+        raise StcError(status, "stc_rotary_turns")
+    return torch.tensor(list(out), dtype=torch.float64)
+
+
+def stc_rotary(x, y, turns, rot_dim, layout, pos=None, pos0=0, amplitude=1.0, inverse=False):
+    """x, y [B, H, N, D] bf16, any strides that are multiples of 8 (y may be x); turns [rot_dim/2]
+    float64; pos [B, N] int32, or None: token n stands at pos0 + n.  inverse: the rotation's
+    transpose, which is its gradient."""
+    if inverse:
+        layout |= STC_ROTARY_INVERSE
+    (_native or _load_native()).rotary(x, y, turns, rot_dim, layout, pos, pos0, amplitude)
+
+
+def stc_rotary_append(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail, tail_cap, turns, rot_dim,
+                      layout, amplitude=1.0, pos=None, pos0=0, n_out=None, dev_status=None):
+    """q [B, Hq, D], k_new, v_new [B, Hkv, D] (slices of one projection's output will do): rotated q
+    to q_out, rotated k_new and v_new to row n_tail[b] of sequence b's tails.  n_out (n_tail itself
+    will do) receives the tails' new lengths."""
+    (_native or _load_native()).rotary_append(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail,
+                                              tail_cap, turns, rot_dim, layout, amplitude, pos, pos0,
+                                              n_out, dev_status)
+
+
+class Rotary:
+    """A model's rotary positions: the frequencies on the device and how they are applied."""
+
+    def __init__(self, rot_dim, layout=STC_ROTARY_HALVES, amplitude=1.0, device="cuda:0", **scaling):
+        """scaling: base, kind, factor, original_len, slow, fast of stc_rotary_turns."""
+        self.rot_dim, self.layout, self.amplitude = rot_dim, layout, amplitude
+        self.turns = stc_rotary_turns(rot_dim, **scaling).to(device)
+
+    def apply(self, x, y, pos=None, pos0=0, inverse=False):
+        stc_rotary(x, y, self.turns, self.rot_dim, self.layout, pos, pos0, self.amplitude, inverse)
+
+
 class RoutedCache:
     """Device buffers of one layer's compressed cache plus per-step outputs.
 
@@ -337,12 +401,19 @@ class RoutedCache:
             self.page_score = src.view(B, Hkv, self.NP)
 
     def build(self, K, V, logits=None, kcount=None, fixed_k=0, mask_in=None, global_k=None,
-              shared=False):
+              shared=False, rotary=None, pos=None, pos0=0):
         """Cache construction: page bounds of K, routing mask + packed store of V.  The mask
         comes from mask_in, from a global budget of N*global_k token-group pairs per stream,
         or from the per-token top kcount[t] / fixed_k of the logits.  shared: the routing
-        inputs are [B, 1, ...], one set per batch element for all its KV heads."""
-        if self.n_cap:
+        inputs are [B, 1, ...], one set per batch element for all its KV heads.  rotary: K comes
+        without positions, [B, Hkv, N, D] with any strides (a projection's output, transposed), and
+        gets them (pos, pos0 as in stc_rotary) on its way into the cache, which needs its own copy
+        (n_cap)."""
+        if rotary is not None:
+            if not self.n_cap:
+                raise ValueError("keys that get positions need a cache with a copy of its own (n_cap)")
+            rotary.apply(K, self.K[:, :, :self.N], pos, pos0)
+        elif self.n_cap:
             self.K[:, :, :self.N].copy_(K)
         else:
             self.K = K

@@ -15,7 +15,7 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")         # Python's way into 
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 
 SOURCES = ["stc_api.hip", "bounds.hip", "router.hip", "route_pack.hip", "flush.hip",
-           "score.hip", "select.hip", "attention.hip", "step.hip"]
+           "score.hip", "select.hip", "attention.hip", "step.hip", "rotary.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

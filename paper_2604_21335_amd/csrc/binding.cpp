@@ -15,7 +15,7 @@ PyObject* g_any_stream;  // the package's own way, for builds of torch without t
 
 struct PythonError {};  // the interpreter's error is set
 
-constexpr at::ScalarType kBf16 = at::kBFloat16, kF32 = at::kFloat, kU8 = at::kByte;
+constexpr at::ScalarType kBf16 = at::kBFloat16, kF32 = at::kFloat, kU8 = at::kByte, kF64 = at::kDouble;
 
 // The arguments of one call, in order.
 class Args {
@@ -60,6 +60,7 @@ class Args {
       Py_XDECREF(dtype);
       throw PythonError();
     }
+    on_device(name, t);
     bytes_ = (size_t)t.numel() * t.element_size();
     return t.data_ptr();
   }
@@ -72,6 +73,55 @@ class Args {
   void* ws() { return tensor("ws"); }
   size_t bytes() const { return bytes_; }  // of the tensor taken last
 
+  // From here on: the call's tensors lie on one device, the current one.
+  void one_device() { one_device_ = true; }
+
+  void need(bool ok, const char* name, const char* what) {
+    if (ok) return;
+    PyErr_Format(PyExc_ValueError, "%s: %s %s", where_, name, what);
+    throw PythonError();
+  }
+
+  // A contiguous tensor of exactly n elements (None: nullptr).
+  template <class... T>
+  void* sized(const char* name, int64_t n, T... types) {
+    PyObject* o = args_[at_];
+    void* p = tensor(name, types...);
+    if (o != Py_None) need(THPVariable_Unpack(o).numel() == n, name, "has another size");
+    return p;
+  }
+
+  // A bf16 tensor of `dims` dimensions whose last one is contiguous.
+  struct Rows {
+    void* p;
+    int64_t size[4], stride[4];  // stride 0 where there is nothing to step over
+  };
+  Rows rows(const char* name, int dims) {
+    PyObject* o = next();
+    if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) {
+      PyErr_Format(PyExc_TypeError, "%s must be a CUDA tensor", name);
+      throw PythonError();
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    on_device(name, t);
+    if (t.scalar_type() != kBf16) {
+      PyErr_Format(PyExc_TypeError, "%s must be bfloat16", name);
+      throw PythonError();
+    }
+    need(t.dim() == dims, name, "has another number of dimensions");
+    Rows r{t.data_ptr(), {}, {}};
+    for (int i = 0; i < dims; ++i) r.size[i] = t.size(i), r.stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    need(r.size[dims - 1] > 1 && r.stride[dims - 1] == 1, name, "must be contiguous in its last dimension");
+    need(t.numel() > 0 && t.numel() / r.size[dims - 1] <= INT32_MAX, name, "is empty or too large");
+    return r;
+  }
+
+  float real() {
+    const double v = PyFloat_AsDouble(next());
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+    return (float)v;
+  }
+
   // What int() takes; index(): whole numbers only.
   int integer() { return number(PyNumber_Long); }
   int index() { return number(PyNumber_Index); }
@@ -81,6 +131,11 @@ class Args {
     PyObject* s = nullptr;
     if (g_device && g_raw_stream) {
       PyObject* dev = PyObject_CallNoArgs(g_device);
+      if (dev && one_device_ && device_ >= 0 && PyLong_AsLong(dev) != device_) {
+        PyErr_Format(PyExc_ValueError, "%s: the tensors are not on the current device", where_);
+        Py_DECREF(dev);
+        throw PythonError();
+      }
       if (dev) s = PyObject_CallOneArg(g_raw_stream, dev);
       Py_XDECREF(dev);
     } else {
@@ -95,6 +150,11 @@ class Args {
 
  private:
   PyObject* next() { return args_[at_++]; }
+  void on_device(const char* name, const at::Tensor& t) {
+    if (!one_device_) return;
+    if (device_ < 0) device_ = t.get_device();
+    need(t.get_device() == device_, name, "is on another device than the tensors before it");
+  }
   int number(PyObject* (*convert)(PyObject*)) {
     PyObject* o = next();
     PyObject* i = PyLong_CheckExact(o) ? Py_NewRef(o) : convert(o);
@@ -109,6 +169,8 @@ class Args {
   Py_ssize_t at_ = 0;
   stc_shape_t shape_;
   size_t bytes_ = 0;
+  bool one_device_ = false;
+  int device_ = -1;
 };
 
 // Runs `body`, which takes the arguments in order and returns the call to make; the call runs without
@@ -244,6 +306,36 @@ STC_PY(compact_tokens, 9,
   auto D = a.index(); auto status = a.i32("dev_status"); auto st = a.stream();
   return [=] { return stc_compact_tokens(src, idx, dst, B, Hkv, N, keep, D, status, st); };)
 
+STC_PY(rotary, 8,
+  a.one_device(); auto x = a.rows("x", 4); auto y = a.rows("y", 4);
+  for (int i = 0; i < 4; ++i) a.need(x.size[i] == y.size[i], "y", "has another shape than x");
+  auto turns = (double*)a.tensor("turns", kF64); auto nturns = a.bytes() / 8; auto rot = a.integer();
+  a.need(!turns || (int64_t)nturns * 2 == rot, "turns", "must have rot_dim/2 elements");
+  auto layout = a.integer(); auto pos = (int32_t*)a.sized("pos", x.size[0] * x.size[2], at::kInt);
+  auto pos0 = a.integer(); auto amp = a.real(); auto st = a.stream();
+  return [=] { return stc_rotary(x.size[0], x.size[1], x.size[2], x.size[3], rot, layout, turns, amp, pos, pos0, x.p, x.stride, y.p, y.stride, st); };)
+
+STC_PY(rotary_append, 17,
+  auto s = *a.shape(); a.one_device();
+  auto q = a.rows("q", 3); auto k = a.rows("k_new", 3); auto v = a.rows("v_new", 3);
+  const auto heads = [&](const Args::Rows& r, const char* name, int32_t H) {
+    a.need(r.size[0] == s.B && r.size[1] == H && r.size[2] == s.D, name, "has another shape");
+    a.need(H == 1 || r.stride[1] == s.D, name, "must have contiguous heads");
+  };
+  heads(q, "q", s.Hq); heads(k, "k_new", s.Hkv); heads(v, "v_new", s.Hkv);
+  const int64_t streams = (int64_t)s.B * s.Hkv * s.D;
+  auto qo = a.sized("q_out", (int64_t)s.B * s.Hq * s.D, kBf16);
+  auto Kt = a.bf16("K_tail"); auto nk = a.bytes(); auto Vt = a.bf16("V_tail"); auto nv = a.bytes();
+  auto n = (int32_t*)a.sized("n_tail", s.B, at::kInt); auto cap = a.integer();
+  a.need(nk == (size_t)streams * cap * 2 && nv == nk, "K_tail, V_tail", "must be [B, Hkv, tail_cap, D]");
+  auto turns = (double*)a.tensor("turns", kF64); auto nturns = a.bytes() / 8; auto rot = a.integer();
+  a.need(!turns || (int64_t)nturns * 2 == rot, "turns", "must have rot_dim/2 elements");
+  auto layout = a.integer(); auto amp = a.real(); auto pos = (int32_t*)a.sized("pos", s.B, at::kInt);
+  auto pos0 = a.integer(); auto n_out = (int32_t*)a.sized("n_out", s.B, at::kInt);
+  auto status = a.i32("dev_status"); auto st = a.stream();
+  const int64_t qs = s.B > 1 ? q.stride[0] : (int64_t)s.Hq * s.D;
+  return [=] { return stc_rotary_append(&s, q.p, qs, k.p, k.stride[0], v.p, v.stride[0], qo, Kt, Vt, n, n_out, cap, rot, layout, turns, amp, pos, pos0, status, st); };)
+
 PyMethodDef methods[] = {
 #define STC_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
     STC_METHOD(build_page_bounds), STC_METHOD(route_and_pack_values), STC_METHOD(select_pages),
@@ -252,6 +344,7 @@ PyMethodDef methods[] = {
     STC_METHOD(decode_attention_union), STC_METHOD(union_pages), STC_METHOD(decode_step),
     STC_METHOD(decode_step_static), STC_METHOD(decode_step_tail), STC_METHOD(flush_tail),
     STC_METHOD(append_tail), STC_METHOD(router_logits), STC_METHOD(compact_tokens),
+    STC_METHOD(rotary), STC_METHOD(rotary_append),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

@@ -1,4 +1,6 @@
 // C ABI of libstc: argument validation and dispatch to the kernel launchers.
+#include <math.h>
+
 #include "../../include/stc.h"
 #include "stc_kernels.hpp"
 
@@ -29,6 +31,11 @@ int num_pages(const stc_shape_t* s) { return (s->N + s->P - 1) / s->P; }
 size_t select_ws_bytes(const stc_shape_t* s, bool per_head = false) {
   return (size_t)s->B * (per_head ? s->Hq : s->Hkv) * num_pages(s) * sizeof(float);
 }
+
+bool rot_dim_ok(int rot_dim, int D) { return rot_dim >= 16 && rot_dim <= D && rot_dim % 16 == 0; }
+
+// Strides of rows that are read in 16-byte pieces, in bf16 elements.
+bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
 
 // Page scores at the front of the workspace of stc_decode_step, padded so that the attention
 // partials behind them start on a 256-byte boundary.
@@ -438,6 +445,70 @@ int stc_router_logits(int32_t B, int32_t Hkv, int32_t N, int32_t d_model, int32_
     return STC_ERR_ALIGN;
   return stc::launch_router_logits(h, W, bias, bias_per_batch ? G : 0, logits, B, Hkv, N, d_model,
                                    G, (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
+int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t* scaling, double* turns) {
+  if (!scaling || !turns) return STC_ERR_NULL;
+  const stc_rotary_scaling_t& s = *scaling;
+  if (!rot_dim_ok(rot_dim, 128) || !(s.base > 1) || !isfinite(s.base)) return STC_ERR_SHAPE;
+  if (s.kind < STC_ROTARY_SCALE_NONE || s.kind > STC_ROTARY_SCALE_WAVELENGTHS) return STC_ERR_SHAPE;
+  if (s.kind != STC_ROTARY_SCALE_NONE && (!(s.factor > 0) || !isfinite(s.factor)))
+    return STC_ERR_SHAPE;
+  if (s.kind >= STC_ROTARY_SCALE_CHANNELS &&
+      (s.original_len < 1 || !(s.slow > 0) || !(s.fast > s.slow) || !isfinite(s.fast)))
+    return STC_ERR_SHAPE;
+  stc::rotary_turns(rot_dim, s, turns);
+  return STC_OK;
+}
+
+int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int32_t layout,
+               const double* turns, float amplitude, const int32_t* pos, int32_t pos0, const void* x,
+               const int64_t* x_stride, void* y, const int64_t* y_stride, void* stream) {
+  if (!turns || !x || !x_stride || !y || !y_stride) return STC_ERR_NULL;
+  if (B < 1 || B > kMaxGridY || H < 1 || N < 1 || (long long)N * H >= (1ll << 31) ||
+      (D != 64 && D != 128) || !rot_dim_ok(rot_dim, D) || !isfinite(amplitude))
+    return STC_ERR_SHAPE;
+  if ((layout & ~STC_ROTARY_INVERSE) != STC_ROTARY_HALVES &&
+      (layout & ~STC_ROTARY_INVERSE) != STC_ROTARY_INTERLEAVED)
+    return STC_ERR_SHAPE;
+  if (!pos && (long long)pos0 + N - 1 > INT32_MAX) return STC_ERR_SHAPE;
+  if (!aligned16(turns) || !aligned16(x) || !aligned16(y) || (pos && ((uintptr_t)pos & 3)))
+    return STC_ERR_ALIGN;
+  const int32_t sizes[3] = {B, H, N};
+  for (int i = 0; i < 3; ++i) {
+    if (!stride_ok(x_stride[i]) || !stride_ok(y_stride[i])) return STC_ERR_ALIGN;
+    if (sizes[i] > 1 && y_stride[i] < D) return STC_ERR_SHAPE;  // rows of y would overlap
+  }
+  return stc::launch_rotary(B, H, N, D, rot_dim, layout, turns, amplitude, pos, pos0, x, x_stride, y,
+                            y_stride, (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
+int stc_rotary_append(const stc_shape_t* shape, const void* q, int64_t q_stride, const void* k_new,
+                      int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                      void* K_tail, void* V_tail, const int32_t* n_tail, int32_t* n_out,
+                      int tail_cap, int rot_dim, int layout, const double* turns, float amplitude,
+                      const int32_t* pos, int32_t pos0, int32_t* dev_status, void* stream) {
+  if (!shape || !q || !k_new || !v_new || !q_out || !K_tail || !V_tail || !n_tail)
+    return STC_ERR_NULL;
+  if (rot_dim != 0 && !turns) return STC_ERR_NULL;
+  if (!shape_ok(shape) || tail_cap < 1 || (rot_dim != 0 && !rot_dim_ok(rot_dim, shape->D)) ||
+      (layout != STC_ROTARY_HALVES && layout != STC_ROTARY_INTERLEAVED) || !isfinite(amplitude))
+    return STC_ERR_SHAPE;
+  if (!pos && (long long)pos0 + tail_cap - 1 > INT32_MAX) return STC_ERR_SHAPE;
+  // in place only where the rows of a sequence stay where they are
+  if (q_out == q && shape->B > 1 && q_stride != (int64_t)shape->Hq * shape->D) return STC_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) ||
+      !aligned16(K_tail) || !aligned16(V_tail) || (turns && !aligned16(turns)) ||
+      ((uintptr_t)n_tail & 3) || ((uintptr_t)n_out & 3) || ((uintptr_t)pos & 3) ||
+      !stride_ok(q_stride) || !stride_ok(k_stride) || !stride_ok(v_stride))
+    return STC_ERR_ALIGN;
+  return stc::launch_rotary_append(*shape, q, q_stride, k_new, k_stride, v_new, v_stride, q_out,
+                                   K_tail, V_tail, n_tail, n_out, tail_cap, rot_dim, layout, turns,
+                                   amplitude, pos, pos0, dev_status, (hipStream_t)stream)
              ? STC_ERR_LAUNCH
              : STC_OK;
 }

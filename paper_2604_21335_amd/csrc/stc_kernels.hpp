@@ -93,6 +93,17 @@ RouterForm router_form(int B, int N, int d_model, int G);
 int launch_router_logits(const void* h, const void* W, const float* bias, int bias_stride,
                          float* logits, int B, int Hkv, int N, int d_model, int G, hipStream_t st);
 
+void rotary_turns(int rot_dim, const stc_rotary_scaling_t& s, double* turns);
+// Strides of b, h and n in elements, multiples of 8.
+int launch_rotary(int B, int H, int N, int D, int rot_dim, int layout, const double* turns,
+                  float amplitude, const int32_t* pos, int pos0, const void* x, const int64_t* xs,
+                  void* y, const int64_t* ys, hipStream_t st);
+int launch_rotary_append(const stc_shape_t& s, const void* q, int64_t q_stride, const void* k_new,
+                         int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                         void* K_tail, void* V_tail, const int32_t* n_tail, int32_t* n_out,
+                         int tail_cap, int rot_dim, int layout, const double* turns, float amplitude,
+                         const int32_t* pos, int pos0, int32_t* dev_status, hipStream_t st);
+
 int launch_compact(const void* src, const int32_t* token_idx, void* dst, int B, int Hkv, int N_src,
                    int n_keep, int D, int32_t* dev_status, hipStream_t st);
 
