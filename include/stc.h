@@ -26,6 +26,8 @@
  *   rotary positions     stc_rotary (a prompt's queries or keys, with its inverse),
  *                        stc_rotary_append (a generated token: rotation, and its key and value
  *                        into tails of different lengths), stc_rotary_turns (frequencies)
+ *   one prefix for all   stc_decode_attention_shared (a batch over one compressed prefix, with
+ *                        tails of different lengths), stc_shared_workspace_bytes
  *   per-query-head form  stc_select_pages_per_head, stc_decode_attention_per_head,
  *                        stc_union_pages + stc_decode_attention_union (shared K/V reads)
  *   helpers              stc_workspace_bytes, stc_bounds_bytes, stc_status_string, stc_version
@@ -380,6 +382,36 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
                       void *K_tail, void *V_tail, const int32_t *n_tail, int32_t *n_out,
                       int tail_cap, int rot_dim, int layout, const double *turns, float amplitude,
                       const int32_t *pos, int32_t pos0, int32_t *dev_status, void *stream);
+
+/*
+ * Decode attention of a batch whose B sequences share ONE compressed prefix (questions about one
+ * document or image, samples of one prompt): the prefix is held once and read once for all of them.
+ * Every query attends the tokens of the listed pages of the prefix and its own sequence's uncompressed
+ * tail, under one softmax; everything else as stc_decode_attention_tail.
+ *   shape    B sequences; Hq, Hkv, D of the model; N, G, N_cap, v_cap_groups of the one prefix
+ *   q        [B, Hq, D] bf16, in
+ *   K, vpacked, mask, tok_off  the cache of a shape with B = 1, in: [Hkv, Ncap, D], [Hkv,
+ *            v_cap_groups, D/G], [Hkv, Ncap], [Hkv, Ncap+1].  Their sizes are not limited to 4 GiB
+ *   page_idx [Hkv, k_pages] int32, in: pages that all sequences attend; 1 <= k_pages <= NP; entries
+ *            outside [0, NP) are skipped; a page must not be listed twice.  NULL: pages 0 .. k_pages-1
+ *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16, in (may be NULL when tail_cap == 0)
+ *   n_tail   [B] int32 on the device, in: rows 0 .. n_tail[b]-1 of sequence b's tails are attended
+ *            (counted as tail_cap if larger); n_tail[b] < 0: b is padding, its rows of out are left as
+ *            they are.  May be NULL when tail_cap == 0: no tails, no padding
+ *   out      [B, Hq, D], out, float (STC_OUT_F32) or bf16 (STC_OUT_BF16).  A query without any token
+ *            (all listed pages outside the prefix, an empty tail) gets zeros
+ *   ws       stc_shared_workspace_bytes(shape, k_pages, tail_cap) bytes; calls whose work overlaps in
+ *            time need one each
+ * For float output the softmax's weights are carried as two bf16 parts (2^-17), for bf16 output as one
+ * (2^-9, the output's own rounding).  The results depend on the sizes, not on other sequences' lengths.
+ */
+enum { STC_OUT_F32 = 0, STC_OUT_BF16 = 1 };
+size_t stc_shared_workspace_bytes(const stc_shape_t *shape, int k_pages, int tail_cap);
+int stc_decode_attention_shared(const stc_shape_t *shape, const void *q, const void *K,
+                                const void *vpacked, const uint16_t *mask, const uint32_t *tok_off,
+                                const int32_t *page_idx, int k_pages, const void *K_tail,
+                                const void *V_tail, const int32_t *n_tail, int tail_cap, int out_type,
+                                void *out, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Per-query-head page selection and attention: the other reading of Quest under grouped-query

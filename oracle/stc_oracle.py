@@ -475,3 +475,41 @@ def rotary(x, pos, turns, rot_dim, interleaved, amplitude=1.0, inverse=False):
     y[..., first] = amplitude * (x[..., first] * np.cos(angle) - x[..., second] * np.sin(angle))
     y[..., second] = amplitude * (x[..., first] * np.sin(angle) + x[..., second] * np.cos(angle))
     return y
+
+
+def shared_attention_all(q_bits, K_bits, V_bits, mask, page_idx, G, K_tail, V_tail, n_tail, P=16):
+    """B sequences over one prefix.  q_bits[B, Hq, D]; K_bits, V_bits [Hkv, N, D] (dense values),
+    mask[Hkv, N]; page_idx[Hkv, k] (entries outside the prefix are skipped) or None: every page;
+    K_tail, V_tail [B, Hkv, cap, D], of which sequence b attends rows 0 .. n_tail[b]-1 (at most
+    cap).  -> (out[B, Hq, D], size[B, Hq, D], top) float64: softmax-weighted sums of the values and
+    of their magnitudes, and the largest sum of magnitudes behind a logit (base e).  A query
+    without tokens gets zeros."""
+    q = bf16_to_f32(q_bits).astype(np.float64)
+    B, Hq, D = q.shape
+    Hkv, N, _ = K_bits.shape
+    R = Hq // Hkv
+    out, size, top = np.zeros(q.shape), np.zeros(q.shape), 0.0
+    for h in range(Hkv):
+        pages = range((N + P - 1) // P) if page_idx is None else page_idx[h]
+        on = np.zeros(N, dtype=bool)
+        for p in pages:
+            if 0 <= p < (N + P - 1) // P:
+                on[p * P:(p + 1) * P] = True
+        K = bf16_to_f32(K_bits[h][on]).astype(np.float64)
+        keep = (np.asarray(mask[h][on]).astype(np.int64)[:, None] >> np.arange(G)) & 1
+        V = bf16_to_f32(V_bits[h][on]).astype(np.float64) * np.repeat(keep, D // G, axis=1)
+        for b in range(B):
+            n = int(min(max(n_tail[b], 0), K_tail.shape[2])) if K_tail is not None else 0
+            Kb, Vb = K, V
+            if n:
+                Kb = np.concatenate([K, bf16_to_f32(K_tail[b, h, :n]).astype(np.float64)])
+                Vb = np.concatenate([V, bf16_to_f32(V_tail[b, h, :n]).astype(np.float64)])
+            if not len(Kb):
+                continue
+            for j in range(h * R, (h + 1) * R):
+                s = Kb @ q[b, j] / math.sqrt(D)
+                top = max(top, float((np.abs(Kb) @ np.abs(q[b, j])).max() / math.sqrt(D)))
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out[b, j], size[b, j] = w @ Vb, w @ np.abs(Vb)
+    return out, size, top

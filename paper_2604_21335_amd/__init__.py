@@ -22,6 +22,7 @@ STC_WS_ROUTE, STC_WS_SELECT, STC_WS_ATTENTION, STC_WS_ATTENTION_TAIL = 1, 2, 3, 
 STC_WS_SELECT_PER_HEAD, STC_WS_ATTENTION_PER_HEAD, STC_WS_STEP, STC_WS_STEP_TAIL = 5, 6, 7, 8
 STC_ROUTE_MASK, STC_ROUTE_TOPK, STC_ROUTE_GLOBAL = 0, 1, 2
 STC_ROUTE_SHARED = 0x100        # flag: one set of routing inputs per batch element
+STC_OUT_F32, STC_OUT_BF16 = 0, 1
 STC_ROTARY_HALVES, STC_ROTARY_INTERLEAVED, STC_ROTARY_INVERSE = 0, 1, 0x100
 STC_ROTARY_SCALE_NONE, STC_ROTARY_SCALE_LINEAR, STC_ROTARY_SCALE_BASE = 0, 1, 2
 STC_ROTARY_SCALE_CHANNELS, STC_ROTARY_SCALE_WAVELENGTHS = 3, 4
@@ -32,7 +33,8 @@ EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bound
            "stc_select_pages_per_head", "stc_decode_attention_per_head", "stc_router_logits",
            "stc_union_pages", "stc_decode_attention_union", "stc_flush_tail",
            "stc_compact_tokens", "stc_decode_step", "stc_decode_step_tail",
-           "stc_decode_step_static", "stc_rotary_turns", "stc_rotary", "stc_rotary_append"]
+           "stc_decode_step_static", "stc_rotary_turns", "stc_rotary", "stc_rotary_append",
+           "stc_shared_workspace_bytes", "stc_decode_attention_shared"]
 
 
 class StcError(RuntimeError):
@@ -133,6 +135,11 @@ def load_library():
     lib.stc_rotary_append.argtypes = [shp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp,
                                       ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, f32, vp, i32, vp,
                                       vp]
+    lib.stc_shared_workspace_bytes.restype = sz
+    lib.stc_shared_workspace_bytes.argtypes = [shp, ctypes.c_int, ctypes.c_int]
+    lib.stc_decode_attention_shared.restype = ctypes.c_int
+    lib.stc_decode_attention_shared.argtypes = [shp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp, vp,
+                                                ctypes.c_int, ctypes.c_int, vp, vp, sz, vp]
     lib.stc_compact_tokens.restype = ctypes.c_int
     lib.stc_compact_tokens.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     _lib = lib
@@ -316,6 +323,19 @@ def stc_rotary_append(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail, tai
                                               n_out, dev_status)
 
 
+def stc_shared_workspace_bytes(shape, k_pages, tail_cap):
+    return int(load_library().stc_shared_workspace_bytes(ctypes.byref(shape), k_pages, tail_cap))
+
+
+def stc_decode_attention_shared(shape, q, K, vpacked, mask, tok_off, page_idx, k_pages, K_tail, V_tail,
+                                n_tail, tail_cap, out, ws):
+    """B sequences over one prefix (K, vpacked, mask, tok_off of a cache with B = 1), each with its own
+    tail of n_tail[b] tokens; out [B, Hq, D] float32 or bfloat16."""
+    (_native or _load_native()).decode_attention_shared(shape, q, K, vpacked, mask, tok_off, page_idx,
+                                                        k_pages, K_tail, V_tail, n_tail, tail_cap, out,
+                                                        ws)
+
+
 class Rotary:
     """A model's rotary positions: the frequencies on the device and how they are applied."""
 
@@ -485,3 +505,49 @@ class RoutedCache:
             self.select(q)
         self.attend(q)
         return self.out
+
+
+class SharedPrefix:
+    """B sequences that continue one prefix: a RoutedCache with B = 1 that holds the prefix, and the
+    sequences' own uncompressed tails, per-step outputs and workspace.  As in RoutedCache, allocation
+    and nothing else; the lengths of the tails lie on the device (n_tail; a negative one marks an
+    element of the batch as padding), so that a step can be captured and replayed."""
+
+    def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32):
+        """rotary: positions for the queries and keys given to append()."""
+        if prefix.B != 1:
+            raise ValueError("the prefix is a cache of one batch element")
+        self.prefix, self.B, self.tail_cap, self.rotary = prefix, B, tail_cap, rotary
+        p, dev = prefix, prefix.device
+        self.shape = make_shape(B, p.Hq, p.Hkv, p.D, p.N, p.G, p.shape.v_cap_groups, N_cap=p.n_cap)
+        self.n_tail = torch.zeros(B, dtype=torch.int32, device=dev)
+        self.K_tail = torch.empty(B, p.Hkv, tail_cap, p.D, dtype=torch.bfloat16, device=dev)
+        self.V_tail = torch.empty_like(self.K_tail)
+        self.q = torch.zeros(B, p.Hq, p.D, dtype=torch.bfloat16, device=dev)
+        self.out = torch.zeros(B, p.Hq, p.D, dtype=out_dtype, device=dev)
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=dev)
+        # the workspace covers every choice of pages
+        need = max(stc_shared_workspace_bytes(self.shape, k, tail_cap) for k in range(1, p.NP + 1))
+        self._ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+
+    def append(self, q, k_new, v_new):
+        """The new token of every sequence: q [B, Hq, D], k_new, v_new [B, Hkv, D] (without positions
+        where rotary is given).  Key and value go to the tails; returns the queries for attend()."""
+        r = self.rotary
+        stc_rotary_append(self.shape, q, k_new, v_new, self.q, self.K_tail, self.V_tail, self.n_tail,
+                          self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
+                          r.layout if r else STC_ROTARY_HALVES, amplitude=r.amplitude if r else 1.0,
+                          pos0=self.prefix.N, n_out=self.n_tail, dev_status=self.dev_status)
+        return self.q
+
+    def attend(self, q, page_idx=None):
+        """page_idx [Hkv, k]: the pages of the prefix to attend; None: all of it."""
+        p = self.prefix
+        k = p.NP if page_idx is None else page_idx.shape[-1]
+        stc_decode_attention_shared(self.shape, q, p.K, p.vpacked, p.mask, p.tok_off, page_idx, k,
+                                    self.K_tail, self.V_tail, self.n_tail, self.tail_cap, self.out,
+                                    self._ws)
+        return self.out
+
+    def step(self, q, k_new, v_new, page_idx=None):
+        return self.attend(self.append(q, k_new, v_new), page_idx)

@@ -15,7 +15,8 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")         # Python's way into 
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 
 SOURCES = ["stc_api.hip", "bounds.hip", "router.hip", "route_pack.hip", "flush.hip",
-           "score.hip", "select.hip", "attention.hip", "step.hip", "rotary.hip"]
+           "score.hip", "select.hip", "attention.hip", "step.hip", "rotary.hip",
+           "shared.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
@@ -30,7 +31,7 @@ HIPCC_FLAGS = [
 # ordinary vector registers (no copies out of the accumulation registers)
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 FILE_FLAGS = {"score.hip": _VGPR_MFMA, "attention.hip": _VGPR_MFMA, "step.hip": _VGPR_MFMA,
-              "router.hip": _VGPR_MFMA}
+              "router.hip": _VGPR_MFMA, "shared.hip": _VGPR_MFMA}
 
 
 def _hipcc():

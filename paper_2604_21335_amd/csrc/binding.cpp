@@ -336,6 +336,25 @@ STC_PY(rotary_append, 17,
   const int64_t qs = s.B > 1 ? q.stride[0] : (int64_t)s.Hq * s.D;
   return [=] { return stc_rotary_append(&s, q.p, qs, k.p, k.stride[0], v.p, v.stride[0], qo, Kt, Vt, n, n_out, cap, rot, layout, turns, amp, pos, pos0, status, st); };)
 
+STC_PY(decode_attention_shared, 14,
+  auto s = *a.shape(); a.one_device();
+  const int64_t Nc = s.N_cap ? s.N_cap : s.N; const int64_t gd = s.G > 0 ? s.D / s.G : 0;
+  const int64_t n_q = (int64_t)s.B * s.Hq * s.D;
+  auto q = a.sized("q", n_q, kBf16); auto K = a.sized("K", s.Hkv * Nc * s.D, kBf16);
+  auto v = a.sized("vpacked", s.Hkv * s.v_cap_groups * gd, kBf16);
+  auto mask = (uint16_t*)a.sized("mask", s.Hkv * Nc, at::kShort, at::kUInt16);
+  auto off = (uint32_t*)a.sized("tok_off", s.Hkv * (Nc + 1), at::kInt, at::kUInt32);
+  auto idx = a.i32("page_idx"); auto nidx = a.bytes() / 4; auto k = a.integer();
+  a.need(!idx || (int64_t)nidx == (int64_t)s.Hkv * k, "page_idx", "must be [Hkv, k_pages]");
+  auto Kt = a.bf16("K_tail"); auto nk = a.bytes(); auto Vt = a.bf16("V_tail"); auto nv = a.bytes();
+  auto n = (int32_t*)a.sized("n_tail", s.B, at::kInt); auto cap = a.integer();
+  const size_t tails = cap > 0 ? (size_t)s.B * s.Hkv * cap * s.D * 2 : 0;
+  a.need(cap <= 0 || ((!Kt || nk == tails) && (!Vt || nv == tails)), "K_tail, V_tail", "must be [B, Hkv, tail_cap, D]");
+  auto out = a.sized("out", n_q, kF32, kBf16);
+  auto type = out && a.bytes() == (size_t)n_q * 2 ? STC_OUT_BF16 : STC_OUT_F32;
+  auto ws = a.ws(); auto nws = a.bytes(); auto st = a.stream();
+  return [=] { return stc_decode_attention_shared(&s, q, K, v, mask, off, idx, k, Kt, Vt, n, cap, type, out, ws, nws, st); };)
+
 PyMethodDef methods[] = {
 #define STC_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
     STC_METHOD(build_page_bounds), STC_METHOD(route_and_pack_values), STC_METHOD(select_pages),
@@ -344,7 +363,7 @@ PyMethodDef methods[] = {
     STC_METHOD(decode_attention_union), STC_METHOD(union_pages), STC_METHOD(decode_step),
     STC_METHOD(decode_step_static), STC_METHOD(decode_step_tail), STC_METHOD(flush_tail),
     STC_METHOD(append_tail), STC_METHOD(router_logits), STC_METHOD(compact_tokens),
-    STC_METHOD(rotary), STC_METHOD(rotary_append),
+    STC_METHOD(rotary), STC_METHOD(rotary_append), STC_METHOD(decode_attention_shared),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

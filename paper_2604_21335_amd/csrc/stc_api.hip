@@ -449,6 +449,39 @@ int stc_router_logits(int32_t B, int32_t Hkv, int32_t N, int32_t d_model, int32_
              : STC_OK;
 }
 
+namespace {
+bool shared_ok(const stc_shape_t* s, int k_pages, int tail_cap) {
+  return shape_ok(s) && k_pages >= 1 && k_pages <= num_pages(s) && tail_cap >= 0 &&
+         tail_cap <= (1 << 30) && s->v_cap_groups >= 1;
+}
+}  // namespace
+
+size_t stc_shared_workspace_bytes(const stc_shape_t* shape, int k_pages, int tail_cap) {
+  if (!shape || !shared_ok(shape, k_pages, tail_cap)) return 0;
+  return stc::shared_ws_bytes(*shape, k_pages, tail_cap);
+}
+
+int stc_decode_attention_shared(const stc_shape_t* shape, const void* q, const void* K,
+                                const void* vpacked, const uint16_t* mask, const uint32_t* tok_off,
+                                const int32_t* page_idx, int k_pages, const void* K_tail,
+                                const void* V_tail, const int32_t* n_tail, int tail_cap, int out_type,
+                                void* out, void* ws, size_t ws_bytes, void* stream) {
+  if (!shape || !q || !K || !vpacked || !mask || !tok_off || !out) return STC_ERR_NULL;
+  if (!shared_ok(shape, k_pages, tail_cap) || (out_type != STC_OUT_F32 && out_type != STC_OUT_BF16))
+    return STC_ERR_SHAPE;
+  if (tail_cap > 0 && (!K_tail || !V_tail || !n_tail)) return STC_ERR_NULL;
+  if (!aligned16(q) || !aligned16(K) || !aligned16(vpacked) || !aligned16(mask) ||
+      !aligned16(tok_off) || (page_idx && !aligned16(page_idx)) || !aligned16(out) ||
+      ((uintptr_t)n_tail & 3) || (tail_cap > 0 && (!aligned16(K_tail) || !aligned16(V_tail))))
+    return STC_ERR_ALIGN;
+  const size_t need = stc::shared_ws_bytes(*shape, k_pages, tail_cap);
+  if (need && (!ws || ws_bytes < need || !aligned16(ws))) return STC_ERR_WORKSPACE;
+  return stc::launch_shared(*shape, q, K, vpacked, mask, tok_off, page_idx, k_pages, K_tail, V_tail,
+                            n_tail, tail_cap, out_type == STC_OUT_BF16, out, ws, (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
 int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t* scaling, double* turns) {
   if (!scaling || !turns) return STC_ERR_NULL;
   const stc_rotary_scaling_t& s = *scaling;

@@ -104,6 +104,12 @@ int launch_rotary_append(const stc_shape_t& s, const void* q, int64_t q_stride, 
                          int tail_cap, int rot_dim, int layout, const double* turns, float amplitude,
                          const int32_t* pos, int pos0, int32_t* dev_status, hipStream_t st);
 
+size_t shared_ws_bytes(const stc_shape_t& s, int k_pages, int tail_cap);
+int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void* vpacked,
+                  const uint16_t* mask, const uint32_t* tok_off, const int32_t* page_idx, int k_pages,
+                  const void* K_tail, const void* V_tail, const int32_t* n_tail, int tail_cap,
+                  bool out_bf16, void* out, void* ws, hipStream_t st);
+
 int launch_compact(const void* src, const int32_t* token_idx, void* dst, int B, int Hkv, int N_src,
                    int n_keep, int D, int32_t* dev_status, hipStream_t st);
 

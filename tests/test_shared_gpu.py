@@ -1,0 +1,401 @@
+"""Decode attention of a batch over one shared prefix, against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_21335_amd as stc
+from oracle import stc_oracle as O
+from tests import parity as PT
+from tests.helpers import bits_to_f64, randn_bf16
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def limits(want, size, top, tokens, D, dtype):
+    """How far an output may be off, from the arithmetic.  e: relative error of a weight.  Two bf16
+    parts leave 2^-16 of it, one leaves 2^-8 (half a step of the last part, relative); the exponent is
+    a float dot product of D terms, scaled and shifted in base 2, off by at most (D + 4) 2^-24 of the
+    sum of magnitudes behind it, which shifts the weight by as much; the exponential itself by 2^-22.
+    Weighted sum and sum of weights each carry e and the roundings of at most `tokens` additions."""
+    e = (2.0 ** -16 if dtype == F32 else 2.0 ** -8) + (D + 4) * 2.0 ** -24 * max(top, 1.0) + 2.0 ** -22
+    lim = (2 * e + (tokens + 64) * 2.0 ** -24) * size
+    return lim + (2.0 ** -8 * (np.abs(want) + lim) if dtype == BF16 else 0) + 1e-30
+
+
+class Case:
+    """Host arrays of a prefix and B tails, and their device copies; everything that must not be read
+    holds NaN."""
+
+    def __init__(self, B, Hq, Hkv, D, N, G, cap, seed=0, n_tail=None, n_cap=0, scale=1.0, keep=None,
+                 v_cap=None):
+        rng = np.random.default_rng(seed)
+        self.B, self.Hq, self.Hkv, self.D, self.N, self.G, self.cap = B, Hq, Hkv, D, N, G, cap
+        self.q = randn_bf16(rng, (B, Hq, D), scale)
+        self.K, self.V = randn_bf16(rng, (Hkv, N, D)), randn_bf16(rng, (Hkv, N, D))
+        self.mask = rng.integers(0, 1 << G, size=(Hkv, N)).astype(np.uint16)
+        if keep is not None:
+            self.mask[:] = keep
+        self.Kt, self.Vt = (randn_bf16(rng, (B, Hkv, max(cap, 1), D)) for _ in range(2))
+        self.n = rng.integers(0, cap + 1, size=B) if n_tail is None else np.resize(n_tail, B)
+        self.n = self.n.astype(np.int32)
+        Nc = n_cap or N
+        off = np.zeros((Hkv, Nc + 1), dtype=np.uint32)
+        kept = ((self.mask[..., None].astype(np.int64) >> np.arange(G)) & 1).sum(-1)
+        off[:, 1:N + 1] = kept.cumsum(1)
+        off[:, N + 1:] = 0xFFFFFFF0                  # past the end: never used
+        self.v_cap = v_cap or max(int(off[:, N].max()), 1) + 3
+        v = np.full((Hkv, self.v_cap, D // G), 0x7FC0, dtype=np.uint16)
+        for h in range(Hkv):
+            packed = O.pack_values(self.V[h], self.mask[h], off[h, :N + 1], G)[:self.v_cap]
+            v[h, :len(packed)] = packed
+        K = np.full((Hkv, Nc, D), 0x7FC0, dtype=np.uint16)
+        K[:, :N] = self.K
+        m = np.full((Hkv, Nc), 0xFFFF, dtype=np.uint16)
+        m[:, :N] = self.mask
+        Kt, Vt = self.Kt.copy(), self.Vt.copy()
+        for b in range(B):
+            Kt[b, :, max(self.n[b], 0):] = 0x7FC0
+            Vt[b, :, max(self.n[b], 0):] = 0x7FC0
+        self.d = dict(q=PT.to_dev_bf16(self.q), K=PT.to_dev_bf16(K), v=PT.to_dev_bf16(v),
+                      mask=PT.to_dev_u16(m), off=torch.from_numpy(off.view(np.int32)).to(DEV),
+                      Kt=PT.to_dev_bf16(Kt) if cap else None, Vt=PT.to_dev_bf16(Vt) if cap else None,
+                      n=torch.from_numpy(self.n).to(DEV))
+        self.shape = stc.make_shape(B, Hq, Hkv, D, N, G, self.v_cap, N_cap=n_cap)
+
+    def run(self, dtype=F32, pages=None, out=None, k=None, **other):
+        d = dict(self.d, **other)
+        k = k or ((self.N + 15) // 16 if pages is None else pages.shape[1])
+        need = stc.stc_shared_workspace_bytes(self.shape, k, self.cap)
+        ws = torch.full((need + 16,), 0xFF, dtype=torch.uint8, device=DEV)       # NaN
+        if out is None:
+            out = torch.full((self.B, self.Hq, self.D), float("nan"), dtype=dtype, device=DEV)
+        p = None if pages is None else torch.from_numpy(pages.astype(np.int32)).to(DEV)
+        stc.stc_decode_attention_shared(self.shape, d["q"], d["K"], d["v"], d["mask"], d["off"], p, k,
+                                        d["Kt"], d["Vt"], d["n"], self.cap, out, ws[:need])
+        torch.cuda.synchronize()
+        assert (ws[need:] == 0xFF).all()
+        return out
+
+    def check(self, dtype=F32, pages=None, k=None):
+        got = self.run(dtype, pages, k=k).double().cpu().numpy()
+        listed = pages if pages is not None or k is None else np.tile(np.arange(k), (self.Hkv, 1))
+        want, size, top = O.shared_attention_all(self.q, self.K, self.V, self.mask, listed, self.G,
+                                                 self.Kt if self.cap else None, self.Vt, self.n)
+        on = self.n >= 0
+        lim = limits(want, size, top, self.N + self.cap, self.D, dtype)
+        bad = ~(np.abs(got - want) <= lim) & on[:, None, None]
+        assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], lim[bad][:4])
+        # errors of different weights are independent, so the whole is far closer than the worst case
+        off = np.linalg.norm((got - want)[on]) / max(np.linalg.norm(want[on]), 1e-30)
+        assert off <= (1e-5 if dtype == F32 else 2.0 ** -8) * max(1.0, top / 50), off
+        return got
+
+
+# rows of a KV head on both sides of every change of the form (32, 64, 128 of them), partly filled
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,G", [(128, 8), (64, 4)])
+@pytest.mark.parametrize("B,R,Hkv", [(1, 1, 1), (3, 5, 2), (2, 16, 1), (33, 1, 2), (4, 16, 2), (13, 5, 1),
+                                     (16, 7, 2), (128, 1, 1), (43, 3, 2), (19, 16, 1)])
+def test_rows(B, R, Hkv, D, G, dtype):
+    Case(B, R * Hkv, Hkv, D, 200, G, 40, seed=B + R).check(dtype)
+
+
+# tokens that end inside a page, a tile, a group's turn, a split
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,Hq,Hkv,D", [(2, 4, 2, 128), (9, 10, 2, 64), (40, 5, 1, 128)])
+@pytest.mark.parametrize("N", [1, 15, 16, 17, 31, 32, 33, 63, 65, 127, 128, 129, 255, 257, 1000, 4001])
+def test_lengths_of_the_prefix(N, B, Hq, Hkv, D, dtype):
+    Case(B, Hq, Hkv, D, N, 8, 5, seed=N).check(dtype)
+
+
+@pytest.mark.parametrize("D,Hkv,R,B", [(128, 2, 4, 8), (64, 1, 16, 11), (128, 3, 1, 70)])
+@pytest.mark.parametrize("cap", [0, 1, 2, 31, 33, 128, 129, 700])
+def test_lengths_of_the_tails(cap, D, Hkv, R, B):
+    n = [0, cap, 1, cap // 2, cap - 1, 2 * cap + 5, -1, 31, 32, 33, 127, 128, 129]
+    Case(B, R * Hkv, Hkv, D, 50, 4, cap, seed=cap, n_tail=np.minimum(n, cap + 7)).check()
+
+
+@pytest.mark.parametrize("G,D", [(1, 64), (1, 128), (2, 64), (8, 64), (16, 128), (4, 128)])
+@pytest.mark.parametrize("B", [2, 50])
+def test_value_groups(G, D, B):
+    Case(B, 4, 2, D, 150, G, 9, seed=G).check()
+
+
+@pytest.mark.parametrize("keep", [0, 0xFF, 1, 0x80])
+def test_tokens_that_keep_nothing_or_all(keep):
+    got = Case(5, 4, 2, 128, 90, 8, 0, keep=keep).check()
+    if keep == 0:
+        assert (got == 0).all()
+
+
+def test_values_behind_the_capacity_count_as_dropped():
+    c = Case(6, 4, 2, 128, 90, 8, 4, keep=0xFF, v_cap=300)
+    c.mask[:, 37] = 0x0F                                       # 300 slots: tokens 0 .. 36, half of 37
+    c.mask[:, 38:] = 0
+    c.check()
+
+
+@pytest.mark.parametrize("B", [2, 30, 40])
+@pytest.mark.parametrize("D", [64, 128])
+def test_page_lists(B, D):
+    """Pages in any order, the ragged last one among them, entries outside the prefix skipped."""
+    rng = np.random.default_rng(B)
+    c = Case(B, 6, 2, D, 1000 - 5, 4, 20, n_cap=1040, seed=B)
+    for k in (1, 2, 5, 63):
+        pages = np.stack([rng.permutation(63)[:k] for _ in range(2)])
+        c.check(pages=pages)
+        pages[0, 0], pages[1, -1] = -1, 63
+        if k > 2:
+            pages[1, 1] = 2**31 - 1
+            pages[0, 2] = -2**31
+        c.check(pages=pages)
+    c.check(k=7)                                               # no list: the first pages
+
+
+def test_nothing_to_attend_gives_zeros():
+    c = Case(4, 4, 2, 64, 40, 4, 6, n_tail=[0, 2, 0, -1])
+    out = torch.full((4, 4, 64), 3.0, device=DEV)
+    pages = np.full((2, 2), -1)
+    c.run(pages=pages, out=out)
+    assert (out[0] == 0).all() and (out[2] == 0).all() and (out[3] == 3).all()
+    assert c.check(pages=pages)[1].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_padding_is_left_as_it_was(dtype):
+    c = Case(70, 4, 2, 128, 100, 8, 12, n_tail=[3, -1, 0, -2**31, 12])
+    out = torch.full((70, 4, 128), 3.0, dtype=dtype, device=DEV)
+    c.run(dtype, out=out)
+    on = torch.from_numpy(c.n >= 0)
+    assert (out[~on] == 3).all() and not (out[on] == 3).all(-1).any()
+    # lengths may be given without tails, to mark padding
+    c = Case(5, 4, 2, 128, 100, 8, 0, n_tail=[0, -1, 0, -1, 0])
+    out = torch.full((5, 4, 128), 3.0, device=DEV)
+    c.run(out=out)
+    assert (out[[1, 3]] == 3).all() and not (out[[0, 2, 4]] == 3).all(-1).any()
+    every = c.run(n=None)
+    assert torch.equal(every[[0, 2, 4]], out[[0, 2, 4]]) and not every.isnan().any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B", [3, 40])
+def test_large_and_ordered_scores(B, dtype):
+    """Weights on one token, maxima that grow from tile to tile or fall, and by less than what moves
+    the running maximum."""
+    Case(B, 4, 2, 128, 300, 8, 30, scale=60.0).check(dtype)
+    for slope in (-1.0, -0.01, 0.01, 1.0):
+        c = Case(B, 4, 2, 128, 300, 8, 30)
+        ramp = np.linspace(-150 * slope, 150 * slope, 300)
+        K = bits_to_f64(c.K)
+        K[..., 0] = ramp
+        q = bits_to_f64(c.q)
+        q[..., 0] = 11.0
+        from tests.helpers import f32_to_bf16_bits
+        c.K, c.q = f32_to_bf16_bits(K), f32_to_bf16_bits(q)
+        c.d["K"], c.d["q"] = PT.to_dev_bf16(c.K), PT.to_dev_bf16(c.q)
+        c.check(dtype)
+
+
+def test_a_sequence_does_not_depend_on_the_others():
+    c = Case(40, 7, 1, 128, 500, 8, 50, seed=3)
+    a = c.run()
+    order = torch.from_numpy(np.random.default_rng(0).permutation(40)).to(DEV)
+    q, Kt, Vt, n = (c.d[x][order].contiguous() for x in ("q", "Kt", "Vt", "n"))
+    b = c.run(q=q, Kt=Kt, Vt=Vt, n=n)
+    assert torch.equal(a[order], b)
+    q[1:] *= 30
+    n[1:] = 0
+    assert torch.equal(c.run(q=q, Kt=Kt, Vt=Vt, n=n)[0], b[0])
+    assert torch.equal(c.run(), a)
+
+
+def test_agrees_with_a_cache_for_every_sequence():
+    """stc_decode_attention_tail over copies of the prefix, tails of one length."""
+    B, Hq, Hkv, D, N, G, n = 6, 8, 2, 128, 333, 8, 21
+    c = Case(B, Hq, Hkv, D, N, G, n, n_tail=[n])
+    s = stc.make_shape(B, Hq, Hkv, D, N, G, c.v_cap)
+    rep = lambda t: t[None].expand(B, *t.shape).contiguous()  # noqa: E731
+    NP = (N + 15) // 16
+    ws = torch.empty(max(16, stc.stc_workspace_bytes(s, stc.STC_WS_ATTENTION_TAIL, NP + 2)),
+                     dtype=torch.uint8, device=DEV)
+    out = torch.empty(B, Hq, D, device=DEV)
+    stc.stc_decode_attention_tail(s, c.d["q"], rep(c.d["K"]), rep(c.d["v"]), rep(c.d["mask"]),
+                                  rep(c.d["off"]), None, NP, c.d["Kt"], c.d["Vt"], n, n, out, ws)
+    # either is within 2e-5 of the sums on such data
+    assert (c.run() - out).abs().max() <= 4e-5
+
+
+def test_offsets_that_pass_32_bits():
+    """A prefix whose keys and values pass 4 GiB, attended at both ends; tails too."""
+    N, D = (1 << 32) // 256 + 4096, 128
+    K = torch.zeros(1, N, D, dtype=BF16, device=DEV)
+    v = torch.zeros(1, N, D, dtype=BF16, device=DEV)
+    mask = torch.ones(1, N, dtype=torch.int16, device=DEV)
+    off = torch.arange(N + 1, dtype=torch.int32, device=DEV)[None]
+    NP = N // 16
+    pages = [0, 1, NP - 3, NP - 1, NP // 2]
+    rng = np.random.default_rng(4)
+    small = Case(40, 2, 1, D, 80, 1, 0, keep=1, n_tail=[0])
+    for i, p in enumerate(pages):
+        K[0, p * 16:p * 16 + 16] = small.d["K"][0, i * 16:i * 16 + 16]
+        v[0, p * 16:p * 16 + 16] = small.d["v"][0, i * 16:i * 16 + 16]
+    s = stc.make_shape(40, 2, 1, D, N, 1, N)
+    idx = torch.tensor([pages], dtype=torch.int32, device=DEV)
+    want, size, top = O.shared_attention_all(small.q, small.K, small.V, small.mask, None, 1, None, None,
+                                             small.n)
+    for B in (40, 3):                                   # both forms
+        s.B = B
+        ws = torch.empty(stc.stc_shared_workspace_bytes(s, 5, 0) + 16, dtype=torch.uint8, device=DEV)
+        out = torch.empty(B, 2, D, device=DEV)
+        stc.stc_decode_attention_shared(s, small.d["q"][:B].contiguous(), K, v, mask, off, idx, 5, None, None,
+                                        None, 0, out, ws)
+        got = out.double().cpu().numpy()
+        assert (np.abs(got - want[:B]) <= limits(want, size, top, 80, D, F32)[:B]).all()
+    # the last tail of a batch starts behind 4 GiB of others
+    cap = 1 << 19
+    Kt = torch.zeros(34, 1, cap, D, dtype=BF16, device=DEV)
+    Vt = torch.zeros(34, 1, cap, D, dtype=BF16, device=DEV)
+    n = torch.zeros(34, dtype=torch.int32, device=DEV)
+    tail = randn_bf16(rng, (1, 1, 50, D))
+    Kt[33, 0, :50] = Vt[33, 0, :50] = PT.to_dev_bf16(tail)[0, 0]
+    n[33] = 50
+    c = Case(34, 2, 1, D, 20, 1, 0, keep=1)
+    s = stc.make_shape(34, 2, 1, D, 20, 1, c.v_cap)
+    ws = torch.empty(stc.stc_shared_workspace_bytes(s, 2, cap) + 16, dtype=torch.uint8, device=DEV)
+    out = torch.empty(34, 2, D, device=DEV)
+    stc.stc_decode_attention_shared(s, c.d["q"], c.d["K"], c.d["v"], c.d["mask"], c.d["off"], None, 2, Kt, Vt,
+                                    n, cap, out, ws)
+    tails = np.repeat(tail, 34, axis=0)
+    want, size, top = O.shared_attention_all(c.q, c.K, c.V, c.mask, None, 1, tails, tails, [0] * 33 + [50])
+    assert (np.abs(out.double().cpu().numpy() - want) <= limits(want, size, top, 70, D, F32)).all()
+
+
+def _prefix(N=200, k_pages=16, Hq=8, Hkv=2, D=128, G=8, rotary=None, n_cap=0):
+    g = torch.Generator(device=DEV).manual_seed(11)
+    c = stc.RoutedCache(1, Hq, Hkv, D, N, G, k_pages, device=DEV, n_cap=n_cap)
+    K = torch.randn(1, Hkv, N, D, device=DEV, generator=g).bfloat16()
+    V = torch.randn(1, Hkv, N, D, device=DEV, generator=g).bfloat16()
+    m = torch.randint(0, 1 << G, (1, Hkv, N), device=DEV, generator=g).to(torch.int16)
+    c.build(K, V, mask_in=m, rotary=rotary)
+    return c, K, V, m
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B", [3, 20])
+def test_a_run_of_steps(B, dtype):
+    """Construction with rotary keys, then tokens appended and attended, against the oracle on the
+    positions, keys and values themselves; a padded element; tails that differ and fill up."""
+    N, Hq, Hkv, D, G, cap, steps = 200, 8, 2, 128, 8, 12, 9
+    rot = stc.Rotary(64, stc.STC_ROTARY_INTERLEAVED, base=1e5, device=DEV)
+    c, K, V, m = _prefix(N, rotary=rot, n_cap=208)
+    b = stc.SharedPrefix(c, B, cap, rotary=rot, out_dtype=dtype)
+    start = np.arange(B) % 5
+    start[-1] = -1
+    b.n_tail.copy_(torch.from_numpy(start.astype(np.int32)))
+    b.K_tail.zero_(), b.V_tail.zero_()
+    g = torch.Generator(device=DEV).manual_seed(2)
+    turns = rot.turns.cpu().numpy()
+    host = lambda t: bits_to_f64(PT.host_bf16(t))  # noqa: E731
+    Kt, Vt = np.zeros((2, B, Hkv, cap, D), dtype=np.uint16)
+    for i in range(steps):
+        x = torch.randn(B, Hq + 2 * Hkv, D, device=DEV, generator=g).bfloat16()
+        out = b.step(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:])
+        n = start + i
+        on = (start >= 0) & (n < cap)
+        e = np.nonzero(on)[0]
+        want_k = O.rotary(host(x[:, Hq:Hq + Hkv]), N + n[:, None], turns, 64, True)
+        got_k = host(b.K_tail)
+        assert np.abs(got_k[e, :, n[e]] - want_k[e]).max() <= 2.0 ** -8 * 6      # |k| < 6
+        Kt[e, :, n[e]] = PT.host_bf16(b.K_tail)[e, :, n[e]]
+        Vt[e, :, n[e]] = PT.host_bf16(x[:, Hq + Hkv:])[e]
+        assert np.array_equal(PT.host_bf16(b.V_tail), Vt) and np.array_equal(PT.host_bf16(b.K_tail), Kt)
+        want, size, top = O.shared_attention_all(
+            PT.host_bf16(b.q), PT.host_bf16(c.K)[0, :, :N], PT.host_bf16(V)[0], PT.host_u16(m)[0], None, G,
+            Kt, Vt, n + 1)
+        lim = limits(want, size, top, N + cap, D, dtype)
+        ok = np.abs(out.double().cpu().numpy() - want) <= lim
+        assert ok[start >= 0].all()
+    assert b.dev_status.item() == int((start + steps - 1 >= cap).any())
+    assert (out[-1] == 0).all()                                 # padding: as allocated
+
+
+def test_steps_captured_and_replayed():
+    """One graph of a step, replayed as the tails grow, with eager work between the replays."""
+    B, cap = 5, 40
+    c, *_ = _prefix()
+    rot = stc.Rotary(128, device=DEV)
+    a, b = (stc.SharedPrefix(c, B, cap, rotary=rot) for _ in range(2))
+    for s in (a, b):
+        s.K_tail.zero_(), s.V_tail.zero_()
+        s.n_tail.copy_(torch.tensor([0, 3, 7, -1, 30], dtype=torch.int32))
+    x = torch.randn(B, 12, 128, device=DEV).bfloat16()
+    warm = stc.SharedPrefix(c, B, cap, rotary=rot)
+    warm.step(x[:, :8], x[:, 8:10], x[:, 10:])                  # LDS limits are raised by a first call
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step(x[:, :8], x[:, 8:10], x[:, 10:])
+    for i in range(14):
+        x.copy_(torch.randn(B, 12, 128, device=DEV))
+        graph.replay()
+        b.step(x[:, :8], x[:, 8:10], x[:, 10:])
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, b.out) and torch.equal(a.K_tail, b.K_tail) and torch.equal(a.n_tail, b.n_tail)
+    assert a.n_tail.tolist() == [14, 17, 21, -1, 40] and a.dev_status.item() == 1
+
+
+def test_two_calls_at_once():
+    c = Case(40, 7, 1, 128, 700, 8, 30)
+    d = Case(3, 8, 2, 64, 900, 4, 60)
+    want = c.run(), d.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [None, None]
+    outs = [torch.empty(40, 7, 128, device=DEV), torch.empty(3, 8, 64, device=DEV)]
+    wss = [torch.empty(stc.stc_shared_workspace_bytes(x.shape, (x.N + 15) // 16, x.cap) + 16, dtype=torch.uint8,
+                       device=DEV) for x in (c, d)]
+    for _ in range(5):
+        for i, (x, st) in enumerate(((c, torch.cuda.current_stream()), (d, side))):
+            with torch.cuda.stream(st):
+                e = x.d
+                stc.stc_decode_attention_shared(x.shape, e["q"], e["K"], e["v"], e["mask"], e["off"], None,
+                                                (x.N + 15) // 16, e["Kt"], e["Vt"], e["n"], x.cap, outs[i], wss[i])
+    torch.cuda.synchronize()
+    got = outs
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_selected_pages_of_the_prefix():
+    """Pages from stc_select_pages for one query, attended by a batch."""
+    c, *_ = _prefix(N=1500, k_pages=20)
+    q = torch.randn(6, 8, 128, device=DEV).bfloat16()
+    c.select(q[:1])
+    b = stc.SharedPrefix(c, 6, 4)
+    out = b.attend(q, c.page_idx[0].contiguous())
+    c.attend(q[:1].contiguous())
+    assert (out[:1] - c.out).abs().max() <= 4e-5
+
+
+def test_tensors_of_another_shape_or_type_are_refused():
+    c = Case(2, 4, 2, 64, 40, 4, 6)
+    d = c.d
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    out = torch.empty(2, 4, 64, device=DEV)
+    ok = [c.shape, d["q"], d["K"], d["v"], d["mask"], d["off"], None, 3, d["Kt"], d["Vt"], d["n"], 6, out, ws]
+    stc.stc_decode_attention_shared(*ok)
+    short = lambda t: t[..., :-1].contiguous()  # noqa: E731
+    for i in (1, 2, 3, 4, 5, 8, 9, 10, 12):
+        with pytest.raises(ValueError):
+            stc.stc_decode_attention_shared(*ok[:i], short(ok[i]), *ok[i + 1:])
+    for i in (1, 2, 3, 4, 5, 8, 9, 10, 12):
+        with pytest.raises(TypeError):
+            stc.stc_decode_attention_shared(*ok[:i], ok[i].double(), *ok[i + 1:])
+    with pytest.raises(TypeError):
+        stc.stc_decode_attention_shared(*ok[:1], ok[1].cpu(), *ok[2:])
+    for i, v in ((6, torch.zeros(2, 2, dtype=torch.int32, device=DEV)), (11, 5), (1, d["q"].transpose(1, 2))):
+        with pytest.raises(ValueError):
+            stc.stc_decode_attention_shared(*ok[:i], v, *ok[i + 1:])
+    for i, v in ((7, 4), (11, -1), (13, ws[:16]), (10, None)):
+        with pytest.raises(stc.StcError):
+            stc.stc_decode_attention_shared(*ok[:i], v, *ok[i + 1:])
