@@ -22,8 +22,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1.0e30f;  // running maximum of a row that has seen no token
-constexpr int kWaves = 4, kRows = 32;
-constexpr int kTailTile = 32;
+constexpr int kRows = 32;      // query rows of a wavefront
+constexpr int kTailTile = 32;  // tokens of a tail's tile
 // A maximum that grows by less than this (base 2) leaves the sums as they are: the weights then reach
 // 2^8, far from the range of a float, and 64 multiplications per tile are saved.
 constexpr float kSlack = 8.0f;
@@ -60,21 +60,22 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// WR of the 4 wavefronts share tiles of T tokens and take 32 query rows each; the 4 / WR groups of them
-// take turns at the tiles.
-template <int D, int WR, int T, int STAGES>
+// WR of the W wavefronts of a workgroup share tiles of T tokens and take 32 query rows each; the W / WR
+// groups of them take turns at the tiles.
+template <int D, int W, int WR, int T, int STAGES>
 struct Cfg {
-  static constexpr int WK = kWaves / WR;
-  static constexpr int GT = 64 * WR;          // threads of a group
+  static constexpr int WK = W / WR;
   static constexpr int CH = D / 8;            // 16-byte pieces of a row
-  static constexpr int RPI = GT / CH;         // rows that a group's load instruction covers
-  static constexpr int NI = T / RPI;          // such instructions for a tile
+  static constexpr int RPW = 64 / CH;         // rows of a wavefront's load, 1 KiB: of one page
+  static constexpr int RPI = RPW * WR;        // rows of a group's load
+  static constexpr int NI = T / RPI;          // such loads for a tile
+  static constexpr int TP = T / kPage;        // pages of a tile
   static constexpr int RB = D * 2;            // bytes of a row
   static constexpr int TILE = T * RB;         // a K or V tile
-  static constexpr int BIAS = 2 * TILE;       // offset of the tile's T biases
-  static constexpr int STAGE = 2 * TILE + T * 4;
+  static constexpr int META = 2 * TILE;       // offset of (offset, mask) of the T tokens of another tile
+  static constexpr int STAGE = 2 * TILE + T * 8;
   static constexpr int MROW = D + 4;          // floats of a row in the merge of the groups
-  static constexpr int MERGE = WK > 1 ? kWaves * (kRows * MROW * 4 + kRows * 8) : 0;
+  static constexpr int MERGE = WK > 1 ? W * (kRows * MROW * 4 + kRows * 8) : 0;
   static constexpr int STAGED = WK * STAGES * STAGE;
   static constexpr int LDS = STAGED > MERGE ? STAGED : MERGE;
 };
@@ -95,38 +96,47 @@ __device__ __forceinline__ uint32_t v_at(uint32_t row, uint32_t piece) {
   return row * (D * 2) + ((piece ^ v_shift<D>(row)) << 4);
 }
 
-// Tiles [tile0, tile1) of one stream for the workgroup's query rows; tile t of key group g is tile
+// Loads of 16, 4 and 2 bytes from base + offset that give zeros at and behind `bytes`: the base and the
+// number of bytes are the same for the wavefront, so a load costs no address arithmetic, and absent
+// tokens and dropped value groups need no branch.
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+__device__ __forceinline__ Rsrc rsrc(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;  // an offset behind every end
+
+// Tiles [tile0, tile1) of one stream for the query rows q_row(0 ..); tile t of key group g is tile
 // t * WK + g of the stream.  The groups' results are merged; the partial result of row r goes to
-// index(r) (negative: nowhere).
-template <int D, int WR, int T, int STAGES, int PARTS, bool TAIL, class Row, class Index>
+// index(r) (negative: nowhere).  TAIL: a wavefront does this on its own (WR = 1, one group).
+template <int D, int W, int WR, int T, int STAGES, int PARTS, bool TAIL, class Row, class Index>
 __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int b_tail,
                                        int n_tok, int tile0, int tile1, Row q_row, Index index) {
-  using C = Cfg<D, WR, T, STAGES>;
+  using C = Cfg<D, W, WR, T, STAGES>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wave / WR, wr = wave % WR;
-  const int gt = wr * 64 + lane;
   const int c = lane & 31, half = lane >> 5;
   unsigned char* my = lds + grp * STAGES * C::STAGE;
 
   // the stream
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G));  // log2(pieces per value group)
+  const int lg_group = lg_upg + 4;                           // log2(bytes per value group)
   const unsigned char *Ks, *Vs;
   const uint16_t* mask_s = nullptr;
   const uint32_t* off_s = nullptr;
   const int32_t* pages = nullptr;
-  int slots;  // token slots
+  int tokens;  // without a list: the first so many are attended
   if constexpr (TAIL) {
     const size_t s = (size_t)b_tail * P.Hkv + kvh;
     Ks = P.Kt + s * P.tail_cap * C::RB;
     Vs = P.Vt + s * P.tail_cap * C::RB;
-    slots = n_tok;
+    tokens = n_tok;
   } else {
     Ks = P.K + (size_t)kvh * P.Ncap * C::RB;
-    Vs = P.v + (size_t)kvh * P.cap * (C::RB / P.G);
+    Vs = P.v + ((size_t)kvh * P.cap << lg_group);
     mask_s = P.mask + (size_t)kvh * P.Ncap;
     off_s = P.off + (size_t)kvh * (P.Ncap + 1);
     pages = P.pages ? P.pages + (size_t)kvh * P.k_pages : nullptr;
-    slots = P.k_pages * kPage;
+    tokens = min(P.N, P.k_pages * kPage);
   }
 
   // query rows: operand of S^T, 8 channels of k-step s per lane
@@ -141,61 +151,95 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     }
   }
 
-  // staging: this thread's piece of rows it * RPI + gt / CH
-  const uint32_t piece = gt % C::CH, row_of = gt / C::CH;
-  const uint32_t grp_of = piece >> lg_upg, below = (1u << grp_of) - 1u;
+  // Staging.  This thread takes piece `piece` of the rows i * RPI + row0 + lane / CH, which all lie in
+  // one page for the wavefront.
+  const uint32_t piece = lane % C::CH, row_in = lane / C::CH;
+  const int row0 = wr * C::RPW;
+  const uint32_t grp_of = piece >> lg_upg, bit = 1u << grp_of;
   const uint32_t within = (piece & ((1u << lg_upg) - 1u)) << 4;
-  const uint32_t gbytes = C::RB / P.G;
-  int tok[C::NI];  // of the tile whose data is requested next; -1: no such token
-  uint32_t mk[C::NI], of[C::NI];
   u32x4 kr[C::NI], vr[C::NI];
-  float bias[C::NI];
+  u32x2 meta;  // packed offset and mask of token `lane` of a tile
 
-  auto ask_meta = [&](int tile) {
+  // With a list, lane j holds page j of a tile, -1 if there is none.
+  auto ask_pages = [&](int tile) {
+    int pg = -1;
+    if (!TAIL && pages) {
+      const int at = tile * C::TP + lane;
+      if (lane < C::TP && at < P.k_pages) pg = pages[at];
+      if ((unsigned)pg >= (unsigned)P.NP) pg = -1;
+    }
+    return pg;
+  };
+  // Tokens of page j of a tile; of the rows r .. of a tile up to its end (or the page's, with a list)
+  auto rows_left = [&](int tile, int pgv, int r) {
+    if (!TAIL && pages) {
+      const int pg = __builtin_amdgcn_readlane(pgv, r / kPage);
+      return pg < 0 ? 0 : max(0, min(kPage, P.N - pg * kPage) - r % kPage);
+    }
+    return max(0, min(T, tokens - tile * T) - r);
+  };
+  auto first_token = [&](int tile, int pgv, int r) -> size_t {
+    if (!TAIL && pages)
+      return (size_t)max(__builtin_amdgcn_readlane(pgv, r / kPage), 0) * kPage + r % kPage;
+    return (size_t)tile * T + r;
+  };
+  // For every load of a tile: f(number of the load, its row in the tile, the row that the base address
+  // stands for).  Without a list a tile is one piece of memory and has one base.
+  auto each = [&](auto f) {
+    if (!TAIL && pages) {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) {
-      const int slot = tile * T + i * C::RPI + (int)row_of;
-      int t = -1;
-      if (slot < slots) {
-        if (TAIL || !pages) {
-          t = slot;
-        } else {
-          const int pg = pages[slot / kPage];
-          t = (pg >= 0 && pg < P.NP) ? pg * kPage + slot % kPage : -1;
-        }
-        if (!TAIL && t >= P.N) t = -1;
-      }
-      tok[i] = t;
-      if constexpr (!TAIL) {
-        mk[i] = 0, of[i] = 0;
-        if (t >= 0) mk[i] = mask_s[t], of[i] = off_s[t];
-      }
+      for (int i = 0; i < C::NI; ++i) f(i, i * C::RPI + row0, i * C::RPI + row0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::NI; ++i) f(i, i * C::RPI + row0, row0);
     }
   };
-  auto ask_data = [&]() {
-#pragma unroll
-    for (int i = 0; i < C::NI; ++i) {
-      kr[i] = u32x4{0, 0, 0, 0}, vr[i] = u32x4{0, 0, 0, 0};
-      bias[i] = tok[i] >= 0 ? 0.0f : -INFINITY;
-      if (tok[i] >= 0) {
-        kr[i] = *(const u32x4*)(Ks + (size_t)tok[i] * C::RB + piece * 16);
-        if constexpr (TAIL) {
-          vr[i] = *(const u32x4*)(Vs + (size_t)tok[i] * C::RB + piece * 16);
-        } else {
-          const uint64_t slot = (uint64_t)of[i] + __popc(mk[i] & below);
-          if (((mk[i] >> grp_of) & 1u) && slot < (uint64_t)P.cap)
-            vr[i] = *(const u32x4*)(Vs + slot * gbytes + within);
-        }
+  // Masks and offsets: one request of a wavefront for a tile, handed to all through shared memory.
+  auto ask_meta = [&](int tile, int pgv) {
+    if constexpr (!TAIL) {
+      long long t = (long long)tile * T + lane;
+      if (pages) {
+        const int pg = __shfl(pgv, lane / kPage);
+        t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
       }
+      meta = u32x2{0u, 0u};
+      if (lane < T && t < (pages ? P.N : tokens)) meta = u32x2{off_s[t], mask_s[t]};
+    }
+  };
+  auto put_meta = [&](unsigned char* st) {
+    if (!TAIL && lane < T) *(u32x2*)(st + C::META + lane * 8) = meta;
+  };
+  auto ask_data = [&](int tile, int pgv, const unsigned char* st) {
+    each([&](int i, int r, int base) {
+      const int n = rows_left(tile, pgv, base) * C::RB;
+      const size_t t = first_token(tile, pgv, base) * C::RB;
+      const uint32_t at = (r - base) * C::RB + lane * 16;
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Ks + t, n), at, 0, 0);
+      if constexpr (TAIL) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Vs + t, n), at, 0, 0);
+    });
+    if constexpr (!TAIL) {
+      u32x2 e[C::NI];
+#pragma unroll
+      for (int i = 0; i < C::NI; ++i)
+        e[i] = *(const u32x2*)(st + C::META + (i * C::RPI + row0 + row_in) * 8);
+      each([&](int i, int r, int base) {
+        // values are addressed from those of the base row on: a tile's lie within T * G groups
+        const uint32_t off0 = __builtin_amdgcn_readfirstlane(e[r == base ? i : 0][0]);
+        const long long room = P.cap - (long long)off0;
+        const uint32_t groups = room < 0 ? 0 : room > T * 16 ? T * 16 : (uint32_t)room;
+        const uint32_t slot = e[i][0] - off0 + __popc(e[i][1] & (bit - 1u));
+        const uint32_t at = (e[i][1] & bit) ? (slot << lg_group) + within : kNowhere;
+        vr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+            rsrc(Vs + ((size_t)(room < 0 ? 0 : off0) << lg_group), groups << lg_group), at, 0, 0);
+      });
     }
   };
   auto put_data = [&](unsigned char* st) {
 #pragma unroll
     for (int i = 0; i < C::NI; ++i) {
-      const uint32_t row = i * C::RPI + row_of;
+      const uint32_t row = i * C::RPI + row0 + row_in;
       *(u32x4*)(st + k_at<D>(row, piece)) = kr[i];
       *(u32x4*)(st + C::TILE + v_at<D>(row, piece)) = vr[i];
-      if (piece == 0) *(float*)(st + C::BIAS + row * 4) = bias[i];
     }
   };
 
@@ -207,113 +251,163 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   float m = kNone, l = 0.0f;  // of row c; l of this lane's tokens
   const float scale = kLog2e / sqrtf((float)D);
 
+  // K operand: token c of a subtile, pieces 2 s + half
+  uint32_t ka[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) ka[s] = k_at<D>(c, 2 * s + half);
   // V operand: lane j of 16 addresses row j/4, channels 4 (j%4) .. of a block of 4 rows by 16 channels
   // and receives channel j of the four rows
   const int j16 = lane & 15;
-  const uint32_t v_row = 4 * half + (j16 >> 2);
-  const uint32_t v_piece = ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1);
+  uint32_t va[D / 32];
+#pragma unroll
+  for (int cb = 0; cb < D / 32; ++cb)
+    va[cb] = C::TILE + v_at<D>(4 * half + (j16 >> 2), cb * 4 + ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1)) +
+             8 * (j16 & 1);
 
-  auto compute = [&](const unsigned char* st) {
+  auto compute = [&](const unsigned char* st, int tile, int pgv) {
+    constexpr int SUBS = T / 32;
+    f32x16 S[SUBS] = {};
 #pragma unroll
-    for (int sub = 0; sub < T / 32; ++sub) {
-      f32x16 S;
+    for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const f32x4 bb = *(const f32x4*)(st + C::BIAS + (sub * 32 + 8 * a + 4 * half) * 4);
+      for (int sub = 0; sub < SUBS; ++sub) {
+        const bf16x8 a = *(const bf16x8*)(st + ka[s] + sub * 32 * C::RB);
+        S[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[s], S[sub], 0, 0, 0);
+      }
+    // register 4 a + i of a lane is token 8 a + 4 half + i of the subtile
+    float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[4 * a + i] = bb[i];
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const int n0 = rows_left(tile, pgv, sub * 32);
+      const int n1 = (TAIL || !pages) ? n0 - kPage : rows_left(tile, pgv, sub * 32 + kPage);
+      if (n0 < kPage || n1 < kPage) {  // absent tokens
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = 8 * (i / 4 % 2) + i % 4 + 4 * half;
+          if (at >= (i < 8 ? n0 : n1)) S[sub][i] = -INFINITY;
+        }
       }
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const bf16x8 a = *(const bf16x8*)(st + k_at<D>(sub * 32 + c, 2 * s + half));
-        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[s], S, 0, 0, 0);
-      }
-      float top = S[0];
+      for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(S[sub][i], S[sub][i + 1]), top);
+    }
+    top = max_halves(top) * scale;
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float m1 = top > m + kSlack ? top : m;  // (other rows' maxima do not matter to a row)
+      const float f = __builtin_amdgcn_exp2f(m - m1);
+      m = m1, l *= f;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, S[i]);
-      top = max_halves(top) * scale;
-      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-        const float m1 = top > m + kSlack ? top : m;  // (other rows' maxima do not matter to a row)
-        const float f = __builtin_amdgcn_exp2f(m - m1);
-        m = m1, l *= f;
+      for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int j = 0; j < 16; ++j) O[i][j] *= f;
+    }
 #pragma unroll
-          for (int j = 0; j < 16; ++j) O[i][j] *= f;
-      }
+    for (int sub = 0; sub < SUBS; ++sub) {
       u32x4 p[PARTS][2];
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        float x = __builtin_amdgcn_exp2f(fmaf(S[i], scale, -m));
-        float y = __builtin_amdgcn_exp2f(fmaf(S[i + 1], scale, -m));
+        float x = __builtin_amdgcn_exp2f(fmaf(S[sub][i], scale, -m));
+        float y = __builtin_amdgcn_exp2f(fmaf(S[sub][i + 1], scale, -m));
         if constexpr (PARTS > 1) l += x + y;
 #pragma unroll
         for (int k = 0; k < PARTS; ++k) {
           const uint32_t w = pack_bf16(x, y);
           p[k][i / 8][i % 8 / 2] = w;
-          if (PARTS == 1) l += bf16_lo(w) + bf16_hi(w);
+          if constexpr (PARTS == 1)  // the weights as they are used
+            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
+                                                __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
           x -= bf16_lo(w), y -= bf16_hi(w);
         }
       }
 #pragma unroll
-      for (int cb = 0; cb < D / 32; ++cb)
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int cb = 0; cb < D / 32; ++cb) {
           i16x4 a[2];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t row = sub * 32 + 16 * ks + 8 * k + v_row;
-            const unsigned char* at = st + C::TILE + v_at<D>(row, cb * 4 + v_piece) + 8 * (j16 & 1);
+          for (int k = 0; k < 2; ++k)
             a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) i16x4*)at);
-          }
-          const bf16x8 va = __builtin_bit_cast(
+                (__attribute__((address_space(3)))
+                 i16x4*)(st + va[cb] + (sub * 32 + 16 * ks + 8 * k) * C::RB));
+          const bf16x8 vv = __builtin_bit_cast(
               bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
           for (int k = PARTS - 1; k >= 0; --k)
-            O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, __builtin_bit_cast(bf16x8, p[k][ks]),
+            O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, p[k][ks]),
                                                             O[cb], 0, 0, 0);
         }
     }
   };
 
+  // Pages are asked for four tiles ahead, masks and offsets three, keys and values one.
+  auto tile_of = [&](int t) { return t * (TAIL ? 1 : C::WK) + (TAIL ? 0 : grp); };
+  auto sync = [&] {
+    if constexpr (WR == 1) wave_lds_sync();
+    else __syncthreads();
+  };
+  const bool has_meta = wr == 0;  // the group's wavefront that fetches them
+  int pg0 = ask_pages(tile_of(tile0)), pg1 = ask_pages(tile_of(tile0 + 1));
+  int pg2 = ask_pages(tile_of(tile0 + 2)), pg3 = ask_pages(tile_of(tile0 + 3));
+  // the second half of a stage's meta data belongs to the tile after the one whose data it holds
+  unsigned char* const st1 = my + (STAGES - 1) * C::STAGE;
+  u32x2 meta1 = {0u, 0u};
+  if (has_meta) {
+    ask_meta(tile_of(tile0), pg0);
+    const u32x2 first = meta;
+    ask_meta(tile_of(tile0 + 1), pg1);
+    meta1 = meta;
+    ask_meta(tile_of(tile0 + 2), pg2);
+    const u32x2 third = meta;
+    meta = first;
+    put_meta(st1);
+    meta = third;
+  }
+  sync();
+  ask_data(tile_of(tile0), pg0, st1);
+  if constexpr (STAGES == 1) sync();
+  auto next_meta = [&](int t, unsigned char* st) {  // of tile t + 1 to shared memory, of t + 3 asked for
+    if (has_meta) {
+      const u32x2 later = meta;
+      meta = meta1;
+      put_meta(st);
+      meta1 = later;
+      ask_meta(tile_of(t + 3), pg3);
+    }
+  };
   if constexpr (STAGES == 2) {
-    ask_meta(tile0 * C::WK + grp);
-    ask_data();
-    ask_meta((tile0 + 1) * C::WK + grp);
     put_data(my);
+    next_meta(tile0, my);
     __syncthreads();
-    for (int t = tile0; t < tile1; ++t) {
+    auto turn = [&](int t, auto stage) {
+      unsigned char *const here = my + stage * C::STAGE, *const there = my + (1 - stage) * C::STAGE;
+      if (t + 1 < tile1) ask_data(tile_of(t + 1), pg1, here);
+      const int pg4 = ask_pages(tile_of(t + 4));
+      compute(here, tile_of(t), pg0);
       if (t + 1 < tile1) {
-        ask_data();
-        ask_meta((t + 2) * C::WK + grp);
+        put_data(there);
+        pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
+        next_meta(t + 1, there);
       }
-      compute(my + ((t - tile0) & 1) * C::STAGE);
-      if (t + 1 < tile1) put_data(my + ((t - tile0 + 1) & 1) * C::STAGE);
       __syncthreads();
+    };
+    for (int t = tile0; t < tile1; t += 2) {
+      turn(t, IC<0>{});
+      if (t + 1 < tile1) turn(t + 1, IC<1>{});
     }
   } else {
-    auto sync = [&] {
-      if constexpr (WR == 1) wave_lds_sync();
-      else __syncthreads();
-    };
-    ask_meta(tile0 * C::WK + grp);
-    ask_data();
-    ask_meta((tile0 + 1) * C::WK + grp);
     for (int t = tile0; t < tile1; ++t) {
       put_data(my);
-      if (t + 1 < tile1) {
-        ask_data();
-        ask_meta((t + 2) * C::WK + grp);
-      }
+      next_meta(t, my);
       sync();
-      compute(my);
+      if (t + 1 < tile1) ask_data(tile_of(t + 1), pg1, my);
+      const int pg4 = ask_pages(tile_of(t + 4));
+      compute(my, tile_of(t), pg0);
       sync();
+      pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
     }
   }
   l = sum_halves(l);
 
-  if constexpr (C::WK == 1) {
+  if constexpr (C::WK == 1 || TAIL) {
     const long long at = index(wr * kRows + c);
     if (at >= 0) {
       float* o = P.acc + at * D;
@@ -329,7 +423,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     __syncthreads();
     constexpr int BUF = kRows * C::MROW * 4;
     float* mine = (float*)(lds + wave * BUF);
-    f32x2* mls = (f32x2*)(lds + kWaves * BUF);
+    f32x2* mls = (f32x2*)(lds + W * BUF);
 #pragma unroll
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
@@ -339,7 +433,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     if (half == 0) mls[wave * kRows + c] = f32x2{m, l};
     __syncthreads();
     constexpr int Q = D / 4;                       // quads of channels
-    for (int i = threadIdx.x; i < WR * kRows * Q; i += 64 * kWaves) {
+    for (int i = threadIdx.x; i < WR * kRows * Q; i += 64 * W) {
       const int r = i / Q, quad = i % Q, w = r / kRows, rr = r % kRows;
       const long long at = index(r);
       if (at < 0) continue;
@@ -363,20 +457,23 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   }
 }
 
-template <int WR>
-constexpr int tile_of() { return WR == 4 ? 64 : 32; }
-template <int WR>
-constexpr int stages_of() { return WR == 4 ? 2 : 1; }
+// Of the forms by their number of wavefronts that share a tile.
+constexpr int form_waves(int wr) { return wr == 8 ? 8 : 4; }
+constexpr int form_tile(int wr) { return wr >= 4 ? 64 : 32; }
+constexpr int form_stages(int wr) { return wr >= 4 ? 2 : 1; }
+template <int D, int WR>
+using Form = Cfg<D, form_waves(WR), WR, form_tile(WR), form_stages(WR)>;
 
-template <int D, int WR, int PARTS>
+template <int D, int WR>
 constexpr int shared_lds() {
-  constexpr int a = Cfg<D, WR, tile_of<WR>(), stages_of<WR>()>::LDS, b = Cfg<D, 1, kTailTile, 1>::LDS;
+  constexpr int a = Form<D, WR>::LDS, b = Cfg<D, form_waves(WR), 1, kTailTile, 1>::STAGED;
   return a > b ? a : b;
 }
 
 template <int D, int WR, int PARTS>
-__global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
+__global__ __launch_bounds__(64 * form_waves(WR), 2) void shared_kernel(SharedParams P) {
   extern __shared__ __align__(16) unsigned char lds[];
+  constexpr int W = form_waves(WR);
   const int id = blockIdx.x;
   if (id < P.prefix_blocks) {
     // the row blocks of a split share its keys and values: same id modulo the 8 XCDs
@@ -385,11 +482,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
     const int u = id / per * kXcds + id % kXcds, rb = id % per / kXcds;
     if (u >= P.Hkv * P.splits) return;
     const int kvh = u / P.splits, split = u % P.splits;
-    constexpr int T = tile_of<WR>(), WK = kWaves / WR;
+    constexpr int T = form_tile(WR), WK = W / WR;
     const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
     const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
     const int rows = P.B * P.R, row0 = rb * WR * kRows;
-    attend<D, WR, T, stages_of<WR>(), PARTS, false>(
+    attend<D, W, WR, T, form_stages(WR), PARTS, false>(
         P, lds, kvh, 0, 0, t0, t1,
         [&](int r) -> const uint16_t* {
           r += row0;
@@ -401,16 +498,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
           if (r >= rows) return -1;
           return ((long long)(r / P.R) * P.Hq + kvh * P.R + r % P.R) * P.splits + split;
         });
-  } else {
-    const int i = id - P.prefix_blocks;
+  } else {  // a piece of a sequence's tail per wavefront
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = (id - P.prefix_blocks) * W + wave;
     const int ts = i % P.tail_splits, s = i / P.tail_splits, kvh = s % P.Hkv, b = s / P.Hkv;
-    const int n = min(P.n_tail[b], P.tail_cap);
+    if (b >= P.B) return;
+    const int n = __builtin_amdgcn_readfirstlane(min(P.n_tail[b], P.tail_cap));
     const int t0 = ts * P.tail_tiles;
-    constexpr int WK = kWaves;
-    const int tiles = (n + kTailTile * WK - 1) / (kTailTile * WK);
+    const int tiles = (n + kTailTile - 1) / kTailTile;
     if (t0 >= tiles) return;  // (n <= 0 among them)
     const int t1 = min(tiles, t0 + P.tail_tiles);
-    attend<D, 1, kTailTile, 1, PARTS, true>(
+    attend<D, W, 1, kTailTile, 1, PARTS, true>(
         P, lds, kvh, b, n, t0, t1,
         [&](int r) -> const uint16_t* {
           return r < P.R ? P.q + ((size_t)b * P.Hq + kvh * P.R + r) * D : nullptr;
@@ -424,41 +522,82 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
 }
 
 // Merges the partial results of a row in a fixed order: the prefix's splits, then those of the tail that
-// hold tokens.  A wavefront per row.
-template <int D>
+// hold tokens.  WPR wavefronts per row; D/4 lanes take four channels each of a partial result, 16 bytes
+// a lane, and the groups of so many lanes share the partial results out.
+template <int D, int WPR>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams P) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= P.B * P.Hq) return;
+  constexpr int L = D / 4, GPW = 64 / L, GROUPS = GPW * WPR, AHEAD = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.x * (4 / WPR) + wave / WPR;
   const int b = row / P.Hq;
-  const int n = P.n_tail ? P.n_tail[b] : 0;
-  if (n < 0) return;  // padding: its rows of the output stay as they are
-  const int per = kTailTile * kWaves * P.tail_tiles;
-  const int nt = P.tail_cap ? (min(n, P.tail_cap) + per - 1) / per : 0;
+  const int n = row < P.B * P.Hq ? (P.n_tail ? P.n_tail[b] : 0) : -1;
+  if (WPR == 1 && n < 0) return;  // padding: its rows of the output stay as they are
+  const int per = kTailTile * P.tail_tiles;
+  const int nt = P.tail_cap && n > 0 ? (min(n, P.tail_cap) + per - 1) / per : 0;
   const long long p0 = (long long)row * P.splits;
-  const long long t0 = (long long)P.B * P.Hq * P.splits + (long long)row * P.tail_splits;
-  const int total = P.splits + nt;
-  auto at = [&](int i) { return i < P.splits ? p0 + i : t0 + (i - P.splits); };
-  float top = kNone;
-  for (int i = lane; i < total; i += 64) top = fmaxf(top, P.ml[at(i) * 2]);
+  const long long t0 = (long long)P.B * P.Hq * P.splits + (long long)row * P.tail_splits - P.splits;
+  const int total = n < 0 ? 0 : P.splits + nt;
+  const f32x4* acc = (const f32x4*)P.acc;
+  const f32x2* ml = (const f32x2*)P.ml;
+  const int group = (WPR > 1 ? wave % WPR : 0) * GPW + lane / L, quad = lane % L;
+  f32x4 o = {0, 0, 0, 0};
+  float top = kNone, sum = 0.0f;  // of this group's partial results
+  for (int i0 = group; i0 < total; i0 += GROUPS * AHEAD) {
+    f32x4 x[AHEAD];
+    f32x2 e[AHEAD];
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s));
-  constexpr int E = D / 64;
-  float o[E] = {}, sum = 0.0f;
-  for (int i = 0; i < total; ++i) {
-    const long long k = at(i);
-    const float f = __builtin_amdgcn_exp2f(P.ml[k * 2] - top);
-    sum += f * P.ml[k * 2 + 1];
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k * GROUPS;
+      const long long at = (i < P.splits ? p0 : t0) + i;
+      e[k] = f32x2{kNone, 0.0f}, x[k] = f32x4{0, 0, 0, 0};
+      if (i < total) e[k] = ml[at], x[k] = acc[at * L + quad];
+    }
+    float top1 = top;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += f * P.acc[k * D + lane * E + e];
+    for (int k = 0; k < AHEAD; ++k) top1 = fmaxf(top1, e[k][0]);
+    const float g = __builtin_amdgcn_exp2f(top - top1);
+    top = top1, sum *= g;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] *= g;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float f = __builtin_amdgcn_exp2f(e[k][0] - top);
+      sum += f * e[k][1];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] += f * x[k][c];
+    }
   }
+  auto join = [&](float top1, float sum1, f32x4 o1) {
+    const float t = fmaxf(top, top1);
+    const float f = __builtin_amdgcn_exp2f(top - t), g = __builtin_amdgcn_exp2f(top1 - t);
+    top = t, sum = sum * f + sum1 * g;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = o[c] * f + o1[c] * g;
+  };
+#pragma unroll
+  for (int s = L; s < 64; s *= 2) {
+    f32x4 o1;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o1[c] = __shfl_xor(o[c], s);
+    join(__shfl_xor(top, s), __shfl_xor(sum, s), o1);
+  }
+  if constexpr (WPR > 1) {
+    __shared__ f32x4 s_o[4][L];
+    __shared__ f32x2 s_e[4];
+    if (lane < L) s_o[wave][lane] = o;
+    if (lane == 0) s_e[wave] = f32x2{top, sum};
+    __syncthreads();
+    if (wave % WPR != 0 || n < 0) return;
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) join(s_e[wave + w][0], s_e[wave + w][1], s_o[wave + w][quad]);
+  }
+  if (lane >= L) return;
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // nothing attended: zeros
   if (P.out_bf16) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      ((uint16_t*)P.out)[(size_t)row * D + lane * E + e] = (uint16_t)pack_bf16(o[e] * inv, 0.0f);
+    ((u32x2*)P.out)[(size_t)row * L + quad] =
+        u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
   } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) ((float*)P.out)[(size_t)row * D + lane * E + e] = o[e] * inv;
+    ((f32x4*)P.out)[(size_t)row * L + quad] = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   }
 }
 
@@ -469,23 +608,32 @@ struct SharedPlan {
 SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   SharedPlan p{};
   const long long rows = (long long)s.B * (s.Hq / s.Hkv);
-  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
   p.row_blocks = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
-  const int per = (p.wr == 4 ? 64 : 32) * (kWaves / p.wr);  // tokens of a tile of all groups
+  const int per = form_tile(p.wr) * (form_waves(p.wr) / p.wr);  // tokens of a tile of all groups
   const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
-  const long long units = (long long)s.Hkv * p.row_blocks;
-  long long want = 512 / units;
-  if (want < 1) want = 1;
-  if (want > tiles) want = tiles;
-  p.split_tiles = (int)((tiles + want - 1) / want);
+  // The row blocks of a split stay on one of 8 XCDs of 32 compute units, so splits come in whole rounds
+  // of an XCD.  Of the splits that fill up to 4 rounds the cheapest: a tile of time for each tile of a
+  // split, two for starting and ending a workgroup, and the traffic of the partial results.
+  const int slots = 32 * (p.wr == 8 ? 1 : 2);
+  double best = 0;
+  int splits = 1;
+  for (int rounds = 1; rounds <= 4; ++rounds) {
+    long long n = 8LL * (rounds * slots / p.row_blocks) / s.Hkv;
+    if (n < 1) continue;
+    if (n > tiles) n = tiles;
+    const double cost = rounds * ((tiles + n - 1) / n + 2.0) + n * (rows * s.Hkv * 1e-4);
+    if (best == 0 || cost < best) best = cost, splits = (int)n;
+  }
+  p.split_tiles = (tiles + splits - 1) / splits;
   p.splits = (tiles + p.split_tiles - 1) / p.split_tiles;
   if (tail_cap > 0) {
-    const int tt = (tail_cap + kTailTile * kWaves - 1) / (kTailTile * kWaves);
+    const int tt = (tail_cap + kTailTile - 1) / kTailTile;
     const long long streams = (long long)s.B * s.Hkv;
-    long long per_wg = streams * tt / 1024;
-    if (per_wg < 1) per_wg = 1;
-    if (per_wg > tt) per_wg = tt;
-    p.tail_tiles = (int)per_wg;
+    long long per_wave = streams * tt / 4096;
+    if (per_wave < 1) per_wave = 1;
+    if (per_wave > tt) per_wave = tt;
+    p.tail_tiles = (int)per_wave;
     p.tail_splits = (tt + p.tail_tiles - 1) / p.tail_tiles;
   }
   return p;
@@ -496,19 +644,22 @@ size_t partials(const stc_shape_t& s, const SharedPlan& p) {
 }
 
 template <int D, int WR, int PARTS>
-int shared_go(const SharedParams& P, int blocks, hipStream_t st) {
+int shared_go(const SharedParams& P, long long tail_waves, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
-  constexpr int lds = shared_lds<D, WR, PARTS>();
+  constexpr int lds = shared_lds<D, WR>(), W = form_waves(WR);
   if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS>, lds, done)) return -1;
-  shared_kernel<D, WR, PARTS><<<blocks, 64 * kWaves, lds, st>>>(P);
+  const long long blocks = P.prefix_blocks + (tail_waves + W - 1) / W;
+  if (blocks * W > INT32_MAX) return -1;
+  shared_kernel<D, WR, PARTS><<<(unsigned)blocks, 64 * W, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 template <int D, int PARTS>
-int shared_rows(const SharedParams& P, int wr, int blocks, hipStream_t st) {
-  return wr == 1   ? shared_go<D, 1, PARTS>(P, blocks, st)
-         : wr == 2 ? shared_go<D, 2, PARTS>(P, blocks, st)
-                   : shared_go<D, 4, PARTS>(P, blocks, st);
+int shared_rows(const SharedParams& P, int wr, long long tail_waves, hipStream_t st) {
+  return wr == 1   ? shared_go<D, 1, PARTS>(P, tail_waves, st)
+         : wr == 2 ? shared_go<D, 2, PARTS>(P, tail_waves, st)
+         : wr == 4 ? shared_go<D, 4, PARTS>(P, tail_waves, st)
+                   : shared_go<D, 8, PARTS>(P, tail_waves, st);
 }
 
 }  // namespace
@@ -536,16 +687,22 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   P.out_bf16 = out_bf16;
   const long long units = (s.Hkv * (long long)p.splits + 7) / 8 * 8;
   P.prefix_blocks = (int)(units * p.row_blocks);
-  const long long blocks = P.prefix_blocks + (long long)s.B * s.Hkv * p.tail_splits;
-  if (blocks > INT32_MAX) return -1;
-  const int rc = s.D == 128 ? (out_bf16 ? shared_rows<128, 1>(P, p.wr, (int)blocks, st)
-                                        : shared_rows<128, 2>(P, p.wr, (int)blocks, st))
-                            : (out_bf16 ? shared_rows<64, 1>(P, p.wr, (int)blocks, st)
-                                        : shared_rows<64, 2>(P, p.wr, (int)blocks, st));
+  const long long tail_waves = (long long)s.B * s.Hkv * p.tail_splits;
+  const int rc = s.D == 128 ? (out_bf16 ? shared_rows<128, 1>(P, p.wr, tail_waves, st)
+                                        : shared_rows<128, 2>(P, p.wr, tail_waves, st))
+                            : (out_bf16 ? shared_rows<64, 1>(P, p.wr, tail_waves, st)
+                                        : shared_rows<64, 2>(P, p.wr, tail_waves, st));
   if (rc) return -1;
   const int rows = s.B * s.Hq;
-  if (s.D == 128) shared_merge_kernel<128><<<(rows + 3) / 4, 256, 0, st>>>(P);
-  else shared_merge_kernel<64><<<(rows + 3) / 4, 256, 0, st>>>(P);
+  const int wpr = p.splits + p.tail_splits > 16 ? 4 : 1;
+  const int groups = (rows * (long long)wpr + 3) / 4;
+  if (s.D == 128) {
+    if (wpr == 4) shared_merge_kernel<128, 4><<<groups, 256, 0, st>>>(P);
+    else shared_merge_kernel<128, 1><<<groups, 256, 0, st>>>(P);
+  } else {
+    if (wpr == 4) shared_merge_kernel<64, 4><<<groups, 256, 0, st>>>(P);
+    else shared_merge_kernel<64, 1><<<groups, 256, 0, st>>>(P);
+  }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
