@@ -22,8 +22,10 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1.0e30f;  // running maximum of a row that has seen no token
+constexpr int kWaves = 8;      // of a workgroup; one workgroup fills a compute unit
 constexpr int kRows = 32;      // query rows of a wavefront
 constexpr int kTailTile = 32;  // tokens of a tail's tile
+constexpr int kXcds = 8;
 // A maximum that grows by less than this (base 2) leaves the sums as they are: the weights then reach
 // 2^8, far from the range of a float, and 64 multiplications per tile are saved.
 constexpr float kSlack = 8.0f;
@@ -40,8 +42,8 @@ struct SharedParams {
   void* out;
   long long cap;
   int B, R, Hq, Hkv, N, NP, G, Ncap, k_pages, tail_cap;
-  int row_blocks, splits, split_tiles, prefix_blocks;  // prefix: tiles (of all key groups) per split
-  int tail_splits, tail_tiles;
+  int row_blocks, splits, split_tiles;  // prefix: tiles (of all key groups) per split
+  int tail_splits, tail_tiles, tail_blocks;
   int out_bf16;
 };
 
@@ -59,12 +61,39 @@ __device__ __forceinline__ float sum_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Over the four lanes that differ in lane bits 4 and 5.
+template <class Op>
+__device__ __forceinline__ float over_groups(float x, Op op) {
+  const uint32_t a = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const uint32_t b = __float_as_uint(op(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
 
-// WR of the W wavefronts of a workgroup share tiles of T tokens and take 32 query rows each; the W / WR
+// The weights of two logits in PARTS bf16 parts, put(part, both as one word); l: their sum, of the
+// weights as they are used.
+template <int PARTS, class Put>
+__device__ __forceinline__ void weights(float s0, float s1, float scale, float m, float& l, Put put) {
+  float x = __builtin_amdgcn_exp2f(fmaf(s0, scale, -m));
+  float y = __builtin_amdgcn_exp2f(fmaf(s1, scale, -m));
+  if constexpr (PARTS > 1) l += x + y;
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    const uint32_t w = pack_bf16(x, y);
+    put(k, w);
+    if constexpr (PARTS == 1)
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
+                                          __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+    x -= bf16_lo(w), y -= bf16_hi(w);
+  }
+}
+
+// WR of the 8 wavefronts of a workgroup share tiles of T tokens and take 32 query rows each; the 8 / WR
 // groups of them take turns at the tiles.
-template <int D, int W, int WR, int T, int STAGES>
+template <int D, int WR, int T, int STAGES>
 struct Cfg {
-  static constexpr int WK = W / WR;
+  static constexpr int WK = kWaves / WR;
   static constexpr int CH = D / 8;            // 16-byte pieces of a row
   static constexpr int RPW = 64 / CH;         // rows of a wavefront's load, 1 KiB: of one page
   static constexpr int RPI = RPW * WR;        // rows of a group's load
@@ -75,7 +104,7 @@ struct Cfg {
   static constexpr int META = 2 * TILE;       // offset of (offset, mask) of the T tokens of another tile
   static constexpr int STAGE = 2 * TILE + T * 8;
   static constexpr int MROW = D + 4;          // floats of a row in the merge of the groups
-  static constexpr int MERGE = WK > 1 ? W * (kRows * MROW * 4 + kRows * 8) : 0;
+  static constexpr int MERGE = WK > 1 ? kWaves * (kRows * MROW * 4 + kRows * 8) : 0;
   static constexpr int STAGED = WK * STAGES * STAGE;
   static constexpr int LDS = STAGED > MERGE ? STAGED : MERGE;
 };
@@ -105,13 +134,13 @@ __device__ __forceinline__ Rsrc rsrc(const void* base, uint32_t bytes) {
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset behind every end
 
-// Tiles [tile0, tile1) of one stream for the query rows q_row(0 ..); tile t of key group g is tile
-// t * WK + g of the stream.  The groups' results are merged; the partial result of row r goes to
-// index(r) (negative: nowhere).  TAIL: a wavefront does this on its own (WR = 1, one group).
-template <int D, int W, int WR, int T, int STAGES, int PARTS, bool TAIL, class Row, class Index>
-__device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int b_tail,
-                                       int n_tok, int tile0, int tile1, Row q_row, Index index) {
-  using C = Cfg<D, W, WR, T, STAGES>;
+// Tiles [tile0, tile1) of the prefix for the query rows q_row(0 ..) of one KV head; tile t of key group
+// g is tile t * WK + g.  The groups' results are merged; the partial result of row r goes to index(r)
+// (negative: nowhere).
+template <int D, int WR, int T, int STAGES, int PARTS, class Row, class Index>
+__device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int tile0,
+                                       int tile1, Row q_row, Index index) {
+  using C = Cfg<D, WR, T, STAGES>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wave / WR, wr = wave % WR;
   const int c = lane & 31, half = lane >> 5;
@@ -120,24 +149,12 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   // the stream
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G));  // log2(pieces per value group)
   const int lg_group = lg_upg + 4;                           // log2(bytes per value group)
-  const unsigned char *Ks, *Vs;
-  const uint16_t* mask_s = nullptr;
-  const uint32_t* off_s = nullptr;
-  const int32_t* pages = nullptr;
-  int tokens;  // without a list: the first so many are attended
-  if constexpr (TAIL) {
-    const size_t s = (size_t)b_tail * P.Hkv + kvh;
-    Ks = P.Kt + s * P.tail_cap * C::RB;
-    Vs = P.Vt + s * P.tail_cap * C::RB;
-    tokens = n_tok;
-  } else {
-    Ks = P.K + (size_t)kvh * P.Ncap * C::RB;
-    Vs = P.v + ((size_t)kvh * P.cap << lg_group);
-    mask_s = P.mask + (size_t)kvh * P.Ncap;
-    off_s = P.off + (size_t)kvh * (P.Ncap + 1);
-    pages = P.pages ? P.pages + (size_t)kvh * P.k_pages : nullptr;
-    tokens = min(P.N, P.k_pages * kPage);
-  }
+  const unsigned char* Ks = P.K + (size_t)kvh * P.Ncap * C::RB;
+  const unsigned char* Vs = P.v + ((size_t)kvh * P.cap << lg_group);
+  const uint16_t* mask_s = P.mask + (size_t)kvh * P.Ncap;
+  const uint32_t* off_s = P.off + (size_t)kvh * (P.Ncap + 1);
+  const int32_t* pages = P.pages ? P.pages + (size_t)kvh * P.k_pages : nullptr;
+  const int tokens = min(P.N, P.k_pages * kPage);  // without a list: the first so many are attended
 
   // query rows: operand of S^T, 8 channels of k-step s per lane
   bf16x8 qf[D / 16];
@@ -163,7 +180,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   // With a list, lane j holds page j of a tile, -1 if there is none.
   auto ask_pages = [&](int tile) {
     int pg = -1;
-    if (!TAIL && pages) {
+    if (pages) {
       const int at = tile * C::TP + lane;
       if (lane < C::TP && at < P.k_pages) pg = pages[at];
       if ((unsigned)pg >= (unsigned)P.NP) pg = -1;
@@ -172,21 +189,21 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   };
   // Tokens of page j of a tile; of the rows r .. of a tile up to its end (or the page's, with a list)
   auto rows_left = [&](int tile, int pgv, int r) {
-    if (!TAIL && pages) {
+    if (pages) {
       const int pg = __builtin_amdgcn_readlane(pgv, r / kPage);
       return pg < 0 ? 0 : max(0, min(kPage, P.N - pg * kPage) - r % kPage);
     }
     return max(0, min(T, tokens - tile * T) - r);
   };
   auto first_token = [&](int tile, int pgv, int r) -> size_t {
-    if (!TAIL && pages)
+    if (pages)
       return (size_t)max(__builtin_amdgcn_readlane(pgv, r / kPage), 0) * kPage + r % kPage;
     return (size_t)tile * T + r;
   };
   // For every load of a tile: f(number of the load, its row in the tile, the row that the base address
   // stands for).  Without a list a tile is one piece of memory and has one base.
   auto each = [&](auto f) {
-    if (!TAIL && pages) {
+    if (pages) {
 #pragma unroll
       for (int i = 0; i < C::NI; ++i) f(i, i * C::RPI + row0, i * C::RPI + row0);
     } else {
@@ -196,18 +213,16 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   };
   // Masks and offsets: one request of a wavefront for a tile, handed to all through shared memory.
   auto ask_meta = [&](int tile, int pgv) {
-    if constexpr (!TAIL) {
-      long long t = (long long)tile * T + lane;
-      if (pages) {
-        const int pg = __shfl(pgv, lane / kPage);
-        t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
-      }
-      meta = u32x2{0u, 0u};
-      if (lane < T && t < (pages ? P.N : tokens)) meta = u32x2{off_s[t], mask_s[t]};
+    long long t = (long long)tile * T + lane;
+    if (pages) {
+      const int pg = __shfl(pgv, lane / kPage);
+      t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
     }
+    meta = u32x2{0u, 0u};
+    if (lane < T && t < (pages ? P.N : tokens)) meta = u32x2{off_s[t], mask_s[t]};
   };
   auto put_meta = [&](unsigned char* st) {
-    if (!TAIL && lane < T) *(u32x2*)(st + C::META + lane * 8) = meta;
+    if (lane < T) *(u32x2*)(st + C::META + lane * 8) = meta;
   };
   auto ask_data = [&](int tile, int pgv, const unsigned char* st) {
     each([&](int i, int r, int base) {
@@ -215,24 +230,21 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       const size_t t = first_token(tile, pgv, base) * C::RB;
       const uint32_t at = (r - base) * C::RB + lane * 16;
       kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Ks + t, n), at, 0, 0);
-      if constexpr (TAIL) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Vs + t, n), at, 0, 0);
     });
-    if constexpr (!TAIL) {
-      u32x2 e[C::NI];
+    u32x2 e[C::NI];
 #pragma unroll
-      for (int i = 0; i < C::NI; ++i)
-        e[i] = *(const u32x2*)(st + C::META + (i * C::RPI + row0 + row_in) * 8);
-      each([&](int i, int r, int base) {
-        // values are addressed from those of the base row on: a tile's lie within T * G groups
-        const uint32_t off0 = __builtin_amdgcn_readfirstlane(e[r == base ? i : 0][0]);
-        const long long room = P.cap - (long long)off0;
-        const uint32_t groups = room < 0 ? 0 : room > T * 16 ? T * 16 : (uint32_t)room;
-        const uint32_t slot = e[i][0] - off0 + __popc(e[i][1] & (bit - 1u));
-        const uint32_t at = (e[i][1] & bit) ? (slot << lg_group) + within : kNowhere;
-        vr[i] = __builtin_amdgcn_raw_buffer_load_b128(
-            rsrc(Vs + ((size_t)(room < 0 ? 0 : off0) << lg_group), groups << lg_group), at, 0, 0);
-      });
-    }
+    for (int i = 0; i < C::NI; ++i)
+      e[i] = *(const u32x2*)(st + C::META + (i * C::RPI + row0 + row_in) * 8);
+    each([&](int i, int r, int base) {
+      // values are addressed from those of the base row on: a tile's lie within T * G groups
+      const uint32_t off0 = __builtin_amdgcn_readfirstlane(e[r == base ? i : 0][0]);
+      const long long room = P.cap - (long long)off0;
+      const uint32_t groups = room < 0 ? 0 : room > T * 16 ? T * 16 : (uint32_t)room;
+      const uint32_t slot = e[i][0] - off0 + __popc(e[i][1] & (bit - 1u));
+      const uint32_t at = (e[i][1] & bit) ? (slot << lg_group) + within : kNowhere;
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          rsrc(Vs + ((size_t)(room < 0 ? 0 : off0) << lg_group), groups << lg_group), at, 0, 0);
+    });
   };
   auto put_data = [&](unsigned char* st) {
 #pragma unroll
@@ -279,7 +291,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
       const int n0 = rows_left(tile, pgv, sub * 32);
-      const int n1 = (TAIL || !pages) ? n0 - kPage : rows_left(tile, pgv, sub * 32 + kPage);
+      const int n1 = !pages ? n0 - kPage : rows_left(tile, pgv, sub * 32 + kPage);
       if (n0 < kPage || n1 < kPage) {  // absent tokens
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -304,20 +316,9 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     for (int sub = 0; sub < SUBS; ++sub) {
       u32x4 p[PARTS][2];
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        float x = __builtin_amdgcn_exp2f(fmaf(S[sub][i], scale, -m));
-        float y = __builtin_amdgcn_exp2f(fmaf(S[sub][i + 1], scale, -m));
-        if constexpr (PARTS > 1) l += x + y;
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
-          const uint32_t w = pack_bf16(x, y);
-          p[k][i / 8][i % 8 / 2] = w;
-          if constexpr (PARTS == 1)  // the weights as they are used
-            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
-                                                __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
-          x -= bf16_lo(w), y -= bf16_hi(w);
-        }
-      }
+      for (int i = 0; i < 16; i += 2)
+        weights<PARTS>(S[sub][i], S[sub][i + 1], scale, m, l,
+                       [&](int k, uint32_t w) { p[k][i / 8][i % 8 / 2] = w; });
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -339,7 +340,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   };
 
   // Pages are asked for four tiles ahead, masks and offsets three, keys and values one.
-  auto tile_of = [&](int t) { return t * (TAIL ? 1 : C::WK) + (TAIL ? 0 : grp); };
+  auto tile_of = [&](int t) { return t * C::WK + grp; };
   auto sync = [&] {
     if constexpr (WR == 1) wave_lds_sync();
     else __syncthreads();
@@ -407,7 +408,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   }
   l = sum_halves(l);
 
-  if constexpr (C::WK == 1 || TAIL) {
+  if constexpr (C::WK == 1) {
     const long long at = index(wr * kRows + c);
     if (at >= 0) {
       float* o = P.acc + at * D;
@@ -423,7 +424,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     __syncthreads();
     constexpr int BUF = kRows * C::MROW * 4;
     float* mine = (float*)(lds + wave * BUF);
-    f32x2* mls = (f32x2*)(lds + W * BUF);
+    f32x2* mls = (f32x2*)(lds + kWaves * BUF);
 #pragma unroll
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
@@ -433,7 +434,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     if (half == 0) mls[wave * kRows + c] = f32x2{m, l};
     __syncthreads();
     constexpr int Q = D / 4;                       // quads of channels
-    for (int i = threadIdx.x; i < WR * kRows * Q; i += 64 * W) {
+    for (int i = threadIdx.x; i < WR * kRows * Q; i += 64 * kWaves) {
       const int r = i / Q, quad = i % Q, w = r / kRows, rr = r % kRows;
       const long long at = index(r);
       if (at < 0) continue;
@@ -457,68 +458,224 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   }
 }
 
+// The tails.  A wavefront takes pieces of P.tail_tiles tiles of 32 tokens, one after the other, with the
+// next tile on its way while one is worked on.  The pieces that hold tokens, in order of sequence, KV head
+// and place, are shared out evenly over the nw wavefronts, which add up the lengths for it; where a piece
+// begins depends on the sizes alone.  The R <= 16 query rows are the columns of 16x16x32 products:
+//   lane (column c, group g of 4) holds tokens 4 g + i and 16 + 4 g + i of S^T, which is the operand of
+//   the second product if the values' tokens are taken in the same order.
+template <int D, int PARTS>
+__device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, int w, int nw) {
+  using C = Cfg<D, 1, kTailTile, 1>;
+  constexpr int RB = C::RB, NI = C::NI;
+  const int lane = threadIdx.x & 63;
+  const int c = lane & 15, g = lane >> 4;
+  const int per = kTailTile * P.tail_tiles;  // tokens of a piece
+  // lane j: tokens of sequence base + j
+  auto lengths = [&](int base) {
+    return base + lane < P.B ? max(0, min(P.n_tail[base + lane], P.tail_cap)) : 0;
+  };
+  auto pieces_of = [&](int n) { return (uint32_t)(n + per - 1) / (uint32_t)per; };
+  uint32_t total = 0;
+  for (int base = 0; base < P.B; base += 64)
+    total += wave_reduce(pieces_of(lengths(base)), OpAdd{}, 0u);
+  const uint64_t all = (uint64_t)total * P.Hkv;
+  uint32_t at = (uint32_t)(all * w / nw);
+  const uint32_t end = (uint32_t)(all * (w + 1) / nw);
+  if (at >= end) return;
+
+  // the sequence that piece `at` belongs to
+  int base = 0, lens = lengths(0), b = 0, n = 0;
+  uint32_t seen = 0, in_b = 0;  // pieces in front of sequence b; of sequence b, all KV heads
+  for (;; base += 64, lens = lengths(base)) {
+    const uint32_t mine = pieces_of(lens), incl = wave_scan(mine, OpAdd{}, 0u);
+    const uint64_t past = __builtin_amdgcn_ballot_w64((seen + incl) * (uint64_t)P.Hkv > at);
+    if (past) {
+      const int j = __builtin_ctzll(past);
+      b = base + j;
+      n = __builtin_amdgcn_readlane(lens, j);
+      in_b = pieces_of(n) * P.Hkv;
+      seen = (seen + __builtin_amdgcn_readlane(incl, j)) * P.Hkv - in_b;
+      break;
+    }
+    seen += __builtin_amdgcn_readlane(incl, 63);
+  }
+  // (`all` > `at`, so some sequence holds it)
+  int kvh, piece, t, t_end;
+  auto open = [&] {  // the place of piece `at` in sequence b
+    const uint32_t np = pieces_of(n), i = at - seen;
+    kvh = i / np, piece = i % np;
+    t = piece * P.tail_tiles;
+    t_end = min((n + kTailTile - 1) / kTailTile, t + P.tail_tiles);
+  };
+  open();
+
+  u32x4 kr[NI], vr[NI];
+  bf16x8 qn[D / 32], qf[D / 32];
+  auto ask = [&] {
+    const size_t row = ((size_t)b * P.Hkv + kvh) * P.tail_cap + (size_t)t * kTailTile;
+    const int bytes = min(kTailTile, n - t * kTailTile) * RB;
+    const Rsrc rk = rsrc(P.Kt + row * RB, bytes), rv = rsrc(P.Vt + row * RB, bytes);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, i * 1024 + lane * 16, 0, 0);
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, i * 1024 + lane * 16, 0, 0);
+    }
+  };
+  auto ask_q = [&] {
+    const Rsrc rq = rsrc(P.q + ((size_t)b * P.Hq + kvh * P.R) * D, P.R * RB);
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+      qn[s] = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, c * RB + s * 64 + g * 16, 0, 0));
+  };
+  ask_q();
+  ask();
+
+  f32x4 O[D / 16];
+  float m = kNone, l = 0.0f;
+  const float scale = kLog2e / sqrtf((float)D);
+  const int row_in = lane / C::CH, col = lane % C::CH;
+  bool more = true, first = true;
+  while (more) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const uint32_t row = i * C::RPW + row_in;
+      *(u32x4*)(st + k_at<D>(row, col)) = kr[i];
+      *(u32x4*)(st + C::TILE + v_at<D>(row, col)) = vr[i];
+    }
+    if (first) {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) qf[s] = qn[s];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) O[i] = f32x4{0, 0, 0, 0};
+      m = kNone, l = 0.0f;
+    }
+    // this tile's place, then the next one's
+    const int rows = n - t * kTailTile;
+    const bool last = t + 1 == t_end;
+    const long long index = (long long)P.B * P.Hq * P.splits +
+                            ((long long)b * P.Hq + kvh * P.R + c) * P.tail_splits + piece;
+    if (!last) {
+      ++t;
+    } else if (++at < end) {
+      if (at - seen >= in_b) {  // the next sequence with a tail
+        seen += in_b;
+        do {
+          if (++b == base + 64) base += 64, lens = lengths(base);
+          n = __builtin_amdgcn_readlane(lens, b - base);
+        } while (n == 0);
+        in_b = pieces_of(n) * P.Hkv;
+      }
+      open();
+      ask_q();
+    } else {
+      more = false;
+    }
+    if (more) ask();
+    wave_lds_sync();
+
+    f32x4 S[2] = {};
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+        S[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            *(const bf16x8*)(st + k_at<D>(a * 16 + c, 4 * s + g)), qf[s], S[a], 0, 0, 0);
+    if (rows < kTailTile) {  // absent tokens
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i / 4 * 16 + 4 * g + i % 4 >= rows) S[i / 4][i % 4] = -INFINITY;
+    }
+    float top = fmaxf(S[0][0], S[1][0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) top = fmaxf(fmaxf(S[0][i], S[1][i]), top);
+    top = over_groups(top, [](float a, float b) { return fmaxf(a, b); }) * scale;
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float m1 = top > m + kSlack ? top : m;
+      const float f = __builtin_amdgcn_exp2f(m - m1);
+      m = m1, l *= f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) O[i][j] *= f;
+    }
+    u32x4 p[PARTS];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+      weights<PARTS>(S[i / 4][i % 4], S[i / 4][i % 4 + 1], scale, m, l,
+                     [&](int k, uint32_t w) { p[k][i / 2] = w; });
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) {
+      i16x4 a[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4*)(st + C::TILE +
+                                                       v_at<D>(16 * k + 4 * g + (c >> 2), cb * 2 + ((c & 3) >> 1)) +
+                                                       8 * (c & 1)));
+      const bf16x8 vv =
+          __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int k = PARTS - 1; k >= 0; --k)
+        O[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, __builtin_bit_cast(bf16x8, p[k]), O[cb], 0, 0, 0);
+    }
+    wave_lds_sync();
+    if (last) {
+      const float sum = over_groups(l, [](float a, float b) { return a + b; });
+      if (c < P.R) {
+#pragma unroll
+        for (int cb = 0; cb < D / 16; ++cb) *(f32x4*)(P.acc + index * D + cb * 16 + 4 * g) = O[cb];
+        if (g == 0) *(f32x2*)(P.ml + index * 2) = f32x2{m, sum};
+      }
+    }
+    first = last;
+  }
+}
+
 // Of the forms by their number of wavefronts that share a tile.
-constexpr int form_waves(int wr) { return wr == 8 ? 8 : 4; }
 constexpr int form_tile(int wr) { return wr >= 4 ? 64 : 32; }
 constexpr int form_stages(int wr) { return wr >= 4 ? 2 : 1; }
 template <int D, int WR>
-using Form = Cfg<D, form_waves(WR), WR, form_tile(WR), form_stages(WR)>;
+using Form = Cfg<D, WR, form_tile(WR), form_stages(WR)>;
 
 template <int D, int WR>
 constexpr int shared_lds() {
-  constexpr int a = Form<D, WR>::LDS, b = Cfg<D, form_waves(WR), 1, kTailTile, 1>::STAGED;
+  constexpr int a = Form<D, WR>::LDS, b = Cfg<D, 1, kTailTile, 1>::STAGED;
   return a > b ? a : b;
 }
 
 template <int D, int WR, int PARTS>
-__global__ __launch_bounds__(64 * form_waves(WR), 2) void shared_kernel(SharedParams P) {
+__global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
   extern __shared__ __align__(16) unsigned char lds[];
-  constexpr int W = form_waves(WR);
-  const int id = blockIdx.x;
-  if (id < P.prefix_blocks) {
-    // the row blocks of a split share its keys and values: same id modulo the 8 XCDs
-    constexpr int kXcds = 8;
-    const int per = kXcds * P.row_blocks;
-    const int u = id / per * kXcds + id % kXcds, rb = id % per / kXcds;
-    if (u >= P.Hkv * P.splits) return;
-    const int kvh = u / P.splits, split = u % P.splits;
-    constexpr int T = form_tile(WR), WK = W / WR;
-    const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
-    const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
-    const int rows = P.B * P.R, row0 = rb * WR * kRows;
-    attend<D, W, WR, T, form_stages(WR), PARTS, false>(
-        P, lds, kvh, 0, 0, t0, t1,
-        [&](int r) -> const uint16_t* {
-          r += row0;
-          if (r >= rows) return nullptr;
-          return P.q + ((size_t)(r / P.R) * P.Hq + kvh * P.R + r % P.R) * D;
-        },
-        [&](int r) -> long long {
-          r += row0;
-          if (r >= rows) return -1;
-          return ((long long)(r / P.R) * P.Hq + kvh * P.R + r % P.R) * P.splits + split;
-        });
-  } else {  // a piece of a sequence's tail per wavefront
+  if ((int)blockIdx.x < P.tail_blocks) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = (id - P.prefix_blocks) * W + wave;
-    const int ts = i % P.tail_splits, s = i / P.tail_splits, kvh = s % P.Hkv, b = s / P.Hkv;
-    if (b >= P.B) return;
-    const int n = __builtin_amdgcn_readfirstlane(min(P.n_tail[b], P.tail_cap));
-    const int t0 = ts * P.tail_tiles;
-    const int tiles = (n + kTailTile - 1) / kTailTile;
-    if (t0 >= tiles) return;  // (n <= 0 among them)
-    const int t1 = min(tiles, t0 + P.tail_tiles);
-    attend<D, W, 1, kTailTile, 1, PARTS, true>(
-        P, lds, kvh, b, n, t0, t1,
-        [&](int r) -> const uint16_t* {
-          return r < P.R ? P.q + ((size_t)b * P.Hq + kvh * P.R + r) * D : nullptr;
-        },
-        [&](int r) -> long long {
-          if (r >= P.R) return -1;
-          return (long long)P.B * P.Hq * P.splits +
-                 ((long long)b * P.Hq + kvh * P.R + r) * P.tail_splits + ts;
-        });
+    tails<D, PARTS>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE, blockIdx.x * kWaves + wave,
+                    P.tail_blocks * kWaves);
+    return;
   }
+  // the row blocks of a split share its keys and values: same id modulo the 8 XCDs
+  const int id = blockIdx.x - P.tail_blocks;
+  const int each = kXcds * P.row_blocks;
+  const int u = id / each * kXcds + id % kXcds, rb = id % each / kXcds;
+  if (u >= P.Hkv * P.splits) return;
+  const int kvh = u / P.splits, split = u % P.splits;
+  constexpr int T = form_tile(WR), WK = kWaves / WR;
+  const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
+  const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
+  const int rows = P.B * P.R, row0 = rb * WR * kRows;
+  attend<D, WR, T, form_stages(WR), PARTS>(
+      P, lds, kvh, t0, t1,
+      [&](int r) -> const uint16_t* {
+        r += row0;
+        if (r >= rows) return nullptr;
+        return P.q + ((size_t)(r / P.R) * P.Hq + kvh * P.R + r % P.R) * D;
+      },
+      [&](int r) -> long long {
+        r += row0;
+        if (r >= rows) return -1;
+        return ((long long)(r / P.R) * P.Hq + kvh * P.R + r % P.R) * P.splits + split;
+      });
 }
 
 // Merges the partial results of a row in a fixed order: the prefix's splits, then those of the tail that
@@ -602,7 +759,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams P) {
 }
 
 struct SharedPlan {
-  int wr, row_blocks, splits, split_tiles, tail_splits, tail_tiles;
+  int wr, row_blocks, splits, split_tiles, tail_splits, tail_tiles, tail_blocks;
 };
 
 SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
@@ -610,32 +767,42 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   const long long rows = (long long)s.B * (s.Hq / s.Hkv);
   p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
   p.row_blocks = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
-  const int per = form_tile(p.wr) * (form_waves(p.wr) / p.wr);  // tokens of a tile of all groups
+  const int per = form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
   const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
+  const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
+  const long long streams = (long long)s.B * s.Hkv;
+  if (tail_cap > 0) {
+    // pieces for every wavefront of the chip where all tails are full, of 4 tiles at least: a piece's
+    // partial result is 1/8 of the bytes of one tile with 8 query rows
+    long long t = (streams * tail_max + 4 * 2048 - 1) / (4 * 2048);
+    if (t < 4) t = 4;
+    if (t > tail_max) t = tail_max;
+    p.tail_tiles = (int)t;
+    p.tail_splits = (tail_max + p.tail_tiles - 1) / p.tail_tiles;
+  }
   // The row blocks of a split stay on one of 8 XCDs of 32 compute units, so splits come in whole rounds
-  // of an XCD.  Of the splits that fill up to 4 rounds the cheapest: a tile of time for each tile of a
-  // split, two for starting and ending a workgroup, and the traffic of the partial results.
-  const int slots = 32 * (p.wr == 8 ? 1 : 2);
+  // of an XCD; the tails get compute units of their own from the start.  Of the ways to share these out,
+  // with splits that fill up to 4 rounds, the one that ends first: a tile of time for each tile of a
+  // split, two for starting and ending a workgroup, and the traffic of the partial results; a tail's
+  // tile, counted as half full, is half of one.
   double best = 0;
-  int splits = 1;
-  for (int rounds = 1; rounds <= 4; ++rounds) {
-    long long n = 8LL * (rounds * slots / p.row_blocks) / s.Hkv;
-    if (n < 1) continue;
-    if (n > tiles) n = tiles;
-    const double cost = rounds * ((tiles + n - 1) / n + 2.0) + n * (rows * s.Hkv * 1e-4);
-    if (best == 0 || cost < best) best = cost, splits = (int)n;
+  int splits = 1, tail_slots = tail_cap > 0 ? 1 : 0;
+  const int most = tail_cap > 0 ? (int)((streams * p.tail_splits + 8 * kWaves - 1) / (8 * kWaves)) : 0;
+  for (int ts = tail_slots; ts <= 31; ts += ts < 4 ? 1 : 4) {
+    const double tails = tail_cap > 0 ? 2.0 + 0.25 * streams * tail_max / (8.0 * kWaves * ts) : 0;
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+      long long n = (long long)kXcds * ((32 * rounds - ts) / p.row_blocks) / s.Hkv;
+      if (n < 1) continue;
+      if (n > tiles) n = tiles;
+      const double prefix = rounds * ((tiles + n - 1) / n + 2.0);
+      const double cost = (prefix > tails ? prefix : tails) + n * (rows * s.Hkv * 1e-4);
+      if (best == 0 || cost < best) best = cost, splits = (int)n, tail_slots = ts;
+    }
+    if (ts >= most) break;
   }
   p.split_tiles = (tiles + splits - 1) / splits;
   p.splits = (tiles + p.split_tiles - 1) / p.split_tiles;
-  if (tail_cap > 0) {
-    const int tt = (tail_cap + kTailTile - 1) / kTailTile;
-    const long long streams = (long long)s.B * s.Hkv;
-    long long per_wave = streams * tt / 4096;
-    if (per_wave < 1) per_wave = 1;
-    if (per_wave > tt) per_wave = tt;
-    p.tail_tiles = (int)per_wave;
-    p.tail_splits = (tt + p.tail_tiles - 1) / p.tail_tiles;
-  }
+  p.tail_blocks = kXcds * tail_slots;
   return p;
 }
 
@@ -644,22 +811,20 @@ size_t partials(const stc_shape_t& s, const SharedPlan& p) {
 }
 
 template <int D, int WR, int PARTS>
-int shared_go(const SharedParams& P, long long tail_waves, hipStream_t st) {
+int shared_go(const SharedParams& P, int blocks, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
-  constexpr int lds = shared_lds<D, WR>(), W = form_waves(WR);
+  constexpr int lds = shared_lds<D, WR>();
   if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS>, lds, done)) return -1;
-  const long long blocks = P.prefix_blocks + (tail_waves + W - 1) / W;
-  if (blocks * W > INT32_MAX) return -1;
-  shared_kernel<D, WR, PARTS><<<(unsigned)blocks, 64 * W, lds, st>>>(P);
+  shared_kernel<D, WR, PARTS><<<blocks, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 template <int D, int PARTS>
-int shared_rows(const SharedParams& P, int wr, long long tail_waves, hipStream_t st) {
-  return wr == 1   ? shared_go<D, 1, PARTS>(P, tail_waves, st)
-         : wr == 2 ? shared_go<D, 2, PARTS>(P, tail_waves, st)
-         : wr == 4 ? shared_go<D, 4, PARTS>(P, tail_waves, st)
-                   : shared_go<D, 8, PARTS>(P, tail_waves, st);
+int shared_rows(const SharedParams& P, int wr, int blocks, hipStream_t st) {
+  return wr == 1   ? shared_go<D, 1, PARTS>(P, blocks, st)
+         : wr == 2 ? shared_go<D, 2, PARTS>(P, blocks, st)
+         : wr == 4 ? shared_go<D, 4, PARTS>(P, blocks, st)
+                   : shared_go<D, 8, PARTS>(P, blocks, st);
 }
 
 }  // namespace
@@ -685,13 +850,14 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   P.row_blocks = p.row_blocks, P.splits = p.splits, P.split_tiles = p.split_tiles;
   P.tail_splits = p.tail_splits, P.tail_tiles = p.tail_tiles > 0 ? p.tail_tiles : 1;
   P.out_bf16 = out_bf16;
-  const long long units = (s.Hkv * (long long)p.splits + 7) / 8 * 8;
-  P.prefix_blocks = (int)(units * p.row_blocks);
-  const long long tail_waves = (long long)s.B * s.Hkv * p.tail_splits;
-  const int rc = s.D == 128 ? (out_bf16 ? shared_rows<128, 1>(P, p.wr, tail_waves, st)
-                                        : shared_rows<128, 2>(P, p.wr, tail_waves, st))
-                            : (out_bf16 ? shared_rows<64, 1>(P, p.wr, tail_waves, st)
-                                        : shared_rows<64, 2>(P, p.wr, tail_waves, st));
+  const long long units = (s.Hkv * (long long)p.splits + kXcds - 1) / kXcds * kXcds;
+  if (units * p.row_blocks > (1 << 30)) return -1;
+  P.tail_blocks = p.tail_blocks;
+  const int blocks = (int)(units * p.row_blocks) + p.tail_blocks;
+  const int rc = s.D == 128 ? (out_bf16 ? shared_rows<128, 1>(P, p.wr, blocks, st)
+                                        : shared_rows<128, 2>(P, p.wr, blocks, st))
+                            : (out_bf16 ? shared_rows<64, 1>(P, p.wr, blocks, st)
+                                        : shared_rows<64, 2>(P, p.wr, blocks, st));
   if (rc) return -1;
   const int rows = s.B * s.Hq;
   const int wpr = p.splits + p.tail_splits > 16 ? 4 : 1;
