@@ -101,11 +101,11 @@ struct Cfg {
   static constexpr int TP = T / kPage;        // pages of a tile
   static constexpr int RB = D * 2;            // bytes of a row
   static constexpr int TILE = T * RB;         // a K or V tile
-  static constexpr int META = 2 * TILE;       // offset of (offset, mask) of the T tokens of another tile
-  static constexpr int STAGE = 2 * TILE + T * 8;
+  static constexpr int STAGE = 2 * TILE;      // a power of two
+  static constexpr int META = T * 8;          // packed offset and mask of the tokens of a tile
   static constexpr int MROW = D + 4;          // floats of a row in the merge of the groups
   static constexpr int MERGE = WK > 1 ? kWaves * (kRows * MROW * 4 + kRows * 8) : 0;
-  static constexpr int STAGED = WK * STAGES * STAGE;
+  static constexpr int STAGED = WK * STAGES * (STAGE + META);
   static constexpr int LDS = STAGED > MERGE ? STAGED : MERGE;
 };
 
@@ -144,7 +144,6 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wave / WR, wr = wave % WR;
   const int c = lane & 31, half = lane >> 5;
-  unsigned char* my = lds + grp * STAGES * C::STAGE;
 
   // the stream
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G));  // log2(pieces per value group)
@@ -154,7 +153,9 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const uint16_t* mask_s = P.mask + (size_t)kvh * P.Ncap;
   const uint32_t* off_s = P.off + (size_t)kvh * (P.Ncap + 1);
   const int32_t* pages = P.pages ? P.pages + (size_t)kvh * P.k_pages : nullptr;
-  const int tokens = min(P.N, P.k_pages * kPage);  // without a list: the first so many are attended
+  // Tiles behind the last one are empty.  Without a list the first `tokens` tokens are attended.
+  const int end_page = min(P.k_pages, tile1 * C::WK * C::TP);
+  const int tokens = min(P.N, end_page * kPage);
 
   // query rows: operand of S^T, 8 channels of k-step s per lane
   bf16x8 qf[D / 16];
@@ -175,14 +176,13 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const uint32_t grp_of = piece >> lg_upg, bit = 1u << grp_of;
   const uint32_t within = (piece & ((1u << lg_upg) - 1u)) << 4;
   u32x4 kr[C::NI], vr[C::NI];
-  u32x2 meta;  // packed offset and mask of token `lane` of a tile
 
   // With a list, lane j holds page j of a tile, -1 if there is none.
   auto ask_pages = [&](int tile) {
     int pg = -1;
     if (pages) {
       const int at = tile * C::TP + lane;
-      if (lane < C::TP && at < P.k_pages) pg = pages[at];
+      if (lane < C::TP && at < end_page) pg = pages[at];
       if ((unsigned)pg >= (unsigned)P.NP) pg = -1;
     }
     return pg;
@@ -218,23 +218,28 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       const int pg = __shfl(pgv, lane / kPage);
       t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
     }
-    meta = u32x2{0u, 0u};
-    if (lane < T && t < (pages ? P.N : tokens)) meta = u32x2{off_s[t], mask_s[t]};
+    u32x2 e = {0u, 0u};
+    if (lane < T && t < (pages ? P.N : tokens)) e = u32x2{off_s[t], mask_s[t]};
+    return e;
   };
-  auto put_meta = [&](unsigned char* st) {
-    if (lane < T) *(u32x2*)(st + C::META + lane * 8) = meta;
+  unsigned char* const metas = lds + C::WK * STAGES * C::STAGE + grp * STAGES * C::META;
+  auto put_meta = [&](int slot, u32x2 e) {
+    if (lane < T) *(u32x2*)(metas + slot * C::META + lane * 8) = e;
   };
-  auto ask_data = [&](int tile, int pgv, const unsigned char* st) {
+  u32x2 e[C::NI];  // this thread's rows of a tile: packed offset, mask
+  auto get_meta = [&](int slot) {
+#pragma unroll
+    for (int i = 0; i < C::NI; ++i)
+      e[i] = *(const u32x2*)(metas + slot * C::META + (i * C::RPI + row0 + row_in) * 8);
+  };
+  auto ask_keys = [&](int tile, int pgv) {
     each([&](int i, int r, int base) {
       const int n = rows_left(tile, pgv, base) * C::RB;
       const size_t t = first_token(tile, pgv, base) * C::RB;
-      const uint32_t at = (r - base) * C::RB + lane * 16;
-      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Ks + t, n), at, 0, 0);
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Ks + t, n), (r - base) * C::RB + lane * 16, 0, 0);
     });
-    u32x2 e[C::NI];
-#pragma unroll
-    for (int i = 0; i < C::NI; ++i)
-      e[i] = *(const u32x2*)(st + C::META + (i * C::RPI + row0 + row_in) * 8);
+  };
+  auto ask_values = [&]() {
     each([&](int i, int r, int base) {
       // values are addressed from those of the base row on: a tile's lie within T * G groups
       const uint32_t off0 = __builtin_amdgcn_readfirstlane(e[r == base ? i : 0][0]);
@@ -246,13 +251,27 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
           rsrc(Vs + ((size_t)(room < 0 ? 0 : off0) << lg_group), groups << lg_group), at, 0, 0);
     });
   };
-  auto put_data = [&](unsigned char* st) {
+  auto ask_data = [&](int tile, int pgv, int slot) {
+    get_meta(slot);
+    ask_keys(tile, pgv);
+    ask_values();
+  };
+
+  // Offsets in shared memory, of one stage; STAGE apart from those of the other
+  const uint32_t mine = grp * STAGES * C::STAGE;
+  uint32_t pk[C::NI], pv[C::NI];
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) {
-      const uint32_t row = i * C::RPI + row0 + row_in;
-      *(u32x4*)(st + k_at<D>(row, piece)) = kr[i];
-      *(u32x4*)(st + C::TILE + v_at<D>(row, piece)) = vr[i];
-    }
+  for (int i = 0; i < C::NI; ++i) {
+    const uint32_t row = i * C::RPI + row0 + row_in;
+    pk[i] = mine + k_at<D>(row, piece), pv[i] = mine + C::TILE + v_at<D>(row, piece);
+  }
+  auto put_keys = [&] {
+#pragma unroll
+    for (int i = 0; i < C::NI; ++i) *(u32x4*)(lds + pk[i]) = kr[i];
+  };
+  auto put_values = [&] {
+#pragma unroll
+    for (int i = 0; i < C::NI; ++i) *(u32x4*)(lds + pv[i]) = vr[i];
   };
 
   f32x16 O[D / 32];
@@ -266,43 +285,32 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   // K operand: token c of a subtile, pieces 2 s + half
   uint32_t ka[D / 16];
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) ka[s] = k_at<D>(c, 2 * s + half);
+  for (int s = 0; s < D / 16; ++s) ka[s] = mine + k_at<D>(c, 2 * s + half);
   // V operand: lane j of 16 addresses row j/4, channels 4 (j%4) .. of a block of 4 rows by 16 channels
   // and receives channel j of the four rows
   const int j16 = lane & 15;
   uint32_t va[D / 32];
 #pragma unroll
   for (int cb = 0; cb < D / 32; ++cb)
-    va[cb] = C::TILE + v_at<D>(4 * half + (j16 >> 2), cb * 4 + ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1)) +
+    va[cb] = mine + C::TILE + v_at<D>(4 * half + (j16 >> 2), cb * 4 + ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1)) +
              8 * (j16 & 1);
 
-  auto compute = [&](const unsigned char* st, int tile, int pgv) {
-    constexpr int SUBS = T / 32;
-    f32x16 S[SUBS] = {};
+  // S^T of a subtile's 32 tokens: register 4 a + i of a lane is token 8 a + 4 half + i.
+  auto largest = [&](const f32x16& S) {
+    float top = fmaxf(S[0], S[1]);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s)
+    for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(S[i], S[i + 1]), top);
+    return top;
+  };
+  auto absent = [&](f32x16& S, int n0, int n1) {  // tokens of either page that are there
 #pragma unroll
-      for (int sub = 0; sub < SUBS; ++sub) {
-        const bf16x8 a = *(const bf16x8*)(st + ka[s] + sub * 32 * C::RB);
-        S[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[s], S[sub], 0, 0, 0);
-      }
-    // register 4 a + i of a lane is token 8 a + 4 half + i of the subtile
-    float top = -INFINITY;
-#pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub) {
-      const int n0 = rows_left(tile, pgv, sub * 32);
-      const int n1 = !pages ? n0 - kPage : rows_left(tile, pgv, sub * 32 + kPage);
-      if (n0 < kPage || n1 < kPage) {  // absent tokens
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 8 * (i / 4 % 2) + i % 4 + 4 * half;
-          if (at >= (i < 8 ? n0 : n1)) S[sub][i] = -INFINITY;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(S[sub][i], S[sub][i + 1]), top);
+    for (int i = 0; i < 16; ++i) {
+      const int at = 8 * (i / 4 % 2) + i % 4 + 4 * half;
+      if (at >= (i < 8 ? n0 : n1)) S[i] = -INFINITY;
     }
-    top = max_halves(top) * scale;
+  };
+  // The running maximum takes a subtile's largest logit in.
+  auto take_top = [&](float top) {
     if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
       const float m1 = top > m + kSlack ? top : m;  // (other rows' maxima do not matter to a row)
       const float f = __builtin_amdgcn_exp2f(m - m1);
@@ -312,31 +320,88 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 #pragma unroll
         for (int j = 0; j < 16; ++j) O[i][j] *= f;
     }
+  };
+  auto value = [&](int sub, int cb, int ks) {  // operand of O^T
+    i16x4 a[2];
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub) {
-      u32x4 p[PARTS][2];
-#pragma unroll
-      for (int i = 0; i < 16; i += 2)
-        weights<PARTS>(S[sub][i], S[sub][i + 1], scale, m, l,
+    for (int k = 0; k < 2; ++k)
+      a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) i16x4*)(lds + va[cb] + (sub * 32 + 16 * ks + 8 * k) * C::RB));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // One subtile, and the logits of the next (NEXT): the products with the next one's keys, which depend on
+  // nothing, stand between the exponentials of this one, and the next one's maximum between the products
+  // with this one's values.  A matrix instruction takes 32 cycles of its unit and 4 of the wavefront's
+  // issue, so 6 or 7 vector instructions fit behind each.  Operands are read two products ahead.  The
+  // compiler, left to itself, gathers the reads in front and spills; sched_barrier keeps the order.
+  // between(product) is the tile's other work, done between the products too.
+  auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, int tile1, int pgv1, auto between) {
+    constexpr int QK = D / 16, PV = D / 16, PER = 16 / QK;  // products of either kind, weights for each
+    u32x4 p[PARTS][2];
+    f32x16 N = {};
+    bf16x8 kf[3], vf[3];
+    auto read_k = [&](auto s) { kf[s % 3] = *(const bf16x8*)(lds + ka[s] + sub1 * 32 * C::RB); };
+    auto read_v = [&](auto s) { vf[s % 3] = value(sub, s % (D / 32), s / (D / 32)); };
+    auto weigh = [&](auto s) {
+      static_for<0, PER / 2>([&](auto j) {
+        constexpr int i = PER * s + 2 * j;
+        weights<PARTS>(S[i], S[i + 1], scale, m, l,
                        [&](int k, uint32_t w) { p[k][i / 8][i % 8 / 2] = w; });
+      });
+    };
+    if constexpr (NEXT) read_k(IC<0>{}), read_k(IC<1>{});
+    __builtin_amdgcn_sched_barrier(0);
+    weigh(IC<0>{});
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, QK>([&](auto s) {
+      if constexpr (NEXT) {
+        if constexpr (s + 2 < QK) read_k(IC<s + 2>{});
+        N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s % 3], qf[s], N, 0, 0, 0);
+      }
+      if constexpr (s + 1 < QK) weigh(IC<s + 1>{});
+      if constexpr (s + 2 == QK) read_v(IC<0>{});
+      if constexpr (s + 1 == QK) read_v(IC<1>{});
+      between(s);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    float top = 0.0f;
+    static_for<0, PV>([&](auto s) {
+      if constexpr (s + 2 < PV) read_v(IC<s + 2>{});
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int k = PARTS - 1; k >= 0; --k)
+        O[s % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            vf[s % 3], __builtin_bit_cast(bf16x8, p[k][s / (D / 32)]), O[s % (D / 32)], 0, 0, 0);
+      if constexpr (NEXT) {  // the products of N are through after two more
+        if constexpr (s == 2) top = fmaxf(N[0], N[1]);
+        if constexpr (s >= 2 && s < PV - 1) {
+          constexpr int STEPS = PV - 3, FROM = 2 + 14 * (s - 2) / STEPS / 2 * 2,
+                        TO = 2 + 14 * (s - 1) / STEPS / 2 * 2;
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) {
-          i16x4 a[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3)))
-                 i16x4*)(st + va[cb] + (sub * 32 + 16 * ks + 8 * k) * C::RB));
-          const bf16x8 vv = __builtin_bit_cast(
-              bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k)
-            O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, p[k][ks]),
-                                                            O[cb], 0, 0, 0);
+          for (int i = FROM; i < TO; i += 2) top = fmaxf(fmaxf(N[i], N[i + 1]), top);
         }
+      }
+      between(IC<QK + s>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (NEXT) {
+      const int n0 = rows_left(tile1, pgv1, sub1 * 32);
+      const int n1 = !pages ? n0 - kPage : rows_left(tile1, pgv1, sub1 * 32 + kPage);
+      if (n0 < kPage || n1 < kPage) absent(N, n0, n1), top = largest(N);
+      S = N;
+      take_top(max_halves(top) * scale);
     }
+  };
+  // Logits of a subtile on their own.
+  auto logits = [&](f32x16& S, int tile, int pgv) {
+    f32x16 N = {};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(lds + ka[s]), qf[s], N, 0, 0, 0);
+    const int n0 = rows_left(tile, pgv, 0);
+    const int n1 = !pages ? n0 - kPage : rows_left(tile, pgv, kPage);
+    if (n0 < kPage || n1 < kPage) absent(N, n0, n1);
+    S = N;
+    take_top(max_halves(largest(N)) * scale);
   };
 
   // Pages are asked for four tiles ahead, masks and offsets three, keys and values one.
@@ -348,62 +413,70 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const bool has_meta = wr == 0;  // the group's wavefront that fetches them
   int pg0 = ask_pages(tile_of(tile0)), pg1 = ask_pages(tile_of(tile0 + 1));
   int pg2 = ask_pages(tile_of(tile0 + 2)), pg3 = ask_pages(tile_of(tile0 + 3));
-  // the second half of a stage's meta data belongs to the tile after the one whose data it holds
-  unsigned char* const st1 = my + (STAGES - 1) * C::STAGE;
-  u32x2 meta1 = {0u, 0u};
+  u32x2 meta1 = {0u, 0u}, meta2 = {0u, 0u};  // of tiles t + 1 (then t + 2) and t + 2 (t + 3)
   if (has_meta) {
-    ask_meta(tile_of(tile0), pg0);
-    const u32x2 first = meta;
-    ask_meta(tile_of(tile0 + 1), pg1);
-    meta1 = meta;
-    ask_meta(tile_of(tile0 + 2), pg2);
-    const u32x2 third = meta;
-    meta = first;
-    put_meta(st1);
-    meta = third;
+    const u32x2 meta0 = ask_meta(tile_of(tile0), pg0);
+    meta1 = ask_meta(tile_of(tile0 + 1), pg1);
+    meta2 = ask_meta(tile_of(tile0 + 2), pg2);
+    put_meta(0, meta0);
   }
   sync();
-  ask_data(tile_of(tile0), pg0, st1);
+  ask_data(tile_of(tile0), pg0, 0);
   if constexpr (STAGES == 1) sync();
-  auto next_meta = [&](int t, unsigned char* st) {  // of tile t + 1 to shared memory, of t + 3 asked for
+  auto next_meta = [&](int t, int slot) {  // of tile t + 1 to shared memory, of t + 3 asked for
     if (has_meta) {
-      const u32x2 later = meta;
-      meta = meta1;
-      put_meta(st);
-      meta1 = later;
-      ask_meta(tile_of(t + 3), pg3);
+      put_meta(slot, meta1);
+      meta1 = meta2;
+      meta2 = ask_meta(tile_of(t + 3), pg3);
     }
+    const int pg4 = ask_pages(tile_of(t + 4));
+    pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
   };
+  f32x16 S;
   if constexpr (STAGES == 2) {
-    put_data(my);
-    next_meta(tile0, my);
-    __syncthreads();
-    auto turn = [&](int t, auto stage) {
-      unsigned char *const here = my + stage * C::STAGE, *const there = my + (1 - stage) * C::STAGE;
-      if (t + 1 < tile1) ask_data(tile_of(t + 1), pg1, here);
-      const int pg4 = ask_pages(tile_of(t + 4));
-      compute(here, tile_of(t), pg0);
-      if (t + 1 < tile1) {
-        put_data(there);
-        pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
-        next_meta(t + 1, there);
-      }
-      __syncthreads();
+    // A tile's second half needs the next tile's keys, so that one has to be there by then: it is stored
+    // in front of the first half, when nobody reads the tile before any more.
+    auto flip = [&](auto& a) {
+#pragma unroll
+      for (uint32_t& x : a) x ^= C::STAGE;
     };
-    for (int t = tile0; t < tile1; t += 2) {
-      turn(t, IC<0>{});
-      if (t + 1 < tile1) turn(t + 1, IC<1>{});
+    put_keys(), put_values();
+    flip(pk), flip(pv);
+    int pgt = pg0;
+    next_meta(tile0, 1);
+    __syncthreads();
+    ask_data(tile_of(tile0 + 1), pg0, 1);
+    logits(S, tile_of(tile0), pgt);
+    for (int t = tile0; t < tile1; ++t) {
+      const int slot = (t - tile0) & 1;
+      const int pgn = pg0;
+      constexpr int QK = D / 16;
+      block(IC<1>{}, S, 0, 1, tile_of(t), pgt, [&](auto s) {
+        if constexpr (s == 1) put_keys();
+        if constexpr (s == QK / 2) put_values();
+        if constexpr (s == QK + 1) next_meta(t + 1, slot);
+      });
+      flip(pk), flip(pv), flip(ka);
+      __syncthreads();
+      block(IC<1>{}, S, 1, 0, tile_of(t + 1), pgn, [&](auto s) {
+        if constexpr (s == 1) get_meta(slot);
+        if constexpr (s == QK / 2) ask_keys(tile_of(t + 2), pg0);
+        if constexpr (s == QK) ask_values();
+      });
+      flip(va);
+      __syncthreads();
+      pgt = pgn;
     }
   } else {
     for (int t = tile0; t < tile1; ++t) {
-      put_data(my);
-      next_meta(t, my);
+      put_keys(), put_values();
+      const int pgt = pg0;
+      next_meta(t, 0);
       sync();
-      if (t + 1 < tile1) ask_data(tile_of(t + 1), pg1, my);
-      const int pg4 = ask_pages(tile_of(t + 4));
-      compute(my, tile_of(t), pg0);
+      ask_data(tile_of(t + 1), pg0, 0);
+      logits(S, tile_of(t), pgt);
+      block(IC<0>{}, S, 0, 0, 0, 0, [](auto) {});
       sync();
-      pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
     }
   }
   l = sum_halves(l);
@@ -423,13 +496,13 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   } else {
     __syncthreads();
     constexpr int BUF = kRows * C::MROW * 4;
-    float* mine = (float*)(lds + wave * BUF);
+    float* own = (float*)(lds + wave * BUF);
     f32x2* mls = (f32x2*)(lds + kWaves * BUF);
 #pragma unroll
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
       for (int a = 0; a < 4; ++a)
-        *(f32x4*)(mine + c * C::MROW + cb * 32 + 8 * a + 4 * half) =
+        *(f32x4*)(own + c * C::MROW + cb * 32 + 8 * a + 4 * half) =
             f32x4{O[cb][4 * a], O[cb][4 * a + 1], O[cb][4 * a + 2], O[cb][4 * a + 3]};
     if (half == 0) mls[wave * kRows + c] = f32x2{m, l};
     __syncthreads();
@@ -772,10 +845,10 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
   const long long streams = (long long)s.B * s.Hkv;
   if (tail_cap > 0) {
-    // pieces for every wavefront of the chip where all tails are full, of 4 tiles at least: a piece's
-    // partial result is 1/8 of the bytes of one tile with 8 query rows
+    // 4 pieces for every wavefront of the chip where all tails are full, but not so small that their
+    // partial results pass 1/16 of their keys and values
     long long t = (streams * tail_max + 4 * 2048 - 1) / (4 * 2048);
-    if (t < 4) t = 4;
+    if (t < (s.Hq / s.Hkv + 1) / 2) t = (s.Hq / s.Hkv + 1) / 2;
     if (t > tail_max) t = tail_max;
     p.tail_tiles = (int)t;
     p.tail_splits = (tail_max + p.tail_tiles - 1) / p.tail_tiles;
@@ -789,7 +862,7 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   int splits = 1, tail_slots = tail_cap > 0 ? 1 : 0;
   const int most = tail_cap > 0 ? (int)((streams * p.tail_splits + 8 * kWaves - 1) / (8 * kWaves)) : 0;
   for (int ts = tail_slots; ts <= 31; ts += ts < 4 ? 1 : 4) {
-    const double tails = tail_cap > 0 ? 2.0 + 0.25 * streams * tail_max / (8.0 * kWaves * ts) : 0;
+    const double tails = tail_cap > 0 ? 2.0 + 0.6 * streams * tail_max / (8.0 * kWaves * ts) : 0;
     for (int rounds = 1; rounds <= 4; ++rounds) {
       long long n = (long long)kXcds * ((32 * rounds - ts) / p.row_blocks) / s.Hkv;
       if (n < 1) continue;
