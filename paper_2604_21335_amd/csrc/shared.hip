@@ -40,7 +40,8 @@ struct SharedParams {
   const int32_t* n_tail;
   float *acc, *ml;  // partial results: weighted value sums [index][D], (maximum, sum of weights)
   void* out;
-  long long cap;
+  long long v_stride;  // value groups of a KV head
+  uint32_t cap;        // the same, as far as 32-bit offsets reach
   int B, R, Hq, Hkv, N, NP, G, Ncap, k_pages, tail_cap;
   int row_blocks, splits, split_tiles;  // prefix: tiles (of all key groups) per split
   int tail_splits, tail_tiles, tail_blocks;
@@ -130,14 +131,16 @@ __device__ __forceinline__ uint32_t v_at(uint32_t row, uint32_t piece) {
 // tokens and dropped value groups need no branch.
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 __device__ __forceinline__ Rsrc rsrc(const void* base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+  // (clamped numbers come out of vector instructions: back to a scalar register)
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readfirstlane(bytes),
+                                           0x00027000);
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset behind every end
 
 // Tiles [tile0, tile1) of the prefix for the query rows q_row(0 ..) of one KV head; tile t of key group
 // g is tile t * WK + g.  The groups' results are merged; the partial result of row r goes to index(r)
 // (negative: nowhere).
-template <int D, int WR, int T, int STAGES, int PARTS, class Row, class Index>
+template <int D, int WR, int T, int STAGES, int PARTS, bool LIST, class Row, class Index>
 __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int tile0,
                                        int tile1, Row q_row, Index index) {
   using C = Cfg<D, WR, T, STAGES>;
@@ -149,10 +152,10 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G));  // log2(pieces per value group)
   const int lg_group = lg_upg + 4;                           // log2(bytes per value group)
   const unsigned char* Ks = P.K + (size_t)kvh * P.Ncap * C::RB;
-  const unsigned char* Vs = P.v + ((size_t)kvh * P.cap << lg_group);
+  const unsigned char* Vs = P.v + ((size_t)kvh * P.v_stride << lg_group);
   const uint16_t* mask_s = P.mask + (size_t)kvh * P.Ncap;
   const uint32_t* off_s = P.off + (size_t)kvh * (P.Ncap + 1);
-  const int32_t* pages = P.pages ? P.pages + (size_t)kvh * P.k_pages : nullptr;
+  const int32_t* pages = LIST ? P.pages + (size_t)kvh * P.k_pages : nullptr;
   // Tiles behind the last one are empty.  Without a list the first `tokens` tokens are attended.
   const int end_page = min(P.k_pages, tile1 * C::WK * C::TP);
   const int tokens = min(P.N, end_page * kPage);
@@ -177,50 +180,45 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const uint32_t within = (piece & ((1u << lg_upg) - 1u)) << 4;
   u32x4 kr[C::NI], vr[C::NI];
 
-  // With a list, lane j holds page j of a tile, -1 if there is none.
-  auto ask_pages = [&](int tile) {
-    int pg = -1;
-    if (pages) {
-      const int at = tile * C::TP + lane;
-      if (lane < C::TP && at < end_page) pg = pages[at];
-      if ((unsigned)pg >= (unsigned)P.NP) pg = -1;
-    }
-    return pg;
+  // What a tile's requests go by.  With a list, lane j holds page j of the tile, -1 if there is none.
+  struct Tile {
+    int at, page;
+    bool ragged;  // some of its tokens are absent
   };
-  // Tokens of page j of a tile; of the rows r .. of a tile up to its end (or the page's, with a list)
-  auto rows_left = [&](int tile, int pgv, int r) {
-    if (pages) {
-      const int pg = __builtin_amdgcn_readlane(pgv, r / kPage);
+  auto look = [&](int tile) {
+    Tile x{tile, -1, false};
+    if constexpr (LIST) {
+      const int at = tile * C::TP + lane;
+      if (lane < C::TP && at < end_page) x.page = pages[at];
+      if ((unsigned)x.page >= (unsigned)P.NP) x.page = -1;
+      x.ragged = __builtin_amdgcn_ballot_w64(lane < C::TP && (x.page < 0 || x.page == P.NP - 1)) != 0;
+    } else {
+      x.ragged = (tile + 1) * T > tokens;
+    }
+    return x;
+  };
+  // Tokens from row r of a tile on that are there, up to the tile's end (the page's, with a list)
+  auto rows_left = [&](const Tile& x, int r) {
+    if constexpr (LIST) {
+      const int pg = __builtin_amdgcn_readlane(x.page, r / kPage);
       return pg < 0 ? 0 : max(0, min(kPage, P.N - pg * kPage) - r % kPage);
     }
-    return max(0, min(T, tokens - tile * T) - r);
-  };
-  auto first_token = [&](int tile, int pgv, int r) -> size_t {
-    if (pages)
-      return (size_t)max(__builtin_amdgcn_readlane(pgv, r / kPage), 0) * kPage + r % kPage;
-    return (size_t)tile * T + r;
-  };
-  // For every load of a tile: f(number of the load, its row in the tile, the row that the base address
-  // stands for).  Without a list a tile is one piece of memory and has one base.
-  auto each = [&](auto f) {
-    if (pages) {
-#pragma unroll
-      for (int i = 0; i < C::NI; ++i) f(i, i * C::RPI + row0, i * C::RPI + row0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::NI; ++i) f(i, i * C::RPI + row0, row0);
-    }
+    return max(0, min(T, tokens - x.at * T) - r);
   };
   // Masks and offsets: one request of a wavefront for a tile, handed to all through shared memory.
-  auto ask_meta = [&](int tile, int pgv) {
-    long long t = (long long)tile * T + lane;
-    if (pages) {
-      const int pg = __shfl(pgv, lane / kPage);
-      t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
+  auto ask_meta = [&](const Tile& x) {
+    if constexpr (LIST) {
+      const int pg = __shfl(x.page, lane / kPage);
+      const long long t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
+      u32x2 e = {0u, 0u};
+      if (lane < T && t < P.N) e = u32x2{off_s[t], mask_s[t]};
+      return e;
+    } else {
+      const int n = rows_left(x, 0);
+      const size_t t = (size_t)x.at * T;
+      return u32x2{__builtin_amdgcn_raw_buffer_load_b32(rsrc(off_s + t, n * 4), lane * 4, 0, 0),
+                   __builtin_amdgcn_raw_buffer_load_b16(rsrc(mask_s + t, n * 2), lane * 2, 0, 0)};
     }
-    u32x2 e = {0u, 0u};
-    if (lane < T && t < (pages ? P.N : tokens)) e = u32x2{off_s[t], mask_s[t]};
-    return e;
   };
   unsigned char* const metas = lds + C::WK * STAGES * C::STAGE + grp * STAGES * C::META;
   auto put_meta = [&](int slot, u32x2 e) {
@@ -232,29 +230,40 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     for (int i = 0; i < C::NI; ++i)
       e[i] = *(const u32x2*)(metas + slot * C::META + (i * C::RPI + row0 + row_in) * 8);
   };
-  auto ask_keys = [&](int tile, int pgv) {
-    each([&](int i, int r, int base) {
-      const int n = rows_left(tile, pgv, base) * C::RB;
-      const size_t t = first_token(tile, pgv, base) * C::RB;
-      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(Ks + t, n), (r - base) * C::RB + lane * 16, 0, 0);
-    });
+  auto ask_keys = [&](const Tile& x) {
+    if constexpr (LIST) {
+#pragma unroll
+      for (int i = 0; i < C::NI; ++i) {
+        const int r = i * C::RPI + row0;
+        const int pg = max(__builtin_amdgcn_readlane(x.page, r / kPage), 0);
+        kr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+            rsrc(Ks + ((size_t)pg * kPage + r % kPage) * C::RB, rows_left(x, r) * C::RB), lane * 16, 0, 0);
+      }
+    } else {  // a tile is one piece of memory
+      const Rsrc k = rsrc(Ks + (size_t)x.at * T * C::RB, rows_left(x, 0) * C::RB);
+#pragma unroll
+      for (int i = 0; i < C::NI; ++i)
+        kr[i] = __builtin_amdgcn_raw_buffer_load_b128(k, (i * C::RPI + row0) * C::RB + lane * 16, 0, 0);
+    }
+  };
+  // The values of the groups from `first` on, `most` of them at most
+  auto values_at = [&](uint32_t first, uint32_t most) {
+    const uint32_t room = __builtin_amdgcn_readfirstlane(P.cap > first ? P.cap - first : 0u);
+    return rsrc(Vs + ((size_t)(room ? first : 0u) << lg_group), min(room, most) << lg_group);
   };
   auto ask_values = [&]() {
-    each([&](int i, int r, int base) {
-      // values are addressed from those of the base row on: a tile's lie within T * G groups
-      const uint32_t off0 = __builtin_amdgcn_readfirstlane(e[r == base ? i : 0][0]);
-      const long long room = P.cap - (long long)off0;
-      const uint32_t groups = room < 0 ? 0 : room > T * 16 ? T * 16 : (uint32_t)room;
+    Rsrc v;
+    uint32_t off0 = 0;
+#pragma unroll
+    for (int i = 0; i < C::NI; ++i) {
+      if (LIST || i == 0) {  // addressed from the first row's on: a tile's values lie within T * G groups
+        off0 = __builtin_amdgcn_readfirstlane(e[i][0]);
+        v = values_at(off0, T * 16);
+      }
       const uint32_t slot = e[i][0] - off0 + __popc(e[i][1] & (bit - 1u));
       const uint32_t at = (e[i][1] & bit) ? (slot << lg_group) + within : kNowhere;
-      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(
-          rsrc(Vs + ((size_t)(room < 0 ? 0 : off0) << lg_group), groups << lg_group), at, 0, 0);
-    });
-  };
-  auto ask_data = [&](int tile, int pgv, int slot) {
-    get_meta(slot);
-    ask_keys(tile, pgv);
-    ask_values();
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(v, at, 0, 0);
+    }
   };
 
   // Offsets in shared memory, of one stage; STAGE apart from those of the other
@@ -302,7 +311,8 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(S[i], S[i + 1]), top);
     return top;
   };
-  auto absent = [&](f32x16& S, int n0, int n1) {  // tokens of either page that are there
+  auto hide = [&](f32x16& S, const Tile& x, int sub) {  // absent tokens
+    const int n0 = rows_left(x, sub * 32), n1 = LIST ? rows_left(x, sub * 32 + kPage) : n0 - kPage;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int at = 8 * (i / 4 % 2) + i % 4 + 4 * half;
@@ -335,7 +345,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   // issue, so 6 or 7 vector instructions fit behind each.  Operands are read two products ahead.  The
   // compiler, left to itself, gathers the reads in front and spills; sched_barrier keeps the order.
   // between(product) is the tile's other work, done between the products too.
-  auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, int tile1, int pgv1, auto between) {
+  auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, const Tile& x1, auto between) {
     constexpr int QK = D / 16, PV = D / 16, PER = 16 / QK;  // products of either kind, weights for each
     u32x4 p[PARTS][2];
     f32x16 N = {};
@@ -384,22 +394,18 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (NEXT) {
-      const int n0 = rows_left(tile1, pgv1, sub1 * 32);
-      const int n1 = !pages ? n0 - kPage : rows_left(tile1, pgv1, sub1 * 32 + kPage);
-      if (n0 < kPage || n1 < kPage) absent(N, n0, n1), top = largest(N);
+      if (x1.ragged) hide(N, x1, sub1), top = largest(N);
       S = N;
       take_top(max_halves(top) * scale);
     }
   };
   // Logits of a subtile on their own.
-  auto logits = [&](f32x16& S, int tile, int pgv) {
+  auto logits = [&](f32x16& S, const Tile& x) {
     f32x16 N = {};
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
       N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(lds + ka[s]), qf[s], N, 0, 0, 0);
-    const int n0 = rows_left(tile, pgv, 0);
-    const int n1 = !pages ? n0 - kPage : rows_left(tile, pgv, kPage);
-    if (n0 < kPage || n1 < kPage) absent(N, n0, n1);
+    if (x.ragged) hide(N, x, 0);
     S = N;
     take_top(max_halves(largest(N)) * scale);
   };
@@ -411,26 +417,26 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     else __syncthreads();
   };
   const bool has_meta = wr == 0;  // the group's wavefront that fetches them
-  int pg0 = ask_pages(tile_of(tile0)), pg1 = ask_pages(tile_of(tile0 + 1));
-  int pg2 = ask_pages(tile_of(tile0 + 2)), pg3 = ask_pages(tile_of(tile0 + 3));
-  u32x2 meta1 = {0u, 0u}, meta2 = {0u, 0u};  // of tiles t + 1 (then t + 2) and t + 2 (t + 3)
+  Tile x0 = look(tile_of(tile0)), x1 = look(tile_of(tile0 + 1)), x2 = look(tile_of(tile0 + 2));
+  Tile x3 = look(tile_of(tile0 + 3));
+  u32x2 meta1 = {0u, 0u}, meta2 = {0u, 0u};  // of tiles x1 and x2
   if (has_meta) {
-    const u32x2 meta0 = ask_meta(tile_of(tile0), pg0);
-    meta1 = ask_meta(tile_of(tile0 + 1), pg1);
-    meta2 = ask_meta(tile_of(tile0 + 2), pg2);
+    const u32x2 meta0 = ask_meta(x0);
+    meta1 = ask_meta(x1);
+    meta2 = ask_meta(x2);
     put_meta(0, meta0);
   }
   sync();
-  ask_data(tile_of(tile0), pg0, 0);
+  get_meta(0);
+  ask_keys(x0), ask_values();
   if constexpr (STAGES == 1) sync();
-  auto next_meta = [&](int t, int slot) {  // of tile t + 1 to shared memory, of t + 3 asked for
+  auto next_meta = [&](int t, int slot) {  // x1's to shared memory, x3's asked for; on to the next tile
     if (has_meta) {
       put_meta(slot, meta1);
       meta1 = meta2;
-      meta2 = ask_meta(tile_of(t + 3), pg3);
+      meta2 = ask_meta(x3);
     }
-    const int pg4 = ask_pages(tile_of(t + 4));
-    pg0 = pg1, pg1 = pg2, pg2 = pg3, pg3 = pg4;
+    x0 = x1, x1 = x2, x2 = x3, x3 = look(tile_of(t + 4));
   };
   f32x16 S;
   if constexpr (STAGES == 2) {
@@ -442,40 +448,42 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     };
     put_keys(), put_values();
     flip(pk), flip(pv);
-    int pgt = pg0;
+    Tile here = x0;
     next_meta(tile0, 1);
     __syncthreads();
-    ask_data(tile_of(tile0 + 1), pg0, 1);
-    logits(S, tile_of(tile0), pgt);
+    get_meta(1);
+    ask_keys(x0), ask_values();
+    logits(S, here);
     for (int t = tile0; t < tile1; ++t) {
       const int slot = (t - tile0) & 1;
-      const int pgn = pg0;
+      const Tile next = x0;
       constexpr int QK = D / 16;
-      block(IC<1>{}, S, 0, 1, tile_of(t), pgt, [&](auto s) {
+      block(IC<1>{}, S, 0, 1, here, [&](auto s) {
         if constexpr (s == 1) put_keys();
         if constexpr (s == QK / 2) put_values();
         if constexpr (s == QK + 1) next_meta(t + 1, slot);
       });
       flip(pk), flip(pv), flip(ka);
       __syncthreads();
-      block(IC<1>{}, S, 1, 0, tile_of(t + 1), pgn, [&](auto s) {
+      block(IC<1>{}, S, 1, 0, next, [&](auto s) {
         if constexpr (s == 1) get_meta(slot);
-        if constexpr (s == QK / 2) ask_keys(tile_of(t + 2), pg0);
+        if constexpr (s == QK / 2) ask_keys(x0);
         if constexpr (s == QK) ask_values();
       });
       flip(va);
       __syncthreads();
-      pgt = pgn;
+      here = next;
     }
   } else {
     for (int t = tile0; t < tile1; ++t) {
       put_keys(), put_values();
-      const int pgt = pg0;
+      const Tile here = x0;
       next_meta(t, 0);
       sync();
-      ask_data(tile_of(t + 1), pg0, 0);
-      logits(S, tile_of(t), pgt);
-      block(IC<0>{}, S, 0, 0, 0, 0, [](auto) {});
+      get_meta(0);
+      ask_keys(x0), ask_values();
+      logits(S, here);
+      block(IC<0>{}, S, 0, 0, here, [](auto) {});
       sync();
     }
   }
@@ -718,7 +726,7 @@ constexpr int shared_lds() {
   return a > b ? a : b;
 }
 
-template <int D, int WR, int PARTS>
+template <int D, int WR, int PARTS, bool LIST>
 __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
@@ -737,7 +745,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
   const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
   const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
   const int rows = P.B * P.R, row0 = rb * WR * kRows;
-  attend<D, WR, T, form_stages(WR), PARTS>(
+  attend<D, WR, T, form_stages(WR), PARTS, LIST>(
       P, lds, kvh, t0, t1,
       [&](int r) -> const uint16_t* {
         r += row0;
@@ -883,21 +891,27 @@ size_t partials(const stc_shape_t& s, const SharedPlan& p) {
   return (size_t)s.B * s.Hq * (p.splits + p.tail_splits);
 }
 
-template <int D, int WR, int PARTS>
+template <int D, int WR, int PARTS, bool LIST>
 int shared_go(const SharedParams& P, int blocks, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int lds = shared_lds<D, WR>();
-  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS>, lds, done)) return -1;
-  shared_kernel<D, WR, PARTS><<<blocks, 64 * kWaves, lds, st>>>(P);
+  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS, LIST>, lds, done)) return -1;
+  shared_kernel<D, WR, PARTS, LIST><<<blocks, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 template <int D, int PARTS>
 int shared_rows(const SharedParams& P, int wr, int blocks, hipStream_t st) {
-  return wr == 1   ? shared_go<D, 1, PARTS>(P, blocks, st)
-         : wr == 2 ? shared_go<D, 2, PARTS>(P, blocks, st)
-         : wr == 4 ? shared_go<D, 4, PARTS>(P, blocks, st)
-                   : shared_go<D, 8, PARTS>(P, blocks, st);
+#define STC_GO(WR)                                                \
+  if (wr == WR)                                                   \
+    return P.pages ? shared_go<D, WR, PARTS, true>(P, blocks, st) \
+                   : shared_go<D, WR, PARTS, false>(P, blocks, st);
+  STC_GO(1)
+  STC_GO(2)
+  STC_GO(4)
+  STC_GO(8)
+#undef STC_GO
+  return -1;
 }
 
 }  // namespace
@@ -917,7 +931,8 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   P.mask = mask, P.off = tok_off, P.pages = page_idx;
   P.Kt = (const unsigned char*)K_tail, P.Vt = (const unsigned char*)V_tail, P.n_tail = n_tail;
   P.acc = (float*)ws, P.ml = P.acc + partials(s, p) * s.D;
-  P.out = out, P.cap = s.v_cap_groups;
+  P.out = out, P.v_stride = s.v_cap_groups;
+  P.cap = (uint32_t)(s.v_cap_groups < UINT32_MAX ? s.v_cap_groups : UINT32_MAX);
   P.B = s.B, P.R = s.Hq / s.Hkv, P.Hq = s.Hq, P.Hkv = s.Hkv, P.N = s.N, P.G = s.G;
   P.NP = (s.N + kPage - 1) / kPage, P.Ncap = token_cap(s), P.k_pages = k_pages, P.tail_cap = tail_cap;
   P.row_blocks = p.row_blocks, P.splits = p.splits, P.split_tiles = p.split_tiles;
