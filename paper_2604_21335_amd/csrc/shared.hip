@@ -72,12 +72,10 @@ __device__ __forceinline__ float over_groups(float x, Op op) {
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
-// The weights of two logits in PARTS bf16 parts, put(part, both as one word); l: their sum, of the
-// weights as they are used.
+// Two weights in PARTS bf16 parts, put(part, both as one word); l: their sum, of the weights as they are
+// used.
 template <int PARTS, class Put>
-__device__ __forceinline__ void weights(float s0, float s1, float scale, float m, float& l, Put put) {
-  float x = __builtin_amdgcn_exp2f(fmaf(s0, scale, -m));
-  float y = __builtin_amdgcn_exp2f(fmaf(s1, scale, -m));
+__device__ __forceinline__ void split(float x, float y, float& l, Put put) {
   if constexpr (PARTS > 1) l += x + y;
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) {
@@ -89,6 +87,22 @@ __device__ __forceinline__ void weights(float s0, float s1, float scale, float m
     x -= bf16_lo(w), y -= bf16_hi(w);
   }
 }
+__device__ __forceinline__ float weight(float s, float scale, float m) {
+  return __builtin_amdgcn_exp2f(fmaf(s, scale, -m));
+}
+
+// Shared memory by its address: with a pointer to an array every access adds the array's.
+template <class T>
+using Lds = __attribute__((address_space(3))) T*;
+template <class T>
+__device__ __forceinline__ Lds<T> lds_at(uint32_t address) {
+  return (Lds<T>)(uintptr_t)address;
+}
+__device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
+  return (uint32_t)(uintptr_t)(Lds<unsigned char>)p;
+}
+// The value is made in front of this place: the compiler would gather such work behind the products.
+__device__ __forceinline__ void made_by_now(float& x) { asm volatile("" : "+v"(x)); }
 
 // WR of the 8 wavefronts of a workgroup share tiles of T tokens and take 32 query rows each; the 8 / WR
 // groups of them take turns at the tiles.
@@ -103,10 +117,10 @@ struct Cfg {
   static constexpr int RB = D * 2;            // bytes of a row
   static constexpr int TILE = T * RB;         // a K or V tile
   static constexpr int STAGE = 2 * TILE;      // a power of two
-  static constexpr int META = T * 8;          // packed offset and mask of the tokens of a tile
+  static constexpr int META = 64 * 8;         // packed offset and mask of a wavefront's rows of a tile
   static constexpr int MROW = D + 4;          // floats of a row in the merge of the groups
   static constexpr int MERGE = WK > 1 ? kWaves * (kRows * MROW * 4 + kRows * 8) : 0;
-  static constexpr int STAGED = WK * STAGES * (STAGE + META);
+  static constexpr int STAGED = WK * STAGES * STAGE + kWaves * META;
   static constexpr int LDS = STAGED > MERGE ? STAGED : MERGE;
 };
 
@@ -205,30 +219,29 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     }
     return max(0, min(T, tokens - x.at * T) - r);
   };
-  // Masks and offsets: one request of a wavefront for a tile, handed to all through shared memory.
+  // Masks and offsets: a lane asks for one of the wavefront's rows of a tile, and shared memory hands them
+  // round.
+  const int meta_row = lane / C::RPW % C::NI * C::RPI + row0 + lane % C::RPW;
   auto ask_meta = [&](const Tile& x) {
     if constexpr (LIST) {
-      const int pg = __shfl(x.page, lane / kPage);
-      const long long t = pg < 0 ? P.N : (long long)pg * kPage + lane % kPage;
-      u32x2 e = {0u, 0u};
-      if (lane < T && t < P.N) e = u32x2{off_s[t], mask_s[t]};
-      return e;
+      const int pg = __shfl(x.page, meta_row / kPage);
+      const long long t = pg < 0 ? P.N : (long long)pg * kPage + meta_row % kPage;
+      u32x2 m = {0u, 0u};
+      if (t < P.N) m = u32x2{off_s[t], mask_s[t]};
+      return m;
     } else {
       const int n = rows_left(x, 0);
       const size_t t = (size_t)x.at * T;
-      return u32x2{__builtin_amdgcn_raw_buffer_load_b32(rsrc(off_s + t, n * 4), lane * 4, 0, 0),
-                   __builtin_amdgcn_raw_buffer_load_b16(rsrc(mask_s + t, n * 2), lane * 2, 0, 0)};
+      return u32x2{__builtin_amdgcn_raw_buffer_load_b32(rsrc(off_s + t, n * 4), meta_row * 4, 0, 0),
+                   __builtin_amdgcn_raw_buffer_load_b16(rsrc(mask_s + t, n * 2), meta_row * 2, 0, 0)};
     }
   };
-  unsigned char* const metas = lds + C::WK * STAGES * C::STAGE + grp * STAGES * C::META;
-  auto put_meta = [&](int slot, u32x2 e) {
-    if (lane < T) *(u32x2*)(metas + slot * C::META + lane * 8) = e;
-  };
+  const uint32_t metas = lds_address(lds) + C::WK * STAGES * C::STAGE + wave * C::META;
+  auto put_meta = [&](u32x2 m) { *lds_at<u32x2>(metas + lane * 8) = m; };
   u32x2 e[C::NI];  // this thread's rows of a tile: packed offset, mask
-  auto get_meta = [&](int slot) {
+  auto get_meta = [&] {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i)
-      e[i] = *(const u32x2*)(metas + slot * C::META + (i * C::RPI + row0 + row_in) * 8);
+    for (int i = 0; i < C::NI; ++i) e[i] = *lds_at<const u32x2>(metas + (i * C::RPW + row_in) * 8);
   };
   auto ask_keys = [&](const Tile& x) {
     if constexpr (LIST) {
@@ -266,8 +279,9 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     }
   };
 
-  // Offsets in shared memory, of one stage; STAGE apart from those of the other
-  const uint32_t mine = grp * STAGES * C::STAGE;
+  // Addresses in shared memory, of one stage; those of the other differ in the bit of STAGE (the memory
+  // is the kernel's only and starts at 0)
+  const uint32_t mine = lds_address(lds) + grp * STAGES * C::STAGE;
   uint32_t pk[C::NI], pv[C::NI];
 #pragma unroll
   for (int i = 0; i < C::NI; ++i) {
@@ -276,11 +290,11 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   }
   auto put_keys = [&] {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) *(u32x4*)(lds + pk[i]) = kr[i];
+    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(pk[i]) = kr[i];
   };
   auto put_values = [&] {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) *(u32x4*)(lds + pv[i]) = vr[i];
+    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(pv[i]) = vr[i];
   };
 
   f32x16 O[D / 32];
@@ -336,61 +350,63 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) i16x4*)(lds + va[cb] + (sub * 32 + 16 * ks + 8 * k) * C::RB));
+          lds_at<i16x4>(va[cb] + (sub * 32 + 16 * ks + 8 * k) * C::RB));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  // One subtile, and the logits of the next (NEXT): the products with the next one's keys, which depend on
-  // nothing, stand between the exponentials of this one, and the next one's maximum between the products
-  // with this one's values.  A matrix instruction takes 32 cycles of its unit and 4 of the wavefront's
-  // issue, so 6 or 7 vector instructions fit behind each.  Operands are read two products ahead.  The
-  // compiler, left to itself, gathers the reads in front and spills; sched_barrier keeps the order.
-  // between(product) is the tile's other work, done between the products too.
+  // One subtile, and the logits of the next (NEXT).  A matrix instruction takes 32 cycles of its unit and 4
+  // of the wavefront's issue, so vector work for 32 cycles fits behind each: the products with the next
+  // one's keys, which depend on nothing, stand between the exponentials of this one, and the next one's
+  // maximum between the products with this one's values, of which the first half needs the first half of
+  // the weights only.  Operands are read two products ahead.  The compiler, left to itself, gathers the
+  // reads in front and spills; sched_barrier keeps the order.  between(product) is the tile's other work.
   auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, const Tile& x1, auto between) {
-    constexpr int QK = D / 16, PV = D / 16, PER = 16 / QK;  // products of either kind, weights for each
+    constexpr int QK = D / 16, HALF = D / 32;  // products of the logits; of the values, per half
+    constexpr int STEPS = 2 * QK;
     u32x4 p[PARTS][2];
     f32x16 N = {};
     bf16x8 kf[3], vf[3];
-    auto read_k = [&](auto s) { kf[s % 3] = *(const bf16x8*)(lds + ka[s] + sub1 * 32 * C::RB); };
-    auto read_v = [&](auto s) { vf[s % 3] = value(sub, s % (D / 32), s / (D / 32)); };
-    auto weigh = [&](auto s) {
-      static_for<0, PER / 2>([&](auto j) {
-        constexpr int i = PER * s + 2 * j;
-        weights<PARTS>(S[i], S[i + 1], scale, m, l,
-                       [&](int k, uint32_t w) { p[k][i / 8][i % 8 / 2] = w; });
-      });
-    };
-    if constexpr (NEXT) read_k(IC<0>{}), read_k(IC<1>{});
-    __builtin_amdgcn_sched_barrier(0);
-    weigh(IC<0>{});
-    __builtin_amdgcn_sched_barrier(0);
-    static_for<0, QK>([&](auto s) {
-      if constexpr (NEXT) {
-        if constexpr (s + 2 < QK) read_k(IC<s + 2>{});
-        N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s % 3], qf[s], N, 0, 0, 0);
+    auto read = [&](auto s) {  // the operand of product s
+      if constexpr (s < QK) {
+        if constexpr (NEXT) kf[s % 3] = *lds_at<const bf16x8>(ka[s] + sub1 * 32 * C::RB);
+      } else if constexpr (s < STEPS) {
+        constexpr int v = s - QK;
+        vf[v % 3] = value(sub, v % HALF, v / HALF);
       }
-      if constexpr (s + 1 < QK) weigh(IC<s + 1>{});
-      if constexpr (s + 2 == QK) read_v(IC<0>{});
-      if constexpr (s + 1 == QK) read_v(IC<1>{});
-      between(s);
-      __builtin_amdgcn_sched_barrier(0);
-    });
+    };
+    // Pair j of the weights: its exponentials behind product pair_at(j), its parts and sum one product on
+    constexpr auto pair_at = [](int j) { return D == 128 ? 3 * j / 2 : j < 4 ? j : 4 + (j - 4) / 2; };
+    float w[8][2];
     float top = 0.0f;
-    static_for<0, PV>([&](auto s) {
-      if constexpr (s + 2 < PV) read_v(IC<s + 2>{});
+    read(IC<0>{}), read(IC<1>{});
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, STEPS>([&](auto s) {
+      static_for<0, 8>([&](auto j) {
+        if constexpr (pair_at(j) + 1 == s)
+          split<PARTS>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
+      });
+      read(IC<s + 2>{});
+      if constexpr (s < QK) {
+        if constexpr (NEXT) N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s % 3], qf[s], N, 0, 0, 0);
+      } else {
+        constexpr int v = s - QK;
 #pragma unroll
-      for (int k = PARTS - 1; k >= 0; --k)
-        O[s % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            vf[s % 3], __builtin_bit_cast(bf16x8, p[k][s / (D / 32)]), O[s % (D / 32)], 0, 0, 0);
-      if constexpr (NEXT) {  // the products of N are through after two more
-        if constexpr (s == 2) top = fmaxf(N[0], N[1]);
-        if constexpr (s >= 2 && s < PV - 1) {
-          constexpr int STEPS = PV - 3, FROM = 2 + 14 * (s - 2) / STEPS / 2 * 2,
-                        TO = 2 + 14 * (s - 1) / STEPS / 2 * 2;
+        for (int k = PARTS - 1; k >= 0; --k)
+          O[v % HALF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              vf[v % 3], __builtin_bit_cast(bf16x8, p[k][v / HALF]), O[v % HALF], 0, 0, 0);
+        if constexpr (v == HALF) made_by_now(l);
+        if constexpr (NEXT && v >= HALF) {  // N is through
+          constexpr int FROM = 16 * (v - HALF) / HALF, TO = 16 * (v - HALF + 1) / HALF;
+          if constexpr (v == HALF) top = N[0];
 #pragma unroll
           for (int i = FROM; i < TO; i += 2) top = fmaxf(fmaxf(N[i], N[i + 1]), top);
+          made_by_now(top);
         }
       }
-      between(IC<QK + s>{});
+      static_for<0, 8>([&](auto j) {
+        if constexpr (pair_at(j) == s)
+          w[j][0] = weight(S[2 * j], scale, m), w[j][1] = weight(S[2 * j + 1], scale, m);
+      });
+      between(s);
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (NEXT) {
@@ -404,39 +420,36 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     f32x16 N = {};
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
-      N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(lds + ka[s]), qf[s], N, 0, 0, 0);
+      N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*lds_at<const bf16x8>(ka[s]), qf[s], N, 0, 0, 0);
     if (x.ragged) hide(N, x, 0);
     S = N;
     take_top(max_halves(largest(N)) * scale);
   };
 
-  // Pages are asked for four tiles ahead, masks and offsets three, keys and values one.
+  // Pages are asked for three tiles ahead and waited for, masks and offsets two or three, keys and values
+  // one.
   auto tile_of = [&](int t) { return t * C::WK + grp; };
   auto sync = [&] {
     if constexpr (WR == 1) wave_lds_sync();
     else __syncthreads();
   };
-  const bool has_meta = wr == 0;  // the group's wavefront that fetches them
   Tile x0 = look(tile_of(tile0)), x1 = look(tile_of(tile0 + 1)), x2 = look(tile_of(tile0 + 2));
-  Tile x3 = look(tile_of(tile0 + 3));
-  u32x2 meta1 = {0u, 0u}, meta2 = {0u, 0u};  // of tiles x1 and x2
-  if (has_meta) {
+  u32x2 meta1, meta2;  // of tiles x1 and x2
+  {
     const u32x2 meta0 = ask_meta(x0);
     meta1 = ask_meta(x1);
     meta2 = ask_meta(x2);
-    put_meta(0, meta0);
+    put_meta(meta0);
   }
-  sync();
-  get_meta(0);
+  wave_lds_sync();
+  get_meta();
   ask_keys(x0), ask_values();
-  if constexpr (STAGES == 1) sync();
-  auto next_meta = [&](int t, int slot) {  // x1's to shared memory, x3's asked for; on to the next tile
-    if (has_meta) {
-      put_meta(slot, meta1);
-      meta1 = meta2;
-      meta2 = ask_meta(x3);
-    }
-    x0 = x1, x1 = x2, x2 = x3, x3 = look(tile_of(t + 4));
+  Tile here = x0;
+  auto next = [&](int t) {  // on to the tile behind t, its masks and offsets to shared memory
+    x0 = x1, x1 = x2, x2 = look(tile_of(t + 3));
+    put_meta(meta1);
+    meta1 = meta2;
+    meta2 = ask_meta(x2);
   };
   f32x16 S;
   if constexpr (STAGES == 2) {
@@ -448,39 +461,38 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     };
     put_keys(), put_values();
     flip(pk), flip(pv);
-    Tile here = x0;
-    next_meta(tile0, 1);
+    wave_lds_sync();
+    next(tile0);
+    wave_lds_sync();
+    get_meta();
     __syncthreads();
-    get_meta(1);
     ask_keys(x0), ask_values();
     logits(S, here);
     for (int t = tile0; t < tile1; ++t) {
-      const int slot = (t - tile0) & 1;
-      const Tile next = x0;
-      constexpr int QK = D / 16;
+      const Tile after = x0;
       block(IC<1>{}, S, 0, 1, here, [&](auto s) {
         if constexpr (s == 1) put_keys();
-        if constexpr (s == QK / 2) put_values();
-        if constexpr (s == QK + 1) next_meta(t + 1, slot);
+        if constexpr (s == D / 32) put_values();
+        if constexpr (s == D / 16) next(t + 1);
+        if constexpr (s == D / 8 - 1) get_meta();
       });
       flip(pk), flip(pv), flip(ka);
       __syncthreads();
-      block(IC<1>{}, S, 1, 0, next, [&](auto s) {
-        if constexpr (s == 1) get_meta(slot);
-        if constexpr (s == QK / 2) ask_keys(x0);
-        if constexpr (s == QK) ask_values();
+      block(IC<1>{}, S, 1, 0, after, [&](auto s) {
+        if constexpr (s == D / 32) ask_keys(x0);
+        if constexpr (s == D / 16) ask_values();
       });
       flip(va);
       __syncthreads();
-      here = next;
+      here = after;
     }
   } else {
     for (int t = tile0; t < tile1; ++t) {
       put_keys(), put_values();
-      const Tile here = x0;
-      next_meta(t, 0);
+      here = x0;
+      next(t);
       sync();
-      get_meta(0);
+      get_meta();
       ask_keys(x0), ask_values();
       logits(S, here);
       block(IC<0>{}, S, 0, 0, here, [](auto) {});
@@ -684,8 +696,8 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
     u32x4 p[PARTS];
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      weights<PARTS>(S[i / 4][i % 4], S[i / 4][i % 4 + 1], scale, m, l,
-                     [&](int k, uint32_t w) { p[k][i / 2] = w; });
+      split<PARTS>(weight(S[i / 4][i % 4], scale, m), weight(S[i / 4][i % 4 + 1], scale, m), l,
+                   [&](int k, uint32_t w) { p[k][i / 2] = w; });
 #pragma unroll
     for (int cb = 0; cb < D / 16; ++cb) {
       i16x4 a[2];
