@@ -116,7 +116,7 @@ struct Cfg {
   static constexpr int TP = T / kPage;        // pages of a tile
   static constexpr int RB = D * 2;            // bytes of a row
   static constexpr int TILE = T * RB;         // a K or V tile
-  static constexpr int STAGE = 2 * TILE;      // a power of two
+  static constexpr int STAGE = 2 * TILE;
   static constexpr int META = 64 * 8;         // packed offset and mask of a wavefront's rows of a tile
   static constexpr int MROW = D + 4;          // floats of a row in the merge of the groups
   static constexpr int MERGE = WK > 1 ? kWaves * (kRows * MROW * 4 + kRows * 8) : 0;
@@ -192,8 +192,6 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   const int row0 = wr * C::RPW;
   const uint32_t grp_of = piece >> lg_upg, bit = 1u << grp_of;
   const uint32_t within = (piece & ((1u << lg_upg) - 1u)) << 4;
-  u32x4 kr[C::NI], vr[C::NI];
-
   // What a tile's requests go by.  With a list, lane j holds page j of the tile, -1 if there is none.
   struct Tile {
     int at, page;
@@ -238,12 +236,14 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   };
   const uint32_t metas = lds_address(lds) + C::WK * STAGES * C::STAGE + wave * C::META;
   auto put_meta = [&](u32x2 m) { *lds_at<u32x2>(metas + lane * 8) = m; };
-  u32x2 e[C::NI];  // this thread's rows of a tile: packed offset, mask
-  auto get_meta = [&] {
+  // This thread's rows of a tile: packed offset and mask, keys, values.
+  using Meta = u32x2[C::NI];
+  using Data = u32x4[C::NI];
+  auto get_meta = [&](Meta& e) {
 #pragma unroll
     for (int i = 0; i < C::NI; ++i) e[i] = *lds_at<const u32x2>(metas + (i * C::RPW + row_in) * 8);
   };
-  auto ask_keys = [&](const Tile& x) {
+  auto ask_keys = [&](const Tile& x, Data& kr) {
     if constexpr (LIST) {
 #pragma unroll
       for (int i = 0; i < C::NI; ++i) {
@@ -264,7 +264,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     const uint32_t room = __builtin_amdgcn_readfirstlane(P.cap > first ? P.cap - first : 0u);
     return rsrc(Vs + ((size_t)(room ? first : 0u) << lg_group), min(room, most) << lg_group);
   };
-  auto ask_values = [&]() {
+  auto ask_values = [&](const Meta& e, Data& vr) {
     Rsrc v;
     uint32_t off0 = 0;
 #pragma unroll
@@ -279,8 +279,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     }
   };
 
-  // Addresses in shared memory, of one stage; those of the other differ in the bit of STAGE (the memory
-  // is the kernel's only and starts at 0)
+  // Addresses in shared memory, where this thread's pieces go: of one stage at a time
   const uint32_t mine = lds_address(lds) + grp * STAGES * C::STAGE;
   uint32_t pk[C::NI], pv[C::NI];
 #pragma unroll
@@ -288,13 +287,15 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     const uint32_t row = i * C::RPI + row0 + row_in;
     pk[i] = mine + k_at<D>(row, piece), pv[i] = mine + C::TILE + v_at<D>(row, piece);
   }
-  auto put_keys = [&] {
+  auto put = [&](const uint32_t (&at)[C::NI], const Data& x) {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(pk[i]) = kr[i];
+    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(at[i]) = x[i];
   };
-  auto put_values = [&] {
+  // on to the next stage of a ring: from stage `at`
+  auto advance = [&](auto& a, int at) {
+    const uint32_t by = at == STAGES - 1 ? (uint32_t)(1 - STAGES) * C::STAGE : (uint32_t)C::STAGE;
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(pv[i]) = vr[i];
+    for (uint32_t& x : a) x += by;
   };
 
   f32x16 O[D / 32];
@@ -357,42 +358,46 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   // of the wavefront's issue, so vector work for 32 cycles fits behind each: the products with the next
   // one's keys, which depend on nothing, stand between the exponentials of this one, and the next one's
   // maximum between the products with this one's values, of which the first half needs the first half of
-  // the weights only.  Operands are read two products ahead.  The compiler, left to itself, gathers the
+  // the weights only.  Operands are read three products ahead.  The compiler, left to itself, gathers the
   // reads in front and spills; sched_barrier keeps the order.  between(product) is the tile's other work.
-  auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, const Tile& x1, auto between) {
+  // The first operands of the block after are read at its end, keys of subtile sub2.
+  bf16x8 ring[4];  // operands on their way
+  auto read_key = [&](auto s, int sub) { ring[s % 4] = *lds_at<const bf16x8>(ka[s] + sub * 32 * C::RB); };
+  auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, int sub2, const Tile& x1, auto between) {
     constexpr int QK = D / 16, HALF = D / 32;  // products of the logits; of the values, per half
     constexpr int STEPS = 2 * QK;
     u32x4 p[PARTS][2];
     f32x16 N = {};
-    bf16x8 kf[3], vf[3];
     auto read = [&](auto s) {  // the operand of product s
       if constexpr (s < QK) {
-        if constexpr (NEXT) kf[s % 3] = *lds_at<const bf16x8>(ka[s] + sub1 * 32 * C::RB);
+        if constexpr (NEXT) read_key(s, sub1);
       } else if constexpr (s < STEPS) {
-        constexpr int v = s - QK;
-        vf[v % 3] = value(sub, v % HALF, v / HALF);
+        ring[s % 4] = value(sub, (s - QK) % HALF, (s - QK) / HALF);
+      } else if constexpr (NEXT) {
+        read_key(IC<s - STEPS>{}, sub2);
       }
     };
     // Pair j of the weights: its exponentials behind product pair_at(j), its parts and sum one product on
     constexpr auto pair_at = [](int j) { return D == 128 ? 3 * j / 2 : j < 4 ? j : 4 + (j - 4) / 2; };
+    static_assert(STEPS % 4 == 0, "the ring goes on where the block before left it");
     float w[8][2];
     float top = 0.0f;
-    read(IC<0>{}), read(IC<1>{});
+    if constexpr (!NEXT) read(IC<QK>{}), read(IC<QK + 1>{}), read(IC<QK + 2>{});
     __builtin_amdgcn_sched_barrier(0);
     static_for<0, STEPS>([&](auto s) {
       static_for<0, 8>([&](auto j) {
         if constexpr (pair_at(j) + 1 == s)
           split<PARTS>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
       });
-      read(IC<s + 2>{});
+      if constexpr (NEXT || s >= QK) read(IC<s + 3>{});
       if constexpr (s < QK) {
-        if constexpr (NEXT) N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s % 3], qf[s], N, 0, 0, 0);
+        if constexpr (NEXT) N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[s % 4], qf[s], N, 0, 0, 0);
       } else {
         constexpr int v = s - QK;
 #pragma unroll
         for (int k = PARTS - 1; k >= 0; --k)
           O[v % HALF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              vf[v % 3], __builtin_bit_cast(bf16x8, p[k][v / HALF]), O[v % HALF], 0, 0, 0);
+              ring[s % 4], __builtin_bit_cast(bf16x8, p[k][v / HALF]), O[v % HALF], 0, 0, 0);
         if constexpr (v == HALF) made_by_now(l);
         if constexpr (NEXT && v >= HALF) {  // N is through
           constexpr int FROM = 16 * (v - HALF) / HALF, TO = 16 * (v - HALF + 1) / HALF;
@@ -426,76 +431,100 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     take_top(max_halves(largest(N)) * scale);
   };
 
-  // Pages are asked for three tiles ahead and waited for, masks and offsets two or three, keys and values
-  // one.
   auto tile_of = [&](int t) { return t * C::WK + grp; };
-  auto sync = [&] {
-    if constexpr (WR == 1) wave_lds_sync();
-    else __syncthreads();
-  };
-  Tile x0 = look(tile_of(tile0)), x1 = look(tile_of(tile0 + 1)), x2 = look(tile_of(tile0 + 2));
-  u32x2 meta1, meta2;  // of tiles x1 and x2
-  {
-    const u32x2 meta0 = ask_meta(x0);
-    meta1 = ask_meta(x1);
-    meta2 = ask_meta(x2);
-    put_meta(meta0);
-  }
-  wave_lds_sync();
-  get_meta();
-  ask_keys(x0), ask_values();
-  Tile here = x0;
-  auto next = [&](int t) {  // on to the tile behind t, its masks and offsets to shared memory
-    x0 = x1, x1 = x2, x2 = look(tile_of(t + 3));
-    put_meta(meta1);
-    meta1 = meta2;
-    meta2 = ask_meta(x2);
-  };
   f32x16 S;
-  if constexpr (STAGES == 2) {
-    // A tile's second half needs the next tile's keys, so that one has to be there by then: it is stored
-    // in front of the first half, when nobody reads the tile before any more.
-    auto flip = [&](auto& a) {
+  Meta e;
+  Data kr, vr;
+  if constexpr (STAGES > 1) {
+    // Tile t + A is stored while tile t is worked on, whose last reader was done a turn ago; tile t + A + 1
+    // is on its way, and so are the masks and offsets of the one after.  One barrier a turn.
+    constexpr int A = STAGES - 1, SUBS = T / 32, QK = D / 16;
+    static_assert(A + 1 >= 2 + 2 / SUBS, "the keys of the block after are there");
+    Tile q[A + 3];  // of tiles t, ..
 #pragma unroll
-      for (uint32_t& x : a) x ^= C::STAGE;
-    };
-    put_keys(), put_values();
-    flip(pk), flip(pv);
-    wave_lds_sync();
-    next(tile0);
-    wave_lds_sync();
-    get_meta();
+    for (int i = 0; i < A + 3; ++i) q[i] = look(tile_of(tile0 + i));
+    auto tile = [&](int t, auto i) { return LIST ? q[i] : look(tile_of(t + i)); };
+    u32x2 m[A + 2];
+#pragma unroll
+    for (int i = 0; i < A + 2; ++i) m[i] = ask_meta(q[i]);
+    Data k0[A], v0[A];
+    static_for<0, A + 1>([&](auto i) {
+      put_meta(m[i]);
+      wave_lds_sync();
+      get_meta(e);
+      wave_lds_sync();
+      if constexpr (i < A) ask_keys(q[i], k0[i]), ask_values(e, v0[i]);
+      else ask_keys(q[i], kr), ask_values(e, vr);
+    });
+    u32x2 meta = m[A + 1];
+    int put_stage = 0, key_stage = 0, value_stage = 0;
+    auto on = [](int& s) { s = s == STAGES - 1 ? 0 : s + 1; };
+    static_for<0, A>([&](auto i) {
+      put(pk, k0[i]), put(pv, v0[i]);
+      advance(pk, put_stage), advance(pv, put_stage), on(put_stage);
+    });
     __syncthreads();
-    ask_keys(x0), ask_values();
-    logits(S, here);
+    logits(S, q[0]);
+    if constexpr (SUBS == 1) advance(ka, key_stage), on(key_stage);
+    static_for<0, 3>([&](auto s) { read_key(s, SUBS - 1); });
     for (int t = tile0; t < tile1; ++t) {
-      const Tile after = x0;
-      block(IC<1>{}, S, 0, 1, here, [&](auto s) {
-        if constexpr (s == 1) put_keys();
-        if constexpr (s == D / 32) put_values();
-        if constexpr (s == D / 16) next(t + 1);
-        if constexpr (s == D / 8 - 1) get_meta();
-      });
-      flip(pk), flip(pv), flip(ka);
+      auto store = [&](auto s) {
+        if constexpr (s == 0) put(pk, kr);
+        if constexpr (s == 1) put_meta(meta), meta = ask_meta(tile(t, IC<A + 2>{}));
+        if constexpr (s == 2) put(pv, vr);
+        if constexpr (s == 3) get_meta(e);
+        if constexpr (s == 4) advance(pk, put_stage), advance(pv, put_stage), on(put_stage);
+      };
+      auto ask = [&](auto s) {
+        if constexpr (s == 0) ask_keys(tile(t, IC<A + 1>{}), kr);
+        if constexpr (s == 2) ask_values(e, vr);
+      };
+      auto keys_on = [&] { advance(ka, key_stage), on(key_stage); };
+      if constexpr (SUBS == 1) {
+        block(IC<1>{}, S, 0, 0, 0, tile(t, IC<1>{}), [&](auto s) {
+          store(s);
+          if constexpr (s >= QK) ask(IC<s - QK>{});
+          if constexpr (s == QK) keys_on();
+        });
+      } else {
+        block(IC<1>{}, S, 0, 1, 0, tile(t, IC<0>{}), [&](auto s) {
+          if constexpr (s >= QK / 2) store(IC<s - QK / 2>{});
+          if constexpr (s == QK) keys_on();
+        });
+        block(IC<1>{}, S, 1, 0, 1, tile(t, IC<1>{}), [&](auto s) {
+          if constexpr (s >= QK / 2) ask(IC<s - QK / 2>{});
+        });
+      }
+      advance(va, value_stage), on(value_stage);
+      if constexpr (LIST) {
+#pragma unroll
+        for (int i = 0; i < A + 2; ++i) q[i] = q[i + 1];
+        q[A + 2] = look(tile_of(t + A + 3));
+      }
       __syncthreads();
-      block(IC<1>{}, S, 1, 0, after, [&](auto s) {
-        if constexpr (s == D / 32) ask_keys(x0);
-        if constexpr (s == D / 16) ask_values();
-      });
-      flip(va);
-      __syncthreads();
-      here = after;
     }
   } else {
+    auto sync = [&] {
+      if constexpr (WR == 1) wave_lds_sync();
+      else __syncthreads();
+    };
+    Tile x0 = look(tile_of(tile0)), x1 = look(tile_of(tile0 + 1)), x2 = look(tile_of(tile0 + 2));
+    u32x2 m0 = ask_meta(x0), m1 = ask_meta(x1), m2 = ask_meta(x2);
+    put_meta(m0);
+    wave_lds_sync();
+    get_meta(e);
+    ask_keys(x0, kr), ask_values(e, vr);
     for (int t = tile0; t < tile1; ++t) {
-      put_keys(), put_values();
-      here = x0;
-      next(t);
+      put(pk, kr), put(pv, vr);
+      put_meta(m1);
+      const Tile here = x0;
+      x0 = x1, x1 = x2, x2 = look(tile_of(t + 3));
+      m1 = m2, m2 = ask_meta(x2);
       sync();
-      get_meta();
-      ask_keys(x0), ask_values();
+      get_meta(e);
+      ask_keys(x0, kr), ask_values(e, vr);
       logits(S, here);
-      block(IC<0>{}, S, 0, 0, here, [](auto) {});
+      block(IC<0>{}, S, 0, 0, 0, here, [](auto) {});
       sync();
     }
   }
@@ -727,8 +756,8 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
 }
 
 // Of the forms by their number of wavefronts that share a tile.
-constexpr int form_tile(int wr) { return wr >= 4 ? 64 : 32; }
-constexpr int form_stages(int wr) { return wr >= 4 ? 2 : 1; }
+constexpr int form_tile(int wr) { return wr == 8 ? 64 : 32; }
+constexpr int form_stages(int wr) { return wr == 8 ? 3 : wr == 4 ? 4 : 1; }
 template <int D, int WR>
 using Form = Cfg<D, WR, form_tile(WR), form_stages(WR)>;
 
