@@ -176,7 +176,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 
   // query rows: operand of S^T, 8 channels of k-step s per lane
   bf16x8 qf[D / 16];
-  {
+  auto ask_queries = [&] {
     const uint16_t* qr = q_row(wr * kRows + c);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
@@ -184,7 +184,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       if (qr) x = *(const u32x4*)(qr + 16 * s + 8 * half);
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
-  }
+  };
 
   // Staging.  This thread takes piece `piece` of the rows i * RPI + row0 + lane / CH, which all lie in
   // one page for the wavefront.
@@ -448,13 +448,16 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 #pragma unroll
     for (int i = 0; i < A + 2; ++i) m[i] = ask_meta(q[i]);
     Data k0[A], v0[A];
+    static_for<0, A>([&](auto i) { ask_keys(q[i], k0[i]); });
+    ask_keys(q[A], kr);
+    ask_queries();
     static_for<0, A + 1>([&](auto i) {
       put_meta(m[i]);
       wave_lds_sync();
       get_meta(e);
       wave_lds_sync();
-      if constexpr (i < A) ask_keys(q[i], k0[i]), ask_values(e, v0[i]);
-      else ask_keys(q[i], kr), ask_values(e, vr);
+      if constexpr (i < A) ask_values(e, v0[i]);
+      else ask_values(e, vr);
     });
     u32x2 meta = m[A + 1];
     int put_stage = 0, key_stage = 0, value_stage = 0;
@@ -510,10 +513,12 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     };
     Tile x0 = look(tile_of(tile0)), x1 = look(tile_of(tile0 + 1)), x2 = look(tile_of(tile0 + 2));
     u32x2 m0 = ask_meta(x0), m1 = ask_meta(x1), m2 = ask_meta(x2);
+    ask_keys(x0, kr);
+    ask_queries();
     put_meta(m0);
     wave_lds_sync();
     get_meta(e);
-    ask_keys(x0, kr), ask_values(e, vr);
+    ask_values(e, vr);
     for (int t = tile0; t < tile1; ++t) {
       put(pk, kr), put(pv, vr);
       put_meta(m1);
