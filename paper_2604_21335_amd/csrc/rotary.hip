@@ -80,10 +80,15 @@ struct Rows {
   int64_t b, h, n;  // strides in 16-byte pieces
 };
 
-// A thread takes one slot of HPT heads of a token: their loads go out together, and the angles are
-// taken once for all of them.  Neighbouring lanes take the slots of a row, then the rows that lie next
-// to each other in x (heads of a token, or tokens of a head).
-template <int D, int HPT>
+// A thread takes one slot of a row.  Neighbouring lanes take the slots of a row, then the rows that lie next
+// to each other in x (heads of a token, or tokens of a head).  Bound by memory: 16 + 16 bytes in and out
+// for 8 angles, a third of whose arithmetic would fit behind them.  (Four heads a thread, which share their
+// angles, are slower: 338 us against 314 for 4 x 32768 tokens of 28 heads of 128, with two 322.)
+// STREAM: loads and stores past the caches.  In us, with / without: 256 MiB, head by head 84 / 91; the 28
+// heads 297 / 314, into a cache's order 320 / 343; but 64 MiB 22.6 / 20.9, since what was written is read
+// from the last-level cache; and where an instruction stores half lines, D = 64 54 / 48 and half the
+// head rotated 66 / 46.
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(const u32x4* x, u32x4* y,
                                                      const double* __restrict__ turns,
                                                      const int32_t* __restrict__ pos, int pos0, int N,
@@ -91,36 +96,30 @@ __global__ __launch_bounds__(256) void rotary_kernel(const u32x4* x, u32x4* y,
                                                      Rows xs, Rows ys) {
   constexpr int SLOTS = D / 16;
   const bool heads_next = flags & 1, interleaved = flags & 2, inverse = flags & 4, in_place = flags & 8;
-  const uint32_t HG = (H + HPT - 1) / HPT;  // the thread's heads are hg, hg + HG, ..
   const int slot = threadIdx.x % SLOTS;
   const uint32_t row = blockIdx.x * (256 / SLOTS) + threadIdx.x / SLOTS;
-  if (row >= (uint32_t)N * HG) return;
-  const uint32_t minor = heads_next ? HG : N;
+  if (row >= (uint32_t)N * H) return;
+  const uint32_t minor = heads_next ? H : N;
   const int major_at = row / minor, minor_at = row % minor;
-  const int n = heads_next ? major_at : minor_at, hg = heads_next ? minor_at : major_at;
+  const int n = heads_next ? major_at : minor_at, h = heads_next ? minor_at : major_at;
   const int b = blockIdx.y;
   const Slot sl = slot_of(slot, rot_dim, interleaved);
   if (in_place && !sl.rotated) return;
-  const u32x4* xb = x + b * xs.b + n * xs.n;
-  u32x4* yb = y + b * ys.b + n * ys.n;
-  const int p = pos ? pos[(size_t)b * N + n] : pos0 + n;
-  u32x4 v[HPT][2];
-  static_for<0, HPT>([&](auto i) {
-    const int h = min((int)(hg + i * HG), H - 1);  // (the last one again where there is none)
-    v[i][0] = xb[h * xs.h + sl.first];
-    v[i][1] = xb[h * xs.h + sl.second];
-  });
+  const u32x4* xr = x + b * xs.b + h * xs.h + n * xs.n;
+  u32x4* yr = y + b * ys.b + h * ys.h + n * ys.n;
+  u32x4 u = STREAM ? __builtin_nontemporal_load(xr + sl.first) : xr[sl.first];
+  u32x4 w = STREAM ? __builtin_nontemporal_load(xr + sl.second) : xr[sl.second];
   if (sl.rotated) {
-    const Angles a = angles_of(turns, slot, p, amplitude, inverse);
-    static_for<0, HPT>([&](auto i) { rotate(v[i][0], v[i][1], a, interleaved); });
+    const int p = pos ? pos[(size_t)b * N + n] : pos0 + n;
+    rotate(u, w, angles_of(turns, slot, p, amplitude, inverse), interleaved);
   }
-  static_for<0, HPT>([&](auto i) {
-    const int h = hg + i * HG;
-    if (h < H) {
-      yb[h * ys.h + sl.first] = v[i][0];
-      yb[h * ys.h + sl.second] = v[i][1];
-    }
-  });
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store(u, yr + sl.first);
+    __builtin_nontemporal_store(w, yr + sl.second);
+  } else {
+    yr[sl.first] = u;
+    yr[sl.second] = w;
+  }
 }
 
 // One workgroup per element of the batch, so that the element's count can be read by all and then
@@ -200,21 +199,16 @@ int launch_rotary(int B, int H, int N, int D, int rot_dim, int layout, const dou
   const bool same = x == y && xs[0] == ys[0] && xs[1] == ys[1] && xs[2] == ys[2];
   const int flags = (xs[1] <= xs[2] ? 1 : 0) | ((layout & 0xff) == STC_ROTARY_INTERLEAVED ? 2 : 0) |
                     (layout & STC_ROTARY_INVERSE ? 4 : 0) | (same ? 8 : 0);
-  const int hpt = H >= 4 ? 4 : H >= 2 ? 2 : 1;
-  const long long rows = (long long)N * ((H + hpt - 1) / hpt);
+  const long long rows = (long long)N * H;
   const dim3 grid((unsigned)((rows * (D / 16) + 255) / 256), B);
-#define STC_ROTARY(DD, HPT)                                                                   \
-  rotary_kernel<DD, HPT><<<grid, 256, 0, st>>>((const u32x4*)x, (u32x4*)y, turns, pos, pos0, N, H, \
-                                               rot_dim, amplitude, flags, xr, yr)
-  if (D == 128) {
-    if (hpt == 4) STC_ROTARY(128, 4);
-    else if (hpt == 2) STC_ROTARY(128, 2);
-    else STC_ROTARY(128, 1);
-  } else {
-    if (hpt == 4) STC_ROTARY(64, 4);
-    else if (hpt == 2) STC_ROTARY(64, 2);
-    else STC_ROTARY(64, 1);
-  }
+  // every store instruction writes whole lines, and more than the last-level cache holds goes through
+  const bool stream = rot_dim == 128 && !(flags & 2) && rows * B * D * 2 >= (256ll << 20);
+#define STC_ROTARY(DD, STREAM)                                                                    \
+  rotary_kernel<DD, STREAM><<<grid, 256, 0, st>>>((const u32x4*)x, (u32x4*)y, turns, pos, pos0, N, H, \
+                                                  rot_dim, amplitude, flags, xr, yr)
+  if (D == 64) STC_ROTARY(64, false);
+  else if (stream) STC_ROTARY(128, true);
+  else STC_ROTARY(128, false);
 #undef STC_ROTARY
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }

@@ -777,7 +777,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    tails<D, PARTS>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE, blockIdx.x * kWaves + wave,
+    tails<D, PARTS == 1 ? 1 : 3>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE, blockIdx.x * kWaves + wave,
                     P.tail_blocks * kWaves);
     return;
   }

@@ -141,6 +141,26 @@ def test_rows_behind_four_gib():
     assert torch.equal(x, z)
 
 
+@pytest.mark.parametrize("tokens_out", [False, True])
+def test_past_the_caches(tokens_out):
+    """256 MiB and more go past the caches: the same bits as in two calls that do not; and in place."""
+    N, H = (1 << 20) // 8 + 1, 8
+    g = torch.Generator(device=DEV).manual_seed(6)
+    x = torch.empty(1, H, N, 128, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    t = stc.stc_rotary_turns(128, base=1e6).to(DEV)
+    shape = (1, N, H, 128) if tokens_out else (1, H, N, 128)
+    want, got = (torch.empty(shape, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    if tokens_out:
+        want, got = want.transpose(1, 2), got.transpose(1, 2)
+    half = N // 2
+    stc.stc_rotary(x[:, :, :half], want[:, :, :half], t, 128, HALVES, pos0=5)
+    stc.stc_rotary(x[:, :, half:], want[:, :, half:], t, 128, HALVES, pos0=5 + half)
+    stc.stc_rotary(x, got, t, 128, HALVES, pos0=5)
+    assert torch.equal(got, want)
+    stc.stc_rotary(x, x, t, 128, HALVES, pos0=5)
+    assert torch.equal(x, want)
+
+
 @pytest.mark.parametrize("B,Hq,Hkv,D,rot,layout", [
     (1, 1, 1, 64, 64, HALVES), (5, 8, 2, 128, 128, HALVES), (3, 14, 2, 128, 64, INTER),
     (2, 96, 32, 128, 128, INTER), (70, 4, 4, 64, 16, HALVES), (4, 8, 8, 64, 0, HALVES)])
