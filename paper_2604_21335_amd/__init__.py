@@ -511,13 +511,17 @@ class SharedPrefix:
     """B sequences that continue one prefix: a RoutedCache with B = 1 that holds the prefix, and the
     sequences' own uncompressed tails, per-step outputs and workspace.  As in RoutedCache, allocation
     and nothing else; the lengths of the tails lie on the device (n_tail; a negative one marks an
-    element of the batch as padding), so that a step can be captured and replayed."""
+    element of the batch as padding), so that a step can be captured and replayed.  The prefix is
+    whole when the object is made: its own tail is empty (flush moves it into the cache), and it
+    does not grow while sequences continue it."""
 
     def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32):
         """rotary: positions for the queries and keys given to append()."""
         if prefix.B != 1:
             raise ValueError("the prefix is a cache of one batch element")
         self.prefix, self.B, self.tail_cap, self.rotary = prefix, B, tail_cap, rotary
+        self.N = prefix.N
+        self._whole()
         p, dev = prefix, prefix.device
         self.shape = make_shape(B, p.Hq, p.Hkv, p.D, p.N, p.G, p.shape.v_cap_groups, N_cap=p.n_cap)
         self.n_tail = torch.zeros(B, dtype=torch.int32, device=dev)
@@ -530,18 +534,24 @@ class SharedPrefix:
         need = max(stc_shared_workspace_bytes(self.shape, k, tail_cap) for k in range(1, p.NP + 1))
         self._ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
 
+    def _whole(self):
+        if self.prefix.n_tail or self.prefix.N != self.N:
+            raise ValueError("the prefix has a tail of its own or has grown")
+
     def append(self, q, k_new, v_new):
         """The new token of every sequence: q [B, Hq, D], k_new, v_new [B, Hkv, D] (without positions
         where rotary is given).  Key and value go to the tails; returns the queries for attend()."""
+        self._whole()
         r = self.rotary
         stc_rotary_append(self.shape, q, k_new, v_new, self.q, self.K_tail, self.V_tail, self.n_tail,
                           self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
                           r.layout if r else STC_ROTARY_HALVES, amplitude=r.amplitude if r else 1.0,
-                          pos0=self.prefix.N, n_out=self.n_tail, dev_status=self.dev_status)
+                          pos0=self.N, n_out=self.n_tail, dev_status=self.dev_status)
         return self.q
 
     def attend(self, q, page_idx=None):
         """page_idx [Hkv, k]: the pages of the prefix to attend; None: all of it."""
+        self._whole()
         p = self.prefix
         k = p.NP if page_idx is None else page_idx.shape[-1]
         stc_decode_attention_shared(self.shape, q, p.K, p.vpacked, p.mask, p.tok_off, page_idx, k,

@@ -57,3 +57,20 @@ def test_a_prefix_is_one_element():
     cache.B = 2
     with pytest.raises(ValueError):
         stc.SharedPrefix(cache, 4, 16)
+
+
+def test_a_prefix_is_whole():
+    """One with a tail of its own, or that grows while sequences continue it, is refused: its tail would
+    not be attended, and new tokens' positions would move."""
+    cache = stc.RoutedCache.__new__(stc.RoutedCache)
+    cache.B, cache.N, cache.n_tail = 1, 64, 3
+    with pytest.raises(ValueError):
+        stc.SharedPrefix(cache, 4, 16)
+    b = stc.SharedPrefix.__new__(stc.SharedPrefix)
+    b.prefix, b.N = cache, 64
+    for tail, n in ((3, 64), (0, 67)):
+        cache.n_tail, cache.N = tail, n
+        with pytest.raises(ValueError):
+            b.append(None, None, None)
+        with pytest.raises(ValueError):
+            b.attend(None)
