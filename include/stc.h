@@ -402,8 +402,9 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *            (all listed pages outside the prefix, an empty tail) gets zeros
  *   ws       stc_shared_workspace_bytes(shape, k_pages, tail_cap) bytes; calls whose work overlaps in
  *            time need one each
- * For float output the softmax's weights are carried as two bf16 parts (2^-17), for bf16 output as one
- * (2^-9, the output's own rounding).  The results depend on the sizes, not on other sequences' lengths.
+ * For float output the softmax's weights are carried as bf16 parts, two for the prefix (2^-16) and three
+ * for the tails (2^-24), for bf16 output as one (2^-8, as the output's own rounding).  The results depend
+ * on the sizes, not on other sequences' lengths.
  */
 enum { STC_OUT_F32 = 0, STC_OUT_BF16 = 1 };
 size_t stc_shared_workspace_bytes(const stc_shape_t *shape, int k_pages, int tail_cap);

@@ -111,7 +111,7 @@ class Args {
     need(t.dim() == dims, name, "has another number of dimensions");
     Rows r{t.data_ptr(), {}, {}};
     for (int i = 0; i < dims; ++i) r.size[i] = t.size(i), r.stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
-    need(r.size[dims - 1] > 1 && r.stride[dims - 1] == 1, name, "must be contiguous in its last dimension");
+    need(r.size[dims - 1] > 1 && r.size[dims - 1] <= INT32_MAX && r.stride[dims - 1] == 1, name, "must be contiguous in its last dimension");
     need(t.numel() > 0 && t.numel() / r.size[dims - 1] <= INT32_MAX, name, "is empty or too large");
     return r;
   }

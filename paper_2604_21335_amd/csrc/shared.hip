@@ -3,8 +3,21 @@
 // of dense products with the prefix's tokens, as in the attention of a prompt:
 //   S^T[token][row] = K[token][:] . q[row][:]                (v_mfma_f32_32x32x16_bf16)
 //   O^T[chan][row] += V~^T[chan][token] . P^T[token][row]
-// with a running maximum and sum per row.  Every sequence's own tail goes by the same code in workgroups
-// of its own; a second launch merges the partial results of a row.
+// with a running maximum and sum per row.  The logits come out of the first product with a row's in one
+// column, which is the layout the second product wants its weights in: they never leave the registers.
+// Every sequence's own tail goes the same way in workgroups of its own; a second launch merges the
+// partial results of a row.
+//
+// What bounds it (D = 128, half of the value groups kept):
+//   few rows, long prefix: 16 x 28 rows over 32768 tokens 27 us, the bytes of the cache 10.  Of the first
+//     launch's 22, 6 go by before the first product (kernel, masks and offsets, values: a chain of loads),
+//     13 in the loop at half of the matrix units' rate, 2 into writing partial results; the merge takes 5.
+//   many rows: 256 x 28 over 32768 tokens, 136 us, 90 GFLOP of kept values (120 with the dropped ones, which
+//     are multiplied as zeros: 890 TFLOP/s, a library's largest product 1220 .. 1360 on the card).  The
+//     exponentials share the wavefronts' issue with the matrix instructions, and the card's power holds
+//     the clock down; without exponentials it would be 129.
+//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 us at 4.8 TB/s,
+//     where a copy reaches 5.1.
 #include "stc_common.hpp"
 #include "stc_kernels.hpp"
 
@@ -25,7 +38,7 @@ constexpr float kNone = -1.0e30f;  // running maximum of a row that has seen no 
 constexpr int kWaves = 8;      // of a workgroup; one workgroup fills a compute unit
 constexpr int kRows = 32;      // query rows of a wavefront
 constexpr int kTailTile = 32;  // tokens of a tail's tile
-constexpr int kXcds = 8;
+constexpr int kXcds = 8, kUnits = 256;  // XCDs, compute units of all of them
 // A maximum that grows by less than this (base 2) leaves the sums as they are: the weights then reach
 // 2^8, far from the range of a float, and 64 multiplications per tile are saved.
 constexpr float kSlack = 8.0f;
@@ -73,7 +86,10 @@ __device__ __forceinline__ float over_groups(float x, Op op) {
 }
 
 // Two weights in PARTS bf16 parts, put(part, both as one word); l: their sum, of the weights as they are
-// used.
+// used.  A part leaves 2^-8 of what it rounds.  One does for bf16 output, whose own rounding is as large.
+// For float output the prefix takes two (2^-16, and errors of many weights cancel: outputs are off by some
+// 10^-6): three would cost 1 .. 18 % there, where the matrix units are what is short.  The tails take three
+// (2^-24, a float's own), where they are not and a row may have few tokens.
 template <int PARTS, class Put>
 __device__ __forceinline__ void split(float x, float y, float& l, Put put) {
   if constexpr (PARTS > 1) l += x + y;
@@ -105,7 +121,7 @@ __device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
 __device__ __forceinline__ void made_by_now(float& x) { asm volatile("" : "+v"(x)); }
 
 // WR of the 8 wavefronts of a workgroup share tiles of T tokens and take 32 query rows each; the 8 / WR
-// groups of them take turns at the tiles.
+// groups of them take turns at the tiles.  A tile has STAGES places in shared memory.
 template <int D, int WR, int T, int STAGES>
 struct Cfg {
   static constexpr int WK = kWaves / WR;
@@ -438,8 +454,8 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   if constexpr (STAGES > 1) {
     // Tile t + A is stored while tile t is worked on, whose last reader was done a turn ago; tile t + A + 1
     // is on its way, and so are the masks and offsets of the one after.  One barrier a turn.
-    constexpr int A = STAGES - 1, SUBS = T / 32, QK = D / 16;
-    static_assert(A + 1 >= 2 + 2 / SUBS, "the keys of the block after are there");
+    constexpr int A = STAGES - 1, QK = D / 16;
+    static_assert(T == 64 && A >= 2, "two blocks a tile, and the keys of the block after are there");
     Tile q[A + 3];  // of tiles t, ..
 #pragma unroll
     for (int i = 0; i < A + 3; ++i) q[i] = look(tile_of(tile0 + i));
@@ -468,8 +484,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     });
     __syncthreads();
     logits(S, q[0]);
-    if constexpr (SUBS == 1) advance(ka, key_stage), on(key_stage);
-    static_for<0, 3>([&](auto s) { read_key(s, SUBS - 1); });
+    static_for<0, 3>([&](auto s) { read_key(s, 1); });
     for (int t = tile0; t < tile1; ++t) {
       auto store = [&](auto s) {
         if constexpr (s == 0) put(pk, kr);
@@ -482,22 +497,13 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
         if constexpr (s == 0) ask_keys(tile(t, IC<A + 1>{}), kr);
         if constexpr (s == 2) ask_values(e, vr);
       };
-      auto keys_on = [&] { advance(ka, key_stage), on(key_stage); };
-      if constexpr (SUBS == 1) {
-        block(IC<1>{}, S, 0, 0, 0, tile(t, IC<1>{}), [&](auto s) {
-          store(s);
-          if constexpr (s >= QK) ask(IC<s - QK>{});
-          if constexpr (s == QK) keys_on();
-        });
-      } else {
-        block(IC<1>{}, S, 0, 1, 0, tile(t, IC<0>{}), [&](auto s) {
-          if constexpr (s >= QK / 2) store(IC<s - QK / 2>{});
-          if constexpr (s == QK) keys_on();
-        });
-        block(IC<1>{}, S, 1, 0, 1, tile(t, IC<1>{}), [&](auto s) {
-          if constexpr (s >= QK / 2) ask(IC<s - QK / 2>{});
-        });
-      }
+      block(IC<1>{}, S, 0, 1, 0, tile(t, IC<0>{}), [&](auto s) {
+        if constexpr (s >= QK / 2) store(IC<s - QK / 2>{});
+        if constexpr (s == QK) advance(ka, key_stage), on(key_stage);
+      });
+      block(IC<1>{}, S, 1, 0, 1, tile(t, IC<1>{}), [&](auto s) {
+        if constexpr (s >= QK / 2) ask(IC<s - QK / 2>{});
+      });
       advance(va, value_stage), on(value_stage);
       if constexpr (LIST) {
 #pragma unroll
@@ -760,9 +766,13 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
   }
 }
 
-// Of the forms by their number of wavefronts that share a tile.
+// The forms, by the number of wavefronts that share a tile.  Up to 4: tiles of 32 tokens in one place, the
+// next one on its way in registers, and products and exponentials of different wavefronts side by side.
+// 8: tiles of 64 tokens in a ring of three, one barrier a tile, the next logits' products between the
+// exponentials; the ring takes longer to fill.  (A ring of four for 4 wavefronts: 28.6 us where one place
+// takes 26.8, 112 rows over 32768 tokens; two places for 2 or 4 make no difference.)
 constexpr int form_tile(int wr) { return wr == 8 ? 64 : 32; }
-constexpr int form_stages(int wr) { return wr == 8 ? 3 : wr == 4 ? 4 : 1; }
+constexpr int form_stages(int wr) { return wr == 8 ? 3 : 1; }
 template <int D, int WR>
 using Form = Cfg<D, WR, form_tile(WR), form_stages(WR)>;
 
@@ -777,8 +787,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    tails<D, PARTS == 1 ? 1 : 3>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE, blockIdx.x * kWaves + wave,
-                    P.tail_blocks * kWaves);
+    tails<D, PARTS == 1 ? 1 : 3>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE,
+                                 blockIdx.x * kWaves + wave, P.tail_blocks * kWaves);
     return;
   }
   // the row blocks of a split share its keys and values: same id modulo the 8 XCDs
@@ -892,15 +902,25 @@ struct SharedPlan {
 SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   SharedPlan p{};
   const long long rows = (long long)s.B * (s.Hq / s.Hkv);
-  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+  const long long streams = (long long)s.B * s.Hkv;
+  // Wavefronts that share a tile: as many as have rows.  In us, by 1, 2, 4 and 8 of them, 4 KV heads of
+  // 32768 (131072) tokens: 28 rows 17.2, 18.6, 24, 28; 63 rows 20.5, 20.6, 24, 30 and from a list of 2512
+  // pages 30.1 by 1, 27.0 by 2; 112 rows 27.7, 25.6, 26.8, 33 (by 2, 4: 77.9, 68.5); 1792 rows in bf16
+  // 230, 208, 172, 136.  Beyond 128 rows the ring of 8 pays where a compute unit has a long share of the
+  // prefix (315 rows, 1024 tokens: 45.7 by 4, 48.1 by 8; 875 rows, 2048 tokens: 107 and 100), or where it
+  // makes room for the tails (192 rows over 4001 tokens, tails of up to 1000: 159 and 154 for 4 layers; tails
+  // of up to 200 instead, 312 a unit: 20.7 and 24.6).
+  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  const long long blocks8 = (rows + 255) / 256;
+  if (rows > 128 && (blocks8 * s.Hkv * k_pages * kPage > 1792 * kUnits || streams * tail_cap > 400 * kUnits))
+    p.wr = 8;
   p.row_blocks = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
   const int per = form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
   const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
   const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
-  const long long streams = (long long)s.B * s.Hkv;
   if (tail_cap > 0) {
     // 4 pieces for every wavefront of the chip where all tails are full, but not so small that their
-    // partial results pass 1/16 of their keys and values
+    // partial results pass 1/16 of their keys and values (8 and no limit: 166 us for the 4 layers' 153)
     long long t = (streams * tail_max + 4 * 2048 - 1) / (4 * 2048);
     if (t < (s.Hq / s.Hkv + 1) / 2) t = (s.Hq / s.Hkv + 1) / 2;
     if (t > tail_max) t = tail_max;
@@ -994,6 +1014,8 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
                                         : shared_rows<64, 2>(P, p.wr, blocks, st));
   if (rc) return -1;
   const int rows = s.B * s.Hq;
+  // 4 wavefronts for a row of many partial results: 64 of them 17.2 us for the whole call, with one
+  // wavefront 20.4; but 8 of them 29.5 and 28.6
   const int wpr = p.splits + p.tail_splits > 16 ? 4 : 1;
   const int groups = (rows * (long long)wpr + 3) / 4;
   if (s.D == 128) {

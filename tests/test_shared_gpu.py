@@ -102,6 +102,20 @@ def test_rows(B, R, Hkv, D, G, dtype):
     Case(B, R * Hkv, Hkv, D, 200, G, 40, seed=B + R).check(dtype)
 
 
+# many rows beside tails that are long together: 8 wavefronts to a tile
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,R,Hkv,cap,N", [(129, 1, 4, 210, 63), (300, 1, 4, 90, 700), (33, 16, 4, 800, 129),
+                                           (90, 5, 8, 150, 1), (150, 2, 4, 180, 2001)])
+def test_wide_tiles(B, R, Hkv, cap, N, D, dtype):
+    Case(B, R * Hkv, Hkv, D, N, 8, cap, seed=N, n_tail=[0, 3, cap, -1, 40]).check(dtype)
+    c = Case(B, R * Hkv, Hkv, D, N, 4, cap, seed=N + 1, n_tail=[0, 1, -1, 9], n_cap=N + 20)
+    NP = (N + 15) // 16
+    pages = np.stack([np.random.default_rng(h).permutation(NP) for h in range(Hkv)])
+    pages[0, -1] = NP
+    c.check(dtype, pages=pages)
+
+
 # tokens that end inside a page, a tile, a group's turn, a split
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,Hq,Hkv,D", [(2, 4, 2, 128), (9, 10, 2, 64), (40, 5, 1, 128)])
