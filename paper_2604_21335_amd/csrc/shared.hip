@@ -16,8 +16,8 @@
 //     are multiplied as zeros: 890 TFLOP/s, a library's largest product 1220 .. 1360 on the card).  The
 //     exponentials share the wavefronts' issue with the matrix instructions, and the card's power holds
 //     the clock down; without exponentials it would be 129.
-//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 us at 4.8 TB/s,
-//     where a copy reaches 5.1.
+//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 30.5 us, 138 MB at
+//     4.5 TB/s with the merge's launch, where a copy reaches 5.1.
 #include "stc_common.hpp"
 #include "stc_kernels.hpp"
 
@@ -166,11 +166,12 @@ __device__ __forceinline__ Rsrc rsrc(const void* base, uint32_t bytes) {
                                            0x00027000);
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset behind every end
+constexpr int kPast = 2;                    // non-temporal: past the caches
 
 // Tiles [tile0, tile1) of the prefix for the query rows q_row(0 ..) of one KV head; tile t of key group
 // g is tile t * WK + g.  The groups' results are merged; the partial result of row r goes to index(r)
 // (negative: nowhere).
-template <int D, int WR, int T, int STAGES, int PARTS, bool LIST, class Row, class Index>
+template <int D, int WR, int T, int STAGES, int PARTS, bool LIST, bool STREAM, class Row, class Index>
 __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int tile0,
                                        int tile1, Row q_row, Index index) {
   using C = Cfg<D, WR, T, STAGES>;
@@ -266,13 +267,15 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
         const int r = i * C::RPI + row0;
         const int pg = max(__builtin_amdgcn_readlane(x.page, r / kPage), 0);
         kr[i] = __builtin_amdgcn_raw_buffer_load_b128(
-            rsrc(Ks + ((size_t)pg * kPage + r % kPage) * C::RB, rows_left(x, r) * C::RB), lane * 16, 0, 0);
+            rsrc(Ks + ((size_t)pg * kPage + r % kPage) * C::RB, rows_left(x, r) * C::RB), lane * 16, 0,
+            STREAM ? kPast : 0);
       }
     } else {  // a tile is one piece of memory
       const Rsrc k = rsrc(Ks + (size_t)x.at * T * C::RB, rows_left(x, 0) * C::RB);
 #pragma unroll
       for (int i = 0; i < C::NI; ++i)
-        kr[i] = __builtin_amdgcn_raw_buffer_load_b128(k, (i * C::RPI + row0) * C::RB + lane * 16, 0, 0);
+        kr[i] = __builtin_amdgcn_raw_buffer_load_b128(k, (i * C::RPI + row0) * C::RB + lane * 16, 0,
+                                                      STREAM ? kPast : 0);
     }
   };
   // The values of the groups from `first` on, `most` of them at most
@@ -291,7 +294,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       }
       const uint32_t slot = e[i][0] - off0 + __popc(e[i][1] & (bit - 1u));
       const uint32_t at = (e[i][1] & bit) ? (slot << lg_group) + within : kNowhere;
-      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(v, at, 0, 0);
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(v, at, 0, STREAM ? kPast : 0);
     }
   };
 
@@ -645,14 +648,16 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
 
   u32x4 kr[NI], vr[NI];
   bf16x8 qn[D / 32], qf[D / 32];
+  // Past the caches: 64 x 32 heads with tails of 0 .. 256, 138 MB, 36.0 -> 30.5 us in turn with other layers'
+  // (one layer alone, out of the last-level cache: 30.8 -> 32.2).
   auto ask = [&] {
     const size_t row = ((size_t)b * P.Hkv + kvh) * P.tail_cap + (size_t)t * kTailTile;
     const int bytes = min(kTailTile, n - t * kTailTile) * RB;
     const Rsrc rk = rsrc(P.Kt + row * RB, bytes), rv = rsrc(P.Vt + row * RB, bytes);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, i * 1024 + lane * 16, 0, 0);
-      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, i * 1024 + lane * 16, 0, 0);
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, i * 1024 + lane * 16, 0, kPast);
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, i * 1024 + lane * 16, 0, kPast);
     }
   };
   auto ask_q = [&] {
@@ -782,7 +787,7 @@ constexpr int shared_lds() {
   return a > b ? a : b;
 }
 
-template <int D, int WR, int PARTS, bool LIST>
+template <int D, int WR, int PARTS, bool LIST, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
@@ -801,7 +806,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
   const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
   const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
   const int rows = P.B * P.R, row0 = rb * WR * kRows;
-  attend<D, WR, T, form_stages(WR), PARTS, LIST>(
+  attend<D, WR, T, form_stages(WR), PARTS, LIST, STREAM>(
       P, lds, kvh, t0, t1,
       [&](int r) -> const uint16_t* {
         r += row0;
@@ -957,27 +962,31 @@ size_t partials(const stc_shape_t& s, const SharedPlan& p) {
   return (size_t)s.B * s.Hq * (p.splits + p.tail_splits);
 }
 
-template <int D, int WR, int PARTS, bool LIST>
+template <int D, int WR, int PARTS, bool LIST, bool STREAM>
 int shared_go(const SharedParams& P, int blocks, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int lds = shared_lds<D, WR>();
-  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS, LIST>, lds, done)) return -1;
-  shared_kernel<D, WR, PARTS, LIST><<<blocks, 64 * kWaves, lds, st>>>(P);
+  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS, LIST, STREAM>, lds, done)) return -1;
+  shared_kernel<D, WR, PARTS, LIST, STREAM><<<blocks, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
+template <int D, int PARTS, bool LIST>
+int shared_rows(const SharedParams& P, int wr, bool stream, int blocks, hipStream_t st) {
+  if (wr == 1)
+    return stream ? shared_go<D, 1, PARTS, LIST, true>(P, blocks, st)
+                  : shared_go<D, 1, PARTS, LIST, false>(P, blocks, st);
+  if (wr == 2)
+    return stream ? shared_go<D, 2, PARTS, LIST, true>(P, blocks, st)
+                  : shared_go<D, 2, PARTS, LIST, false>(P, blocks, st);
+  return wr == 4 ? shared_go<D, 4, PARTS, LIST, false>(P, blocks, st)
+                 : shared_go<D, 8, PARTS, LIST, false>(P, blocks, st);
+}
+
 template <int D, int PARTS>
-int shared_rows(const SharedParams& P, int wr, int blocks, hipStream_t st) {
-#define STC_GO(WR)                                                \
-  if (wr == WR)                                                   \
-    return P.pages ? shared_go<D, WR, PARTS, true>(P, blocks, st) \
-                   : shared_go<D, WR, PARTS, false>(P, blocks, st);
-  STC_GO(1)
-  STC_GO(2)
-  STC_GO(4)
-  STC_GO(8)
-#undef STC_GO
-  return -1;
+int shared_list(const SharedParams& P, int wr, bool stream, int blocks, hipStream_t st) {
+  return P.pages ? shared_rows<D, PARTS, true>(P, wr, stream, blocks, st)
+                 : shared_rows<D, PARTS, false>(P, wr, stream, blocks, st);
 }
 
 }  // namespace
@@ -1008,10 +1017,16 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   if (units * p.row_blocks > (1 << 30)) return -1;
   P.tail_blocks = p.tail_blocks;
   const int blocks = (int)(units * p.row_blocks) + p.tail_blocks;
-  const int rc = s.D == 128 ? (out_bf16 ? shared_rows<128, 1>(P, p.wr, blocks, st)
-                                        : shared_rows<128, 2>(P, p.wr, blocks, st))
-                            : (out_bf16 ? shared_rows<64, 1>(P, p.wr, blocks, st)
-                                        : shared_rows<64, 2>(P, p.wr, blocks, st));
+  // A prefix that one block of rows reads once goes past the caches from 40 MiB of keys and kept values
+  // (half of them, say) on.  In us with / without, D = 128, 28 rows, 10 prefixes in turn: 4 x 16384 tokens,
+  // 24 MiB, 15.1 / 15.2; 32768 tokens 18.9 / 20.4; 65536 tokens 26.2 / 29.3; 63 rows, 131072 tokens 53 /
+  // 56.  One prefix alone, out of the last-level cache: 131072 tokens 41.6 / 38.4.  (4 wavefronts to a
+  // tile gain 1 .. 3 %, and lose as much.)
+  const bool stream = p.row_blocks == 1 && 3ll * s.Hkv * k_pages * kPage * s.D > (40ll << 20);
+  const int rc = s.D == 128 ? (out_bf16 ? shared_list<128, 1>(P, p.wr, stream, blocks, st)
+                                        : shared_list<128, 2>(P, p.wr, stream, blocks, st))
+                            : (out_bf16 ? shared_list<64, 1>(P, p.wr, stream, blocks, st)
+                                        : shared_list<64, 2>(P, p.wr, stream, blocks, st));
   if (rc) return -1;
   const int rows = s.B * s.Hq;
   // 4 wavefronts for a row of many partial results: 64 of them 17.2 us for the whole call, with one

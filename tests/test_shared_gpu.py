@@ -413,3 +413,14 @@ def test_tensors_of_another_shape_or_type_are_refused():
     for i, v in ((7, 4), (11, -1), (13, ws[:16]), (10, None)):
         with pytest.raises(stc.StcError):
             stc.stc_decode_attention_shared(*ok[:i], v, *ok[i + 1:])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,Hkv,N", [(128, 8, 15000), (64, 16, 15003)])
+@pytest.mark.parametrize("B", [7, 20])
+def test_past_the_caches(B, D, Hkv, N, dtype):
+    """Enough of the prefix in one call for loads past the caches; and with the last pages first."""
+    c = Case(B, 2 * Hkv, Hkv, D, N, 8, 12, seed=B)
+    c.check(dtype)
+    NP = (N + 15) // 16
+    c.check(dtype, pages=np.tile(np.arange(NP)[::-1], (Hkv, 1)))
