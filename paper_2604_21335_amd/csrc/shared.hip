@@ -924,10 +924,14 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
   const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
   if (tail_cap > 0) {
-    // 4 pieces for every wavefront of the chip where all tails are full, but not so small that their
-    // partial results pass 1/16 of their keys and values (8 and no limit: 166 us for the 4 layers' 153)
-    long long t = (streams * tail_max + 4 * 2048 - 1) / (4 * 2048);
-    if (t < (s.Hq / s.Hkv + 1) / 2) t = (s.Hq / s.Hkv + 1) / 2;
+    // 4 pieces for every wavefront of the chip where all tails are full (8 and no limit: 166 us for 153, a
+    // token of 48 sequences through 4 layers), but not so small that their partial results pass 1/16 of
+    // their keys and values; 1/32 where that still leaves a piece for every wavefront (142 -> 137 us there;
+    // 160 tails of 700 tokens would be too few pieces, 14 -> 16)
+    const long long all = streams * tail_max, R = s.Hq / s.Hkv;
+    long long t = (all + 4 * 2048 - 1) / (4 * 2048);
+    const long long least = all >= 2048 * R ? R : (R + 1) / 2;
+    if (t < least) t = least;
     if (t > tail_max) t = tail_max;
     p.tail_tiles = (int)t;
     p.tail_splits = (tail_max + p.tail_tiles - 1) / p.tail_tiles;
