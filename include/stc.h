@@ -402,6 +402,8 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *            (all listed pages outside the prefix, an empty tail) gets zeros
  *   ws       stc_shared_workspace_bytes(shape, k_pages, tail_cap) bytes; calls whose work overlaps in
  *            time need one each
+ * Logits (q . k / sqrt(D)) count up to a magnitude of 2^29; a sequence's larger ones, infinities and NaN
+ * give meaningless results in its own rows of out.
  * For float output the softmax's weights are carried as bf16 parts, two for the prefix (2^-16) and three
  * for the tails (2^-24), for bf16 output as one (2^-8, as the output's own rounding).  The results depend
  * on the sizes, not on other sequences' lengths.

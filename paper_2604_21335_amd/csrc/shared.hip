@@ -103,6 +103,8 @@ __device__ __forceinline__ void split(float x, float y, float& l, Put put) {
     x -= bf16_lo(w), y -= bf16_hi(w);
   }
 }
+// m is a rounded product: it is off from the largest logit's by up to 2^-24 of itself, a factor that all of a
+// row's weights have in common.  Below 2^30 it stays within 2^64.
 __device__ __forceinline__ float weight(float s, float scale, float m) {
   return __builtin_amdgcn_exp2f(fmaf(s, scale, -m));
 }
@@ -613,6 +615,7 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
   };
   auto pieces_of = [&](int n) { return (uint32_t)(n + per - 1) / (uint32_t)per; };
   uint32_t total = 0;
+#pragma unroll 4
   for (int base = 0; base < P.B; base += 64)
     total += wave_reduce(pieces_of(lengths(base)), OpAdd{}, 0u);
   const uint64_t all = (uint64_t)total * P.Hkv;
@@ -956,6 +959,8 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
     }
     if (ts >= most) break;
   }
+  // More row blocks than 4 rounds hold: one split, and half of the units for the tails
+  if (best == 0 && tail_cap > 0) tail_slots = most < 16 ? most : 16;
   p.split_tiles = (tiles + splits - 1) / splits;
   p.splits = (tiles + p.split_tiles - 1) / p.split_tiles;
   p.tail_blocks = kXcds * tail_slots;

@@ -424,3 +424,56 @@ def test_past_the_caches(B, D, Hkv, N, dtype):
     c.check(dtype)
     NP = (N + 15) // 16
     c.check(dtype, pages=np.tile(np.arange(NP)[::-1], (Hkv, 1)))
+
+
+@pytest.mark.parametrize("B,R,Hkv,cap", [(6, 4, 2, 40), (40, 5, 1, 40), (300, 1, 4, 90)])
+def test_what_is_not_finite_stays_in_its_row(B, R, Hkv, cap):
+    """NaN and infinities in one sequence's query, tails or padding do not reach the others."""
+    c = Case(B, R * Hkv, Hkv, 128, 300, 8, cap, n_tail=[3, cap, -1, 7, 0])
+    want = c.run()
+    q, Kt, Vt = (c.d[x].clone() for x in ("q", "Kt", "Vt"))
+    q[0, 0], q[2] = float("nan"), float("inf")
+    q[1, 1] = float("inf")
+    Kt[3, :, 2], Vt[3, :, 1] = float("inf"), float("nan")
+    got = c.run(q=q, Kt=Kt, Vt=Vt)
+    on = torch.from_numpy(c.n >= 0).to(DEV)[:, None].repeat(1, R * Hkv)
+    assert got[0, 0].isnan().all() and got[3].isnan().all()
+    on[0, 0] = on[1, 1] = False
+    on[3] = False
+    assert torch.equal(got[on], want[on]) and got[on].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,cap", [(3, 0), (3, 40), (40, 40), (300, 360)])
+def test_logits_far_below_zero(B, cap, dtype):
+    """Equal logits near the end of what counts: each of them is the largest."""
+    c = Case(B, 1, 1, 128, 300, 8, cap, n_tail=[5, 0, cap])
+    c.K[:], c.Kt[:], c.q[:] = 0x4680, 0x4680, 0xC500           # 2^14 and -2^11: logits of -1.4 * 2^28
+    c.d["K"], c.d["q"] = PT.to_dev_bf16(c.K), PT.to_dev_bf16(c.q)
+    if cap:
+        c.d["Kt"] = PT.to_dev_bf16(c.Kt)
+    got = c.run(dtype).double().cpu().numpy()
+    V = bits_to_f64(c.V[0]) * np.repeat((c.mask[0].astype(int)[:, None] >> np.arange(8)) & 1, 16, axis=1)
+    for b in range(B):
+        n = max(int(c.n[b]), 0) if cap else 0
+        want = (V.sum(0) + (bits_to_f64(c.Vt[b, 0, :n]).sum(0) if n else 0)) / (300 + n)
+        # weights of one; sums of at most 660 values below 6 in float, one rounding to the output's type
+        lim = 660 * 2.0 ** -24 * 6 + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0)
+        assert (np.abs(got[b, 0] - want) <= lim).all()
+
+
+def test_no_tails_at_all():
+    c, *_ = _prefix()
+    q = torch.randn(4, 8, 128, device=DEV).bfloat16()
+    none = stc.SharedPrefix(c, 4, 0)
+    some = stc.SharedPrefix(c, 4, 20)
+    assert (none.attend(q) - some.attend(q)).abs().max() <= 4e-5
+    with pytest.raises(stc.StcError):
+        none.append(q, q[:, :2], q[:, :2])
+
+
+def test_thousands_of_sequences():
+    """More rows than one round of row blocks holds, and lengths that take many scans to add up."""
+    B, R, D = 2100, 16, 64
+    c = Case(B, R, 1, D, 40, 4, 3, n_tail=[0, 3, -1, 2, 1, 3, 0])
+    c.check(BF16)
