@@ -799,10 +799,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
                                  blockIdx.x * kWaves + wave, P.tail_blocks * kWaves);
     return;
   }
-  // the row blocks of a split share its keys and values: same id modulo the 8 XCDs
-  const int id = blockIdx.x - P.tail_blocks;
-  const int each = kXcds * P.row_blocks;
-  const int u = id / each * kXcds + id % kXcds, rb = id % each / kXcds;
+  // Each of the 8 XCDs (id modulo 8) takes an eighth of the row blocks of all splits, in order: those of
+  // one split share its keys and values.
+  const int id = blockIdx.x - P.tail_blocks, each = (gridDim.x - P.tail_blocks) / kXcds;
+  const int at = id % kXcds * each + id / kXcds;
+  const int u = at / P.row_blocks, rb = at % P.row_blocks;
   if (u >= P.Hkv * P.splits) return;
   const int kvh = u / P.splits, split = u % P.splits;
   constexpr int T = form_tile(WR), WK = kWaves / WR;
@@ -939,18 +940,18 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
     p.tail_tiles = (int)t;
     p.tail_splits = (tail_max + p.tail_tiles - 1) / p.tail_tiles;
   }
-  // The row blocks of a split stay on one of 8 XCDs of 32 compute units, so splits come in whole rounds
-  // of an XCD; the tails get compute units of their own from the start.  Of the ways to share these out,
-  // with splits that fill up to 4 rounds, the one that ends first: a tile of time for each tile of a
-  // split, two for starting and ending a workgroup, and the traffic of the partial results; a tail's
-  // tile, counted as half full, is half of one.
+  // An XCD has 32 compute units.  The tails get `ts` of each from the start; the splits' row blocks fill
+  // the others, in up to 4 rounds.  Of the ways to share the units out, the one that ends first: a tile of
+  // time for each tile of a split, two for starting and ending a workgroup, and the traffic of the partial
+  // results; a tail's tile, counted as half full, is 0.6 of one (0.3 and 1.0 are up to 10 and 18 % slower,
+  // at 48 and 64 sequences of 8 KV heads).
   double best = 0;
   int splits = 1, tail_slots = tail_cap > 0 ? 1 : 0;
   const int most = tail_cap > 0 ? (int)((streams * p.tail_splits + 8 * kWaves - 1) / (8 * kWaves)) : 0;
   for (int ts = tail_slots; ts <= 31; ts += ts < 4 ? 1 : 4) {
     const double tails = tail_cap > 0 ? 2.0 + 0.6 * streams * tail_max / (8.0 * kWaves * ts) : 0;
     for (int rounds = 1; rounds <= 4; ++rounds) {
-      long long n = (long long)kXcds * ((32 * rounds - ts) / p.row_blocks) / s.Hkv;
+      long long n = (long long)kXcds * (32 * rounds - ts) / p.row_blocks / s.Hkv;
       if (n < 1) continue;
       if (n > tiles) n = tiles;
       const double prefix = rounds * ((tiles + n - 1) / n + 2.0);
@@ -1022,10 +1023,10 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   P.row_blocks = p.row_blocks, P.splits = p.splits, P.split_tiles = p.split_tiles;
   P.tail_splits = p.tail_splits, P.tail_tiles = p.tail_tiles > 0 ? p.tail_tiles : 1;
   P.out_bf16 = out_bf16;
-  const long long units = (s.Hkv * (long long)p.splits + kXcds - 1) / kXcds * kXcds;
-  if (units * p.row_blocks > (1 << 30)) return -1;
+  const long long items = ((long long)s.Hkv * p.splits * p.row_blocks + kXcds - 1) / kXcds * kXcds;
+  if (items > (1 << 30)) return -1;
   P.tail_blocks = p.tail_blocks;
-  const int blocks = (int)(units * p.row_blocks) + p.tail_blocks;
+  const int blocks = (int)items + p.tail_blocks;
   // A prefix that one block of rows reads once goes past the caches from 40 MiB of keys and kept values
   // (half of them, say) on.  In us with / without, D = 128, 28 rows, 10 prefixes in turn: 4 x 16384 tokens,
   // 24 MiB, 15.1 / 15.2; 32768 tokens 18.9 / 20.4; 65536 tokens 26.2 / 29.3; 63 rows, 131072 tokens 53 /

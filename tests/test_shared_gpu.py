@@ -472,8 +472,8 @@ def test_no_tails_at_all():
         none.append(q, q[:, :2], q[:, :2])
 
 
-def test_thousands_of_sequences():
-    """More rows than one round of row blocks holds, and lengths that take many scans to add up."""
-    B, R, D = 2100, 16, 64
-    c = Case(B, R, 1, D, 40, 4, 3, n_tail=[0, 3, -1, 2, 1, 3, 0])
+@pytest.mark.parametrize("B,R,Hkv", [(2100, 16, 1), (9000, 16, 1), (1500, 5, 3)])
+def test_thousands_of_sequences(B, R, Hkv):
+    """More rows than some rounds of row blocks hold, and lengths that take many scans to add up."""
+    c = Case(B, R * Hkv, Hkv, 64, 40, 4, 3, n_tail=[0, 3, -1, 2, 1, 3, 0])
     c.check(BF16)
