@@ -9,15 +9,15 @@
 // partial results of a row.
 //
 // What bounds it (D = 128, half of the value groups kept):
-//   few rows, long prefix: 16 x 28 rows over 32768 tokens 27 us, the bytes of the cache 10.  Of the first
-//     launch's 22, 6 go by before the first product (kernel, masks and offsets, values: a chain of loads),
+//   few rows, long prefix: 16 x 28 rows over 32768 tokens 26 us, the bytes of the cache 10.  Of the first
+//     launch's 21, 6 go by before the first product (kernel, masks and offsets, values: a chain of loads),
 //     13 in the loop at half of the matrix units' rate, 2 into writing partial results; the merge takes 5.
 //   many rows: 256 x 28 over 32768 tokens, 136 us, 90 GFLOP of kept values (120 with the dropped ones, which
 //     are multiplied as zeros: 890 TFLOP/s, a library's largest product 1220 .. 1360 on the card).  The
 //     exponentials share the wavefronts' issue with the matrix instructions, and the card's power holds
 //     the clock down; without exponentials it would be 129.
-//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 30.5 us, 138 MB at
-//     4.5 TB/s with the merge's launch, where a copy reaches 5.1.
+//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 .. 32 us, 138 MB at
+//     4.3 .. 4.8 TB/s with the merge's launch, where a copy reaches 5.1.
 #include "stc_common.hpp"
 #include "stc_kernels.hpp"
 
