@@ -404,9 +404,9 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *            time need one each
  * Logits (q . k / sqrt(D)) count up to a magnitude of 2^29; a sequence's larger ones, infinities and NaN
  * give meaningless results in its own rows of out.
- * For float output the softmax's weights are carried as bf16 parts, two for the prefix (2^-16) and three
- * for the tails (2^-24), for bf16 output as one (2^-8, as the output's own rounding).  The results depend
- * on the sizes, not on other sequences' lengths.
+ * The softmax's weights are carried as bf16 parts, two for the prefix (2^-16) and three for the tails (2^-24);
+ * sums are float; the output's type says how the result is rounded and nothing else.  The results depend on
+ * the sizes, not on other sequences' lengths.
  */
 enum { STC_OUT_F32 = 0, STC_OUT_BF16 = 1 };
 size_t stc_shared_workspace_bytes(const stc_shape_t *shape, int k_pages, int tail_cap);

@@ -12,10 +12,9 @@
 //   few rows, long prefix: 16 x 28 rows over 32768 tokens 26 us, the bytes of the cache 10.  Of the first
 //     launch's 21, 6 go by before the first product (kernel, masks and offsets, values: a chain of loads),
 //     13 in the loop at half of the matrix units' rate, 2 into writing partial results; the merge takes 5.
-//   many rows: 256 x 28 over 32768 tokens, 136 us, 90 GFLOP of kept values (120 with the dropped ones, which
-//     are multiplied as zeros: 890 TFLOP/s, a library's largest product 1220 .. 1360 on the card).  The
-//     exponentials share the wavefronts' issue with the matrix instructions, and the card's power holds
-//     the clock down; without exponentials it would be 129.
+//   many rows: 256 x 28 over 32768 tokens, 181 us; 90 GFLOP of kept values, 180 with the dropped ones, which are
+//     multiplied as zeros, and the second parts of the weights: 1000 TFLOP/s, a library's largest product 1220 ..
+//     1360 on the card.
 //   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 .. 32 us, 138 MB at
 //     4.3 .. 4.8 TB/s with the merge's launch, where a copy reaches 5.1.
 #include "stc_common.hpp"
@@ -42,6 +41,7 @@ constexpr int kXcds = 8, kUnits = 256;  // XCDs, compute units of all of them
 // A maximum that grows by less than this (base 2) leaves the sums as they are: the weights then reach
 // 2^8, far from the range of a float, and 64 multiplications per tile are saved.
 constexpr float kSlack = 8.0f;
+constexpr int kParts = 2, kTailParts = 3;  // bf16 parts of a weight, in the prefix and in the tails
 
 struct SharedParams {
   const uint16_t* q;
@@ -85,21 +85,19 @@ __device__ __forceinline__ float over_groups(float x, Op op) {
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
-// Two weights in PARTS bf16 parts, put(part, both as one word); l: their sum, of the weights as they are
-// used.  A part leaves 2^-8 of what it rounds.  One does for bf16 output, whose own rounding is as large.
-// For float output the prefix takes two (2^-16, and errors of many weights cancel: outputs are off by some
-// 10^-6): three would cost 1 .. 18 % there, where the matrix units are what is short.  The tails take three
-// (2^-24, a float's own), where they are not and a row may have few tokens.
+// Two weights in PARTS bf16 parts, put(part, both as one word); l: their sum.  A part leaves 2^-8 of what it
+// rounds.  The prefix takes two (2^-16, and errors of many weights cancel: float outputs are off by some 10^-6):
+// three would cost 1 .. 18 % there, where the matrix units are what is short.  One would be 20 % faster with many
+// rows (256 x 28 over 32768 tokens, 181 us -> 145), but puts an error as large as the output's own rounding beside
+// it where the output is bf16: 0.0021 of the output's norm where the rounding alone is 0.0017.  The tails take
+// three (2^-24, a float's own), where the matrix units are not short and a row may have few tokens.
 template <int PARTS, class Put>
 __device__ __forceinline__ void split(float x, float y, float& l, Put put) {
-  if constexpr (PARTS > 1) l += x + y;
+  l += x + y;
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) {
     const uint32_t w = pack_bf16(x, y);
     put(k, w);
-    if constexpr (PARTS == 1)
-      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w),
-                                          __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
     x -= bf16_lo(w), y -= bf16_hi(w);
   }
 }
@@ -173,7 +171,7 @@ constexpr int kPast = 2;                    // non-temporal: past the caches
 // Tiles [tile0, tile1) of the prefix for the query rows q_row(0 ..) of one KV head; tile t of key group
 // g is tile t * WK + g.  The groups' results are merged; the partial result of row r goes to index(r)
 // (negative: nowhere).
-template <int D, int WR, int T, int STAGES, int PARTS, bool LIST, bool STREAM, class Row, class Index>
+template <int D, int WR, int T, int STAGES, bool LIST, bool STREAM, class Row, class Index>
 __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int tile0,
                                        int tile1, Row q_row, Index index) {
   using C = Cfg<D, WR, T, STAGES>;
@@ -387,7 +385,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, int sub2, const Tile& x1, auto between) {
     constexpr int QK = D / 16, HALF = D / 32;  // products of the logits; of the values, per half
     constexpr int STEPS = 2 * QK;
-    u32x4 p[PARTS][2];
+    u32x4 p[kParts][2];
     f32x16 N = {};
     auto read = [&](auto s) {  // the operand of product s
       if constexpr (s < QK) {
@@ -408,7 +406,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     static_for<0, STEPS>([&](auto s) {
       static_for<0, 8>([&](auto j) {
         if constexpr (pair_at(j) + 1 == s)
-          split<PARTS>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
+          split<kParts>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
       });
       if constexpr (NEXT || s >= QK) read(IC<s + 3>{});
       if constexpr (s < QK) {
@@ -416,7 +414,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       } else {
         constexpr int v = s - QK;
 #pragma unroll
-        for (int k = PARTS - 1; k >= 0; --k)
+        for (int k = kParts - 1; k >= 0; --k)
           O[v % HALF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
               ring[s % 4], __builtin_bit_cast(bf16x8, p[k][v / HALF]), O[v % HALF], 0, 0, 0);
         if constexpr (v == HALF) made_by_now(l);
@@ -602,7 +600,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 // begins depends on the sizes alone.  The R <= 16 query rows are the columns of 16x16x32 products:
 //   lane (column c, group g of 4) holds tokens 4 g + i and 16 + 4 g + i of S^T, which is the operand of
 //   the second product if the values' tokens are taken in the same order.
-template <int D, int PARTS>
+template <int D>
 __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, int w, int nw) {
   using C = Cfg<D, 1, kTailTile, 1>;
   constexpr int RB = C::RB, NI = C::NI;
@@ -741,10 +739,10 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
 #pragma unroll
         for (int j = 0; j < 4; ++j) O[i][j] *= f;
     }
-    u32x4 p[PARTS];
+    u32x4 p[kTailParts];
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      split<PARTS>(weight(S[i / 4][i % 4], scale, m), weight(S[i / 4][i % 4 + 1], scale, m), l,
+      split<kTailParts>(weight(S[i / 4][i % 4], scale, m), weight(S[i / 4][i % 4 + 1], scale, m), l,
                    [&](int k, uint32_t w) { p[k][i / 2] = w; });
 #pragma unroll
     for (int cb = 0; cb < D / 16; ++cb) {
@@ -758,7 +756,7 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
       const bf16x8 vv =
           __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-      for (int k = PARTS - 1; k >= 0; --k)
+      for (int k = kTailParts - 1; k >= 0; --k)
         O[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, __builtin_bit_cast(bf16x8, p[k]), O[cb], 0, 0, 0);
     }
     wave_lds_sync();
@@ -790,12 +788,12 @@ constexpr int shared_lds() {
   return a > b ? a : b;
 }
 
-template <int D, int WR, int PARTS, bool LIST, bool STREAM>
+template <int D, int WR, bool LIST, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    tails<D, PARTS == 1 ? 1 : 3>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE,
+    tails<D>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE,
                                  blockIdx.x * kWaves + wave, P.tail_blocks * kWaves);
     return;
   }
@@ -810,7 +808,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) 
   const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
   const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
   const int rows = P.B * P.R, row0 = rb * WR * kRows;
-  attend<D, WR, T, form_stages(WR), PARTS, LIST, STREAM>(
+  attend<D, WR, T, form_stages(WR), LIST, STREAM>(
       P, lds, kvh, t0, t1,
       [&](int r) -> const uint16_t* {
         r += row0;
@@ -972,31 +970,31 @@ size_t partials(const stc_shape_t& s, const SharedPlan& p) {
   return (size_t)s.B * s.Hq * (p.splits + p.tail_splits);
 }
 
-template <int D, int WR, int PARTS, bool LIST, bool STREAM>
+template <int D, int WR, bool LIST, bool STREAM>
 int shared_go(const SharedParams& P, int blocks, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int lds = shared_lds<D, WR>();
-  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, PARTS, LIST, STREAM>, lds, done)) return -1;
-  shared_kernel<D, WR, PARTS, LIST, STREAM><<<blocks, 64 * kWaves, lds, st>>>(P);
+  if (!allow_dynamic_lds((const void*)shared_kernel<D, WR, LIST, STREAM>, lds, done)) return -1;
+  shared_kernel<D, WR, LIST, STREAM><<<blocks, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-template <int D, int PARTS, bool LIST>
+template <int D, bool LIST>
 int shared_rows(const SharedParams& P, int wr, bool stream, int blocks, hipStream_t st) {
   if (wr == 1)
-    return stream ? shared_go<D, 1, PARTS, LIST, true>(P, blocks, st)
-                  : shared_go<D, 1, PARTS, LIST, false>(P, blocks, st);
+    return stream ? shared_go<D, 1, LIST, true>(P, blocks, st)
+                  : shared_go<D, 1, LIST, false>(P, blocks, st);
   if (wr == 2)
-    return stream ? shared_go<D, 2, PARTS, LIST, true>(P, blocks, st)
-                  : shared_go<D, 2, PARTS, LIST, false>(P, blocks, st);
-  return wr == 4 ? shared_go<D, 4, PARTS, LIST, false>(P, blocks, st)
-                 : shared_go<D, 8, PARTS, LIST, false>(P, blocks, st);
+    return stream ? shared_go<D, 2, LIST, true>(P, blocks, st)
+                  : shared_go<D, 2, LIST, false>(P, blocks, st);
+  return wr == 4 ? shared_go<D, 4, LIST, false>(P, blocks, st)
+                 : shared_go<D, 8, LIST, false>(P, blocks, st);
 }
 
-template <int D, int PARTS>
+template <int D>
 int shared_list(const SharedParams& P, int wr, bool stream, int blocks, hipStream_t st) {
-  return P.pages ? shared_rows<D, PARTS, true>(P, wr, stream, blocks, st)
-                 : shared_rows<D, PARTS, false>(P, wr, stream, blocks, st);
+  return P.pages ? shared_rows<D, true>(P, wr, stream, blocks, st)
+                 : shared_rows<D, false>(P, wr, stream, blocks, st);
 }
 
 }  // namespace
@@ -1033,10 +1031,8 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   // 56.  One prefix alone, out of the last-level cache: 131072 tokens 41.6 / 38.4.  (4 wavefronts to a
   // tile gain 1 .. 3 %, and lose as much.)
   const bool stream = p.row_blocks == 1 && 3ll * s.Hkv * k_pages * kPage * s.D > (40ll << 20);
-  const int rc = s.D == 128 ? (out_bf16 ? shared_list<128, 1>(P, p.wr, stream, blocks, st)
-                                        : shared_list<128, 2>(P, p.wr, stream, blocks, st))
-                            : (out_bf16 ? shared_list<64, 1>(P, p.wr, stream, blocks, st)
-                                        : shared_list<64, 2>(P, p.wr, stream, blocks, st));
+  const int rc = s.D == 128 ? shared_list<128>(P, p.wr, stream, blocks, st)
+                            : shared_list<64>(P, p.wr, stream, blocks, st);
   if (rc) return -1;
   const int rows = s.B * s.Hq;
   // 4 wavefronts for a row of many partial results: 64 of them 17.2 us for the whole call, with one

@@ -477,3 +477,14 @@ def test_thousands_of_sequences(B, R, Hkv):
     """More rows than some rounds of row blocks hold, and lengths that take many scans to add up."""
     c = Case(B, R * Hkv, Hkv, 64, 40, 4, 3, n_tail=[0, 3, -1, 2, 1, 3, 0])
     c.check(BF16)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,R,Hkv,cap,N", [(3, 4, 2, 0, 700), (9, 7, 2, 40, 300), (40, 3, 1, 200, 20),
+                                           (150, 2, 4, 180, 500)])
+def test_bf16_output_is_the_float_output_rounded(B, R, Hkv, cap, N, D):
+    """The output's type chooses the output's rounding and nothing else: the weights behind it are those
+    of the float output.  Both runs add the same numbers in the same order, so the one rounding, to the
+    nearest, is all that may lie between them."""
+    c = Case(B, R * Hkv, Hkv, D, N, 8, cap, seed=N + B, n_tail=[cap, 0, 3, cap // 2])
+    assert torch.equal(c.run(BF16), c.run(F32).bfloat16())
