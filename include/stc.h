@@ -397,7 +397,8 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16, in (may be NULL when tail_cap == 0)
  *   n_tail   [B] int32 on the device, in: rows 0 .. n_tail[b]-1 of sequence b's tails are attended
  *            (counted as tail_cap if larger); n_tail[b] < 0: b is padding, its rows of out are left as
- *            they are.  May be NULL when tail_cap == 0: no tails, no padding
+ *            they are.  Must not change while the call works.  May be NULL when tail_cap == 0: no tails,
+ *            no padding
  *   out      [B, Hq, D], out, float (STC_OUT_F32) or bf16 (STC_OUT_BF16).  A query without any token
  *            (all listed pages outside the prefix, an empty tail) gets zeros
  *   ws       stc_shared_workspace_bytes(shape, k_pages, tail_cap) bytes; calls whose work overlaps in

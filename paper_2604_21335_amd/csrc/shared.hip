@@ -621,10 +621,12 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
   const uint32_t end = (uint32_t)(all * (w + 1) / nw);
   if (at >= end) return;
 
-  // the sequence that piece `at` belongs to
-  int base = 0, lens = lengths(0), b = 0, n = 0;
+  // The sequence that piece `at` belongs to.  `all` > `at`, so some sequence holds it; but the lengths are read
+  // anew here, and a caller that changes them meanwhile must not leave a wavefront searching for ever (the
+  // results are then meaningless, within the workspace: a piece's place follows from one reading of a length).
+  int base = 0, lens = lengths(0), b = P.B, n = 0;
   uint32_t seen = 0, in_b = 0;  // pieces in front of sequence b; of sequence b, all KV heads
-  for (;; base += 64, lens = lengths(base)) {
+  for (; base < P.B; base += 64, lens = lengths(base)) {
     const uint32_t mine = pieces_of(lens), incl = wave_scan(mine, OpAdd{}, 0u);
     const uint64_t past = __builtin_amdgcn_ballot_w64((seen + incl) * (uint64_t)P.Hkv > at);
     if (past) {
@@ -637,7 +639,7 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
     }
     seen += __builtin_amdgcn_readlane(incl, 63);
   }
-  // (`all` > `at`, so some sequence holds it)
+  if (b >= P.B) return;
   int kvh, piece, t, t_end;
   auto open = [&] {  // the place of piece `at` in sequence b
     const uint32_t np = pieces_of(n), i = at - seen;
@@ -700,14 +702,15 @@ __device__ __forceinline__ void tails(const SharedParams& P, unsigned char* st, 
     } else if (++at < end) {
       if (at - seen >= in_b) {  // the next sequence with a tail
         seen += in_b;
-        do {
-          if (++b == base + 64) base += 64, lens = lengths(base);
+        n = 0;
+        while (n == 0 && ++b < P.B) {
+          if (b == base + 64) base += 64, lens = lengths(base);
           n = __builtin_amdgcn_readlane(lens, b - base);
-        } while (n == 0);
+        }
         in_b = pieces_of(n) * P.Hkv;
       }
-      open();
-      ask_q();
+      more = n > 0;
+      if (more) open(), ask_q();
     } else {
       more = false;
     }
