@@ -493,7 +493,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
         if constexpr (s == 0) put(pk, kr);
         if constexpr (s == 1) put_meta(meta), meta = ask_meta(tile(t, IC<A + 2>{}));
         if constexpr (s == 2) put(pv, vr);
-        if constexpr (s == 3) get_meta(e);
+        if constexpr (s == 3) wave_lds_sync(), get_meta(e);
         if constexpr (s == 4) advance(pk, put_stage), advance(pv, put_stage), on(put_stage);
       };
       auto ask = [&](auto s) {
