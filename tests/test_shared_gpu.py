@@ -93,7 +93,7 @@ class Case:
         return got
 
 
-# rows of a KV head on both sides of every change of the form (32, 64, 128 of them), partly filled
+# rows of a KV head on both sides of 32, 64 (other forms) and 128 (more blocks of rows), partly filled
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("D,G", [(128, 8), (64, 4)])
 @pytest.mark.parametrize("B,R,Hkv", [(1, 1, 1), (3, 5, 2), (2, 16, 1), (33, 1, 2), (4, 16, 2), (13, 5, 1),
@@ -488,3 +488,50 @@ def test_bf16_output_is_the_float_output_rounded(B, R, Hkv, cap, N, D):
     nearest, is all that may lie between them."""
     c = Case(B, R * Hkv, Hkv, D, N, 8, cap, seed=N + B, n_tail=[cap, 0, 3, cap // 2])
     assert torch.equal(c.run(BF16), c.run(F32).bfloat16())
+
+
+def check_some(c, some, dtype, pages=None):
+    """Case.check for the sequences `some` and the first and last KV head, where the oracle would take long
+    for all of them."""
+    heads = sorted({0, c.Hkv - 1})
+    rows = [h * (c.Hq // c.Hkv) + r for h in heads for r in range(c.Hq // c.Hkv)]
+    got = c.run(dtype, pages).double().cpu().numpy()[some][:, rows]
+    tails = (c.Kt[some][:, heads], c.Vt[some][:, heads]) if c.cap else (None, None)
+    want, size, top = O.shared_attention_all(c.q[some][:, rows], c.K[heads], c.V[heads], c.mask[heads],
+                                             pages if pages is None else pages[heads], c.G, *tails, c.n[some])
+    lim = limits(want, size, top, c.N + c.cap, c.D, dtype)
+    bad = ~(np.abs(got - want) <= lim)
+    assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], lim[bad][:4])
+
+
+# (sequences, query heads to a KV head, KV heads, tokens, room of the tails), tokens that a turn of the
+# loop takes from a split: all tokens that stand between two of one group of wavefronts' tiles
+TURNS = [((2, 16, 8, 20003, 0), 256), ((30, 1, 16, 12003, 9), 256),       # a wavefront to a tile
+         ((4, 16, 8, 20003, 0), 128), ((8, 8, 8, 16003, 40), 128),        # 2
+         ((64, 16, 1, 9003, 33), 64), ((150, 7, 2, 20011, 0), 64),        # 4
+         ((48, 8, 8, 4001, 1000), 64), ((300, 1, 16, 15011, 0), 64)]      # 8: beside tails, a long prefix
+
+
+def turns_of(c, turn, k):
+    """Turns of the splits' loops in the mean, at least (more than 2: some split takes 3): the workspace holds
+    a partial result of every query for each split and each piece of the tails."""
+    parts = stc.stc_shared_workspace_bytes(c.shape, k, c.cap) // (c.B * c.Hq * (c.D + 2) * 4)
+    return k * 16 / parts / turn
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("plan,turn", TURNS)
+def test_many_tiles_a_split(plan, turn, D):
+    """Loops that run for some turns: what they fetch while they work is attended, with and without a list
+    of pages, up to a ragged end."""
+    B, R, Hkv, N, cap = plan
+    c = Case(B, R * Hkv, Hkv, D, N, 8, cap, seed=N, n_tail=[cap, 0, cap // 2, 3], n_cap=N + 20)
+    NP = (N + 15) // 16
+    assert turns_of(c, turn, NP) > 2
+    some = [0, B // 2, B - 1]
+    pages = np.stack([np.random.default_rng(h).permutation(NP)[:NP - 5] for h in range(Hkv)])
+    pages[0, 40], pages[-1, -1], pages[0, 3] = -1, NP, 2**31 - 1
+    pages[0, -1] = NP - 1 if NP - 1 not in pages[0] else pages[0, -1]
+    for dtype in (F32, BF16):
+        check_some(c, some, dtype)
+        check_some(c, some, dtype, pages)
