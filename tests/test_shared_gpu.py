@@ -535,3 +535,49 @@ def test_many_tiles_a_split(plan, turn, D):
     for dtype in (F32, BF16):
         check_some(c, some, dtype)
         check_some(c, some, dtype, pages)
+
+
+def ramp(c, which, per, step, tokens):
+    """Logits of `which` (K or Kt) that rise by `step` in base 2 over `per` tokens, around zero."""
+    from tests.helpers import f32_to_bf16_bits
+    q = f32_to_bf16_bits(bits_to_f64(c.q) * 0.25)
+    q[..., 0] = 0x4100                                         # 8
+    at = np.arange(getattr(c, which).shape[-2]) - tokens / 2
+    getattr(c, which)[..., 0] = f32_to_bf16_bits(at * (step / per * np.sqrt(c.D) / 8.0 / np.log2(np.e)))
+    c.d["q"], c.q, plain = PT.to_dev_bf16(q), q, c.q
+    c.d[which] = PT.to_dev_bf16(getattr(c, which))
+    return plain
+
+
+# Logits that rise from one tile of a group to its next by nearly what moves the running maximum, by a little
+# more and by much more, and that fall.  Sums that are not scaled down when the maximum moves are then off by
+# factors of 2^8 and more.
+STEPS = [7.5, 8.5, 40.0, 1.0, -8.5]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("plan,turn", [t for t in TURNS if t[0] in ((2, 16, 8, 20003, 0), (4, 16, 8, 20003, 0),
+                                                                    (64, 16, 1, 9003, 33), (48, 8, 8, 4001, 1000))])
+def test_maxima_that_move_inside_a_split(plan, turn, D):
+    B, R, Hkv, N, cap = plan
+    c = Case(B, R * Hkv, Hkv, D, N, 8, cap, seed=N, n_tail=[5, 0, cap])
+    assert turns_of(c, turn, (N + 15) // 16) > 2
+    for step in STEPS:
+        # (with 8 wavefronts the maximum may move every 32 tokens)
+        plain = ramp(c, "K", 32 if cap == 1000 else turn, step, N)
+        check_some(c, [0, B - 1], F32)
+        check_some(c, [B // 2], BF16)
+        c.q = plain
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_maxima_that_move_inside_a_tail(D, dtype):
+    """Pieces of 8 tiles of 32 tokens: a call of few long tails with 16 query heads to a KV head."""
+    c = Case(11, 16, 1, D, 50, 4, 700, seed=D, n_tail=[700, 257, 0, 480, 33, 699])
+    for step in STEPS:
+        plain = ramp(c, "Kt", 32, step, 700)
+        for b in range(c.B):
+            c.d["Kt"][b, :, c.n[b]:] = float("nan")
+        check_some(c, list(range(11)), dtype)
+        c.q = plain
