@@ -196,9 +196,8 @@ int launch_rotary(int B, int H, int N, int D, int rot_dim, int layout, const dou
                   float amplitude, const int32_t* pos, int pos0, const void* x, const int64_t* xs,
                   void* y, const int64_t* ys, hipStream_t st) {
   const Rows xr{xs[0] / 8, xs[1] / 8, xs[2] / 8}, yr{ys[0] / 8, ys[1] / 8, ys[2] / 8};
-  const bool same = x == y && xs[0] == ys[0] && xs[1] == ys[1] && xs[2] == ys[2];
   const int flags = (xs[1] <= xs[2] ? 1 : 0) | ((layout & 0xff) == STC_ROTARY_INTERLEAVED ? 2 : 0) |
-                    (layout & STC_ROTARY_INVERSE ? 4 : 0) | (same ? 8 : 0);
+                    (layout & STC_ROTARY_INVERSE ? 4 : 0) | (x == y ? 8 : 0);
   const long long rows = (long long)N * H;
   const dim3 grid((unsigned)((rows * (D / 16) + 255) / 256), B);
   // every store instruction writes whole lines, and more than the last-level cache holds goes through

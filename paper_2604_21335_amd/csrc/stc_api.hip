@@ -514,6 +514,10 @@ int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int3
     if (!stride_ok(x_stride[i]) || !stride_ok(y_stride[i])) return STC_ERR_ALIGN;
     if (sizes[i] > 1 && y_stride[i] < D) return STC_ERR_SHAPE;  // rows of y would overlap
   }
+  // in place only where every row stays where it is: others would be overwritten before they are read
+  if (x == y)
+    for (int i = 0; i < 3; ++i)
+      if (sizes[i] > 1 && x_stride[i] != y_stride[i]) return STC_ERR_SHAPE;
   return stc::launch_rotary(B, H, N, D, rot_dim, layout, turns, amplitude, pos, pos0, x, x_stride, y,
                             y_stride, (hipStream_t)stream)
              ? STC_ERR_LAUNCH

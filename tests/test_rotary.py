@@ -91,6 +91,15 @@ def test_rotary_refuses(kw, status):
     assert _call(**kw) == getattr(stc, "STC_ERR_" + status)
 
 
+# B, H, N = 2, 3, 5; in a dimension of one element the stride does not count
+@pytest.mark.parametrize("ys", [(1920, 640, 128), (1920, 128, 640), (3840, 128, 384)])
+def test_rotary_refuses_another_order_in_place(ys):
+    other = ctypes.c_void_p(0x100000)
+    assert _call(y=other, ys=ys, amp=math.nan) == stc.STC_ERR_SHAPE     # what is refused anyway
+    assert _call(ys=ys) == stc.STC_ERR_SHAPE
+    assert _call(ys=ys, D=64) == stc.STC_ERR_SHAPE
+
+
 def _append(shape=None, **kw):
     a = dict(q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, qo=ctypes.c_void_p(0x2000), Kt=FAKE,
              Vt=FAKE, n=FAKE, n_out=None, cap=16, rot=64, layout=0, turns=FAKE, amp=1.0, pos=None,

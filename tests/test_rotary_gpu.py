@@ -73,6 +73,21 @@ def test_in_place(layout):
     assert torch.equal(x, out)
 
 
+def test_in_place_in_another_order_is_refused():
+    """Rows would be overwritten before they are read; where a dimension holds one element its stride is no
+    order."""
+    x = torch.randn(2, 8, 8, 64, device=DEV).bfloat16()
+    t = stc.stc_rotary_turns(64).to(DEV)
+    before = x.clone()
+    with pytest.raises(stc.StcError) as e:
+        stc.stc_rotary(x, x.transpose(1, 2), t, 64, HALVES)
+    assert e.value.status == stc.STC_ERR_SHAPE and torch.equal(x, before)
+    one, want = x[:1, :1], torch.empty_like(x[:1, :1])
+    stc.stc_rotary(one, want, t, 64, HALVES)
+    stc.stc_rotary(one, one.as_strided(one.shape, (8, 4096, 64, 1)), t, 64, HALVES)
+    assert torch.equal(one, want) and torch.equal(x[1], before[1])
+
+
 @pytest.mark.parametrize("pos", [[0, -1, -5, 1], [2**31 - 1, -2**31, 10**6, 12345678], [3, 3, 3, 3]])
 def test_given_and_far_positions(pos):
     rng = np.random.default_rng(9)
