@@ -345,7 +345,8 @@ int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t *scaling, doubl
  *             strides of b, h and n in elements, multiples of 8, >= 0; a head's D channels (64 or 128)
  *             are contiguous.  So x may be a projection's output [B, N, H, D] and y a cache
  *             [B, H, N_cap, D].  y may be x with the same strides (of dimensions of one element
- *             they do not count); else the two must not overlap, nor rows of y with each other.
+ *             they do not count); else the two must not overlap.  Rows of y must not overlap each other: taken by
+ *             size, each stride is at least what the dimensions of smaller strides span.
  *   rot_dim   16, 32, .. D;  layout  STC_ROTARY_HALVES or _INTERLEAVED, | STC_ROTARY_INVERSE
  *   turns     [rot_dim/2] double, in
  *   amplitude finite; 1 but for methods that raise the logits of long contexts

@@ -1,6 +1,8 @@
 // C ABI of libstc: argument validation and dispatch to the kernel launchers.
 #include <math.h>
 
+#include <algorithm>
+
 #include "../../include/stc.h"
 #include "stc_kernels.hpp"
 
@@ -33,6 +35,21 @@ size_t select_ws_bytes(const stc_shape_t* s, bool per_head = false) {
 }
 
 bool rot_dim_ok(int rot_dim, int D) { return rot_dim >= 16 && rot_dim <= D && rot_dim % 16 == 0; }
+
+// Whether rows of D elements lie apart: every dimension's stride passes all that the dimensions of smaller
+// strides span.  (Strides that interleave without meeting would pass a closer look; no order of a tensor's
+// dimensions and no slice of one has such.)
+bool rows_apart(const int32_t* sizes, const int64_t* strides, int D) {
+  int at[3] = {0, 1, 2};
+  std::sort(at, at + 3, [&](int i, int j) { return strides[i] < strides[j]; });
+  __int128 span = D;
+  for (int i : at) {
+    if (sizes[i] == 1) continue;
+    if (strides[i] < span) return false;
+    span += (__int128)(sizes[i] - 1) * strides[i];
+  }
+  return true;
+}
 
 // Strides of rows that are read in 16-byte pieces, in bf16 elements.
 bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
@@ -510,10 +527,9 @@ int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int3
   if (!aligned16(turns) || !aligned16(x) || !aligned16(y) || (pos && ((uintptr_t)pos & 3)))
     return STC_ERR_ALIGN;
   const int32_t sizes[3] = {B, H, N};
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 3; ++i)
     if (!stride_ok(x_stride[i]) || !stride_ok(y_stride[i])) return STC_ERR_ALIGN;
-    if (sizes[i] > 1 && y_stride[i] < D) return STC_ERR_SHAPE;  // rows of y would overlap
-  }
+  if (!rows_apart(sizes, y_stride, D)) return STC_ERR_SHAPE;
   // in place only where every row stays where it is: others would be overwritten before they are read
   if (x == y)
     for (int i = 0; i < 3; ++i)

@@ -91,6 +91,13 @@ def test_rotary_refuses(kw, status):
     assert _call(**kw) == getattr(stc, "STC_ERR_" + status)
 
 
+# B, H, N, D = 2, 3, 5, 128
+@pytest.mark.parametrize("ys", [(1920, 128, 128), (1920, 128, 256), (640, 128, 384), (1920, 640, 120),
+                                (1912, 640, 128), (1920, 632, 128), (1 << 62, 128, 1 << 61)])
+def test_rotary_refuses_rows_that_overlap(ys):
+    assert _call(y=ctypes.c_void_p(0x100000), ys=ys) == stc.STC_ERR_SHAPE
+
+
 # B, H, N = 2, 3, 5; in a dimension of one element the stride does not count
 @pytest.mark.parametrize("ys", [(1920, 640, 128), (1920, 128, 640), (3840, 128, 384)])
 def test_rotary_refuses_another_order_in_place(ys):

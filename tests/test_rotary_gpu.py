@@ -73,6 +73,26 @@ def test_in_place(layout):
     assert torch.equal(x, out)
 
 
+@pytest.mark.parametrize("order", [(0, 1, 2), (0, 2, 1), (1, 0, 2), (1, 2, 0), (2, 0, 1), (2, 1, 0)])
+@pytest.mark.parametrize("step", [1, 3])
+def test_every_order_of_the_output(order, step):
+    """All orders of sequences, heads and tokens, and every third of them; one row too close is refused."""
+    sizes = (2, 3, 5)
+    whole = [sizes[d] * step for d in order]
+    y = torch.full((*whole, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    back = [order.index(d) for d in range(3)]
+    v = y[::step, ::step, ::step].permute(*back, 3)
+    x = torch.randn(*sizes, 64, device=DEV).bfloat16()
+    t, want = stc.stc_rotary_turns(64).to(DEV), torch.empty_like(x)
+    stc.stc_rotary(x, want, t, 64, INTER, pos0=4)
+    stc.stc_rotary(x, v, t, 64, INTER, pos0=4)
+    assert torch.equal(v, want) and (y == 7).sum() == y.numel() - x.numel()
+    close = y.as_strided((*sizes, 64), (15 * 64, 64, 128, 1))
+    with pytest.raises(stc.StcError):
+        stc.stc_rotary(x, close, t, 64, INTER)
+    assert torch.equal(v, want)
+
+
 def test_in_place_in_another_order_is_refused():
     """Rows would be overwritten before they are read; where a dimension holds one element its stride is no
     order."""
