@@ -352,7 +352,7 @@ int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t *scaling, doubl
  *   amplitude finite; 1 but for methods that raise the logits of long contexts
  *   pos       [B, N] int32, in: the tokens' positions (any value), or NULL: token n of every
  *             sequence stands at pos0 + n, which must not pass 2^31 - 1
- * B <= 65535, N * H < 2^31.
+ * B <= 65535, N * H * D <= 2^36 - 4096.
  */
 int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int32_t layout,
                const double *turns, float amplitude, const int32_t *pos, int32_t pos0, const void *x,

@@ -517,9 +517,11 @@ int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int3
                const double* turns, float amplitude, const int32_t* pos, int32_t pos0, const void* x,
                const int64_t* x_stride, void* y, const int64_t* y_stride, void* stream) {
   if (!turns || !x || !x_stride || !y || !y_stride) return STC_ERR_NULL;
-  if (B < 1 || B > kMaxGridY || H < 1 || N < 1 || (long long)N * H >= (1ll << 31) ||
-      (D != 64 && D != 128) || !rot_dim_ok(rot_dim, D) || !isfinite(amplitude))
+  if (B < 1 || B > kMaxGridY || H < 1 || N < 1 || (D != 64 && D != 128) || !rot_dim_ok(rot_dim, D) ||
+      !isfinite(amplitude))
     return STC_ERR_SHAPE;
+  // a thread for 16 channels, and a launch counts fewer than 2^32 threads, in workgroups of 256
+  if ((long long)N * H > ((1ll << 32) - 256) / (D / 16)) return STC_ERR_SHAPE;
   if ((layout & ~STC_ROTARY_INVERSE) != STC_ROTARY_HALVES &&
       (layout & ~STC_ROTARY_INVERSE) != STC_ROTARY_INTERLEAVED)
     return STC_ERR_SHAPE;

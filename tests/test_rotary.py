@@ -91,6 +91,15 @@ def test_rotary_refuses(kw, status):
     assert _call(**kw) == getattr(stc, "STC_ERR_" + status)
 
 
+@pytest.mark.parametrize("D,H,N", [(64, 1, (1 << 30) - 63), (128, 1, (1 << 29) - 31), (128, 1 << 15, 1 << 14),
+                                   (64, 1 << 10, 1 << 20), (64, 1, 2**31 - 1)])
+def test_rotary_refuses_more_than_a_launch_counts(D, H, N):
+    """2^32 threads and more, a thread for 16 channels, in workgroups of 256."""
+    assert -(-H * N * (D // 16) // 256) * 256 >= 1 << 32
+    s = (H * N * D, N * D, D)
+    assert _call(B=1, D=D, H=H, N=N, xs=s, y=ctypes.c_void_p(0x100000), ys=s) == stc.STC_ERR_SHAPE
+
+
 # B, H, N, D = 2, 3, 5, 128
 @pytest.mark.parametrize("ys", [(1920, 128, 128), (1920, 128, 256), (640, 128, 384), (1920, 640, 120),
                                 (1912, 640, 128), (1920, 632, 128), (1 << 62, 128, 1 << 61)])
