@@ -331,6 +331,7 @@ int stc_append_tail(const stc_shape_t *shape, const void *k_new, const void *v_n
  * read as `turns`.
  *   rot_dim  16, 32, .. 128
  *   turns    [rot_dim/2] double, out, in HOST memory: the caller copies it to the device once
+ * STC_ERR_SHAPE, and nothing written, also where a frequency, times 2^31, would not be a finite number.
  */
 int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t *scaling, double *turns);
 

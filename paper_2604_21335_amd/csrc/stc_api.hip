@@ -509,7 +509,13 @@ int stc_rotary_turns(int32_t rot_dim, const stc_rotary_scaling_t* scaling, doubl
   if (s.kind >= STC_ROTARY_SCALE_CHANNELS &&
       (s.original_len < 1 || !(s.slow > 0) || !(s.fast > s.slow) || !isfinite(s.fast)))
     return STC_ERR_SHAPE;
-  stc::rotary_turns(rot_dim, s, turns);
+  double all[64];
+  stc::rotary_turns(rot_dim, s, all);
+  // base and factor are finite, but their powers and quotients need not be, nor what the farthest position
+  // makes of them
+  for (int j = 0; j < rot_dim / 2; ++j)
+    if (!isfinite(all[j] * 0x1p31)) return STC_ERR_SHAPE;
+  std::copy(all, all + rot_dim / 2, turns);
   return STC_OK;
 }
 
