@@ -362,6 +362,7 @@ class RoutedCache:
         self.device = torch.device(device)
         self.B, self.Hq, self.Hkv, self.D, self.N, self.G = B, Hq, Hkv, D, N, G
         self.n_cap = n_cap
+        self.next_pos = N                   # position of the token behind the cache's last
         self.keep_scores = keep_scores
         self.k_pages = k_pages
         cap = (n_cap or N) * G if v_cap_groups is None else v_cap_groups
@@ -428,7 +429,7 @@ class RoutedCache:
         inputs are [B, 1, ...], one set per batch element for all its KV heads.  rotary: K comes
         without positions, [B, Hkv, N, D] with any strides (a projection's output, transposed), and
         gets them (pos, pos0 as in stc_rotary) on its way into the cache, which needs its own copy
-        (n_cap)."""
+        (n_cap).  pos0 says where the first token stands also for keys that have their positions."""
         if rotary is not None:
             if not self.n_cap:
                 raise ValueError("keys that get positions need a cache with a copy of its own (n_cap)")
@@ -437,6 +438,7 @@ class RoutedCache:
             self.K[:, :, :self.N].copy_(K)
         else:
             self.K = K
+        self.next_pos = pos0 + self.N if pos is None else None      # (given ones lie on the device)
         stc_build_page_bounds(self.shape, self.K, self.bounds)
         mode = STC_ROUTE_MASK if mask_in is not None else STC_ROUTE_TOPK
         if global_k is not None:
@@ -472,6 +474,8 @@ class RoutedCache:
                        self.tok_off, self.vpacked, self.dev_status)
         self.n_tail -= n
         self.N += n
+        if self.next_pos is not None:
+            self.next_pos += n
         self.shape.N = self.N
         self._resize()
 
@@ -515,11 +519,14 @@ class SharedPrefix:
     whole when the object is made: its own tail is empty (flush moves it into the cache), and it
     does not grow while sequences continue it."""
 
-    def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32):
-        """rotary: positions for the queries and keys given to append()."""
+    def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32, pos0=None):
+        """rotary: positions for the queries and keys given to append().  pos0: position of a tail's first
+        token; None: the one behind the prefix's last, which the prefix knows unless it was built from
+        given positions."""
         if prefix.B != 1:
             raise ValueError("the prefix is a cache of one batch element")
         self.prefix, self.B, self.tail_cap, self.rotary = prefix, B, tail_cap, rotary
+        self.pos0 = pos0
         self.N = prefix.N
         self._whole()
         p, dev = prefix, prefix.device
@@ -538,15 +545,22 @@ class SharedPrefix:
         if self.prefix.n_tail or self.prefix.N != self.N:
             raise ValueError("the prefix has a tail of its own or has grown")
 
-    def append(self, q, k_new, v_new):
+    def append(self, q, k_new, v_new, pos=None):
         """The new token of every sequence: q [B, Hq, D], k_new, v_new [B, Hkv, D] (without positions
-        where rotary is given).  Key and value go to the tails; returns the queries for attend()."""
+        where rotary is given).  Key and value go to the tails; returns the queries for attend().
+        pos [B] int32: the tokens' positions; None: pos0 + n_tail."""
         self._whole()
         r = self.rotary
+        pos0 = self.prefix.next_pos if self.pos0 is None else self.pos0
+        if pos0 is None:
+            if r and pos is None:
+                raise ValueError("the prefix was built from given positions: pos0 or pos has to say where "
+                                 "its sequences go on")
+            pos0 = 0
         stc_rotary_append(self.shape, q, k_new, v_new, self.q, self.K_tail, self.V_tail, self.n_tail,
                           self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
                           r.layout if r else STC_ROTARY_HALVES, amplitude=r.amplitude if r else 1.0,
-                          pos0=self.N, n_out=self.n_tail, dev_status=self.dev_status)
+                          pos=pos, pos0=pos0, n_out=self.n_tail, dev_status=self.dev_status)
         return self.q
 
     def attend(self, q, page_idx=None):
@@ -559,5 +573,5 @@ class SharedPrefix:
                                     self._ws)
         return self.out
 
-    def step(self, q, k_new, v_new, page_idx=None):
-        return self.attend(self.append(q, k_new, v_new), page_idx)
+    def step(self, q, k_new, v_new, page_idx=None, pos=None):
+        return self.attend(self.append(q, k_new, v_new, pos), page_idx)

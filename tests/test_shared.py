@@ -74,3 +74,12 @@ def test_a_prefix_is_whole():
             b.append(None, None, None)
         with pytest.raises(ValueError):
             b.attend(None)
+
+
+def test_positions_behind_given_ones_have_to_be_said():
+    cache = stc.RoutedCache.__new__(stc.RoutedCache)
+    cache.B, cache.N, cache.n_tail, cache.next_pos = 1, 64, 0, None
+    b = stc.SharedPrefix.__new__(stc.SharedPrefix)
+    b.prefix, b.N, b.pos0, b.rotary = cache, 64, None, stc.Rotary.__new__(stc.Rotary)
+    with pytest.raises(ValueError, match="pos0"):
+        b.append(None, None, None)

@@ -335,6 +335,44 @@ def test_a_run_of_steps(B, dtype):
     assert (out[-1] == 0).all()                                 # padding: as allocated
 
 
+def test_tails_go_on_where_the_prefix_ends():
+    """Positions behind a prefix that starts somewhere else, has grown, or whose positions were given."""
+    N, B, Hq, Hkv, D, cap = 200, 3, 8, 2, 128, 6
+    rot = stc.Rotary(128, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    K = torch.randn(1, Hkv, N, D, device=DEV, generator=g).bfloat16()
+    m = torch.full((1, Hkv, N), 0xFF, dtype=torch.int16, device=DEV)
+    x = torch.randn(B, Hq + 2 * Hkv, D, device=DEV, generator=g).bfloat16()
+    parts = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    c = stc.RoutedCache(1, Hq, Hkv, D, N, 8, 16, device=DEV, n_cap=224, tail_cap=8)
+
+    def first(pos, given=None, **kw):
+        """Queries and tails' first keys, which have to stand at positions pos."""
+        b = stc.SharedPrefix(c, B, cap, rotary=rot, **kw)
+        b.append(*parts, pos=given)
+        want = torch.empty(B, Hq + Hkv, 1, D, dtype=torch.bfloat16, device=DEV)
+        rot.apply(x[:, :Hq + Hkv, None], want, pos=torch.tensor(pos, dtype=torch.int32, device=DEV)[:, None])
+        assert torch.equal(b.q, want[:, :Hq, 0]) and torch.equal(b.K_tail[:, :, 0], want[:, Hq:, 0])
+    c.build(K, K, mask_in=m, rotary=rot)
+    first([N] * B)
+    c.build(K, K, mask_in=m, rotary=rot, pos0=1000)
+    first([1000 + N] * B)
+    first([7] * B, pos0=7)
+    first([3, 900, -2], given=torch.tensor([3, 900, -2], dtype=torch.int32, device=DEV))
+    c.append(K[:, :, 0].contiguous(), K[:, :, 0].contiguous())
+    c.flush(1, mask_in=m[:, :, :1].contiguous())
+    first([1000 + N + 1] * B)
+    c = stc.RoutedCache(1, Hq, Hkv, D, N, 8, 16, device=DEV, n_cap=224)
+    c.build(K, K, mask_in=m, rotary=rot, pos=torch.arange(N, dtype=torch.int32, device=DEV)[None] * 2)
+    with pytest.raises(ValueError):
+        first([N] * B)
+    first([2 * N] * B, pos0=2 * N)
+    first([3, 900, -2], given=torch.tensor([3, 900, -2], dtype=torch.int32, device=DEV))
+    stc.SharedPrefix(c, B, cap).append(*parts)                 # keys that have their positions
+    c.build(K, K, mask_in=m, pos0=50)
+    first([50 + N] * B)
+
+
 def test_steps_captured_and_replayed():
     """One graph of a step, replayed as the tails grow, with eager work between the replays."""
     B, cap = 5, 40
