@@ -371,7 +371,8 @@ int stc_rotary(int32_t B, int32_t H, int32_t N, int32_t D, int32_t rot_dim, int3
  *   q_out     [B, Hq, D] bf16, out; may be q where q_stride is Hq*D
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16: row n_tail[b] of sequence b's streams is written
  *   n_tail    [B] int32, in.  n_tail[b] < 0: b is padding, nothing of it is read or written.
- *             n_tail[b] >= tail_cap: no room; nothing of b is written, *dev_status becomes 1
+ *             n_tail[b] >= tail_cap: no room; nothing of b is written (a call that attends q_out then
+ *             answers what was there before), *dev_status becomes 1
  *   n_out     [B] int32, out, may be NULL or n_tail itself: n_tail[b] + 1 where a token was appended,
  *             else n_tail[b]
  *   rot_dim   0 (no rotation; turns may be NULL), 16, 32, .. D;  layout without STC_ROTARY_INVERSE

@@ -517,7 +517,10 @@ class SharedPrefix:
     and nothing else; the lengths of the tails lie on the device (n_tail; a negative one marks an
     element of the batch as padding), so that a step can be captured and replayed.  The prefix is
     whole when the object is made: its own tail is empty (flush moves it into the cache), and it
-    does not grow while sequences continue it."""
+    does not grow while sequences continue it.  A sequence whose tail is full takes no more tokens:
+    append() leaves its tail, length and query as they are and sets dev_status to 1, and attend() then
+    answers the query of the step before once more.  The lengths are not known to the host, so nothing
+    is raised: who does not stop a sequence in time looks at dev_status, which stays 1 until cleared."""
 
     def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32, pos0=None):
         """rotary: positions for the queries and keys given to append().  pos0: position of a tail's first

@@ -373,6 +373,27 @@ def test_tails_go_on_where_the_prefix_ends():
     first([50 + N] * B)
 
 
+def test_a_full_tail_repeats_its_last_answer_and_says_so():
+    c, *_ = _prefix()
+    b = stc.SharedPrefix(c, 3, 2, rotary=stc.Rotary(128, device=DEV))
+    b.n_tail.copy_(torch.tensor([0, 1, -1], dtype=torch.int32))
+    b.K_tail.zero_(), b.V_tail.zero_()
+    g = torch.Generator(device=DEV).manual_seed(8)
+    before = None
+    for full in (0, 1, 1):
+        x = torch.randn(3, 12, 128, device=DEV, generator=g).bfloat16()
+        out = b.step(x[:, :8], x[:, 8:10], x[:, 10:]).clone()
+        assert b.dev_status.item() == full
+        if full:
+            assert torch.equal(out[1], before[1]) and torch.equal(b.K_tail[1], keys[1])
+        before, keys = out, b.K_tail.clone()
+    assert b.n_tail.tolist() == [2, 2, -1]
+    b.dev_status.zero_()
+    b.n_tail[:2] = 0
+    out = b.step(x[:, :8], x[:, 8:10], x[:, 10:])
+    assert b.dev_status.item() == 0 and not torch.equal(out[1], before[1])
+
+
 def test_steps_captured_and_replayed():
     """One graph of a step, replayed as the tails grow, with eager work between the replays."""
     B, cap = 5, 40
