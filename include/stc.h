@@ -407,7 +407,10 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *   ws       stc_shared_workspace_bytes(shape, k_pages, tail_cap) bytes; calls whose work overlaps in
  *            time need one each
  * Logits (q . k / sqrt(D)) count up to a magnitude of 2^29; a sequence's larger ones, infinities and NaN
- * give meaningless results in its own rows of out.
+ * give meaningless results in its own rows of out.  Values count up to a magnitude of 2^119 over the number
+ * of tokens attended (a weight may stand at 2^8 before it is divided by the sum); larger ones, infinities and
+ * NaN give meaningless results, NaN where an infinity would be right among them, in their channel of the
+ * queries that attend them, and nowhere else.
  * The softmax's weights are carried as bf16 parts, two for the prefix (2^-16) and three for the tails (2^-24);
  * sums are float; the output's type says how the result is rounded and nothing else.  The results depend on
  * the sizes, not on other sequences' lengths.

@@ -503,6 +503,33 @@ def test_what_is_not_finite_stays_in_its_row(B, R, Hkv, cap):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,R,Hkv,cap", [(6, 4, 2, 40), (30, 2, 1, 0), (40, 5, 1, 40), (300, 1, 4, 90)])
+def test_large_values_and_what_is_not_finite_in_them(B, R, Hkv, cap, dtype):
+    """Values scaled by a power of two, up to the end of what counts, scale the output exactly: |v| < 8, at
+    most 390 tokens, weights of up to 2^8, and 2^3 2^107 <= 2^119 / 390.  NaN and infinities stay in their
+    channel, those of the prefix in all queries of the KV head, those of a tail in its sequence's."""
+    c = Case(B, R * Hkv, Hkv, 128, 300, 8, cap, keep=0xFF, n_tail=[3, cap, 7, 0])
+    ramp(c, "K", 32, 7.5, 300)
+    want = c.run(dtype)
+    far = 2.0 ** 107
+    assert np.abs(bits_to_f64(c.V)).max() < 8 and (not cap or np.abs(bits_to_f64(c.Vt)).max() < 8)
+    big = lambda t: None if t is None else t * far  # noqa: E731
+    assert torch.equal(c.run(dtype, v=big(c.d["v"]), Vt=big(c.d["Vt"])), want * far)
+    h = Hkv - 1
+    v = c.d["v"].clone()                                       # [Hkv, token * 8 + group, 16 channels]
+    v[h, 5 * 8 + 2, 3], v[h, 290 * 8, 0], v[h, 100 * 8 + 7, 15] = float("inf"), float("nan"), float("-inf")
+    Vt = None if not cap else c.d["Vt"].clone()
+    on = torch.ones(B, R * Hkv, 128, dtype=torch.bool, device=DEV)
+    for channel in (2 * 16 + 3, 0, 7 * 16 + 15):
+        on[:, h * R:, channel] = False
+    if cap:
+        Vt[0, 0, 2, 77], Vt[1, 0, cap - 1, 20] = float("inf"), float("nan")
+        on[0, :R, 77] = on[1, :R, 20] = False
+    got = c.run(dtype, v=v, Vt=Vt)
+    assert torch.equal(got[on], want[on]) and got[on].isfinite().all() and not got[~on].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,cap", [(3, 0), (3, 40), (40, 40), (300, 360)])
 def test_logits_far_below_zero(B, cap, dtype):
     """Equal logits near the end of what counts: each of them is the largest."""
