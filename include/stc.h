@@ -396,7 +396,10 @@ int stc_rotary_append(const stc_shape_t *shape, const void *q, int64_t q_stride,
  *   K, vpacked, mask, tok_off  the cache of a shape with B = 1, in: [Hkv, Ncap, D], [Hkv,
  *            v_cap_groups, D/G], [Hkv, Ncap], [Hkv, Ncap+1].  Their sizes are not limited to 4 GiB
  *   page_idx [Hkv, k_pages] int32, in: pages that all sequences attend; 1 <= k_pages <= NP; entries
- *            outside [0, NP) are skipped; a page must not be listed twice.  NULL: pages 0 .. k_pages-1
+ *            outside [0, NP) are skipped; a page must not be listed twice.  NULL: pages 0 .. k_pages-1.
+ *            The list of one query (stc_select_pages on the prefix), or those of up to 16 queries
+ *            merged: stc_union_pages with a shape of B = 1 whose "query heads" of a KV head are the
+ *            queries; the -1 at its end are skipped
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16, in (may be NULL when tail_cap == 0)
  *   n_tail   [B] int32 on the device, in: rows 0 .. n_tail[b]-1 of sequence b's tails are attended
  *            (counted as tail_cap if larger); n_tail[b] < 0: b is padding, its rows of out are left as

@@ -450,6 +450,33 @@ def test_selected_pages_of_the_prefix():
     assert (out[:1] - c.out).abs().max() <= 4e-5
 
 
+def test_pages_that_any_of_some_queries_selected():
+    """The lists of several sequences' queries, merged by stc_union_pages as if they were heads of one
+    sequence, attended by all of them: the pages of the union and no others."""
+    n, k, Hkv = 6, 20, 2
+    c, *_ = _prefix(N=1500, k_pages=k)
+    q = torch.randn(n, 8, 128, device=DEV).bfloat16()
+    lists = []
+    for i in range(n):
+        c.select(q[i:i + 1].contiguous())
+        lists.append(c.page_idx[0].clone())
+    lists = torch.stack(lists, 1).reshape(1, Hkv * n, k).contiguous()
+    cap = min(c.NP, n * k)
+    pages = torch.empty(1, Hkv, cap, dtype=torch.int32, device=DEV)
+    heads = torch.empty(1, Hkv, cap, dtype=torch.int16, device=DEV)
+    stc.stc_union_pages(stc.make_shape(1, Hkv * n, Hkv, 128, 1500, 8, 1), lists, k, pages, heads)
+    b = stc.SharedPrefix(c, n, 4)
+    got = b.attend(q, pages[0]).clone()
+    for h in range(Hkv):
+        union = torch.unique(lists[0, h * n:(h + 1) * n])
+        assert k < len(union) < cap and pages[0, h, :len(union)].tolist() == union.tolist()
+        assert (pages[0, h, len(union):] == -1).all()
+        alone = torch.full((Hkv, cap), -1, dtype=torch.int32, device=DEV)
+        alone[h, :len(union)] = union.flip(0)                  # another order, the other KV head without pages
+        want = b.attend(q, alone)
+        assert (got[:, h * 4:h * 4 + 4] - want[:, h * 4:h * 4 + 4]).abs().max() <= 4e-5
+
+
 def test_tensors_of_another_shape_or_type_are_refused():
     c = Case(2, 4, 2, 64, 40, 4, 6)
     d = c.d
