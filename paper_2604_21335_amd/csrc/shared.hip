@@ -915,15 +915,18 @@ SharedPlan shared_plan(const stc_shape_t& s, int k_pages, int tail_cap) {
   const long long streams = (long long)s.B * s.Hkv;
   // Wavefronts that share a tile: as many as have rows.  In us, by 1, 2, 4 and 8 of them, 4 KV heads of
   // 32768 (131072) tokens: 28 rows 17.2, 18.6, 24, 28; 63 rows 20.5, 20.6, 24, 30 and from a list of 2512
-  // pages 30.1 by 1, 27.0 by 2; 112 rows 27.7, 25.6, 26.8, 33 (by 2, 4: 77.9, 68.5); 1792 rows in bf16
-  // 230, 208, 172, 136.  Beyond 128 rows the ring of 8 pays where a compute unit has a long share of the
-  // prefix (315 rows, 1024 tokens: 45.7 by 4, 48.1 by 8; 875 rows, 2048 tokens: 107 and 100), or where it
-  // makes room for the tails (192 rows over 4001 tokens, tails of up to 1000: 159 and 154 for 4 layers; tails
-  // of up to 200 instead, 312 a unit: 20.7 and 24.6).
+  // pages 30.1 by 1, 27.0 by 2; 112 rows 27.7, 25.6, 26.8, 33 (by 2, 4: 77.9, 68.5); 1792 rows 272, 236, 197,
+  // 176.  Beyond 128 rows the ring of 8 takes 0.9 of the time of two blocks of 4 where a compute unit has a long
+  // share of the prefix.  By 4 and 8: 511 rows over 16384, 32768, 65536 tokens 38.5, 41.0; 63.2, 63.1 (1024
+  // tokens a unit); 117, 108.  So it needs a second block of 4 nearly always: 875 rows (7 blocks, or 4 of 8) over
+  // 32768 tokens 103, 103, 315 rows (3, or 2) over 131072 169, 185.  Or it makes room for the tails: 192 rows over
+  // 4001 tokens, tails of up to 1000, 145 and 139 for 4 layers; tails of up to 200 instead, 312 a unit, 23.0 and
+  // 26.0.
   p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  const long long blocks8 = (rows + 255) / 256;
-  if (rows > 128 && (blocks8 * s.Hkv * k_pages * kPage > 1792 * kUnits || streams * tail_cap > 400 * kUnits))
-    p.wr = 8;
+  const long long blocks4 = (rows + 127) / 128, blocks8 = (rows + 255) / 256;
+  const bool full = 0.9 * 2 * blocks8 < blocks4;
+  const bool long_share = blocks8 * s.Hkv * k_pages * kPage > 1024 * kUnits;
+  if (rows > 128 && ((full && long_share) || streams * tail_cap > 400 * kUnits)) p.wr = 8;
   p.row_blocks = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
   const int per = form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
   const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
@@ -1029,10 +1032,11 @@ int launch_shared(const stc_shape_t& s, const void* q, const void* K, const void
   P.tail_blocks = p.tail_blocks;
   const int blocks = (int)items + p.tail_blocks;
   // A prefix that one block of rows reads once goes past the caches from 40 MiB of keys and kept values
-  // (half of them, say) on.  In us with / without, D = 128, 28 rows, 10 prefixes in turn: 4 x 16384 tokens,
-  // 24 MiB, 15.1 / 15.2; 32768 tokens 18.9 / 20.4; 65536 tokens 26.2 / 29.3; 63 rows, 131072 tokens 53 /
-  // 56.  One prefix alone, out of the last-level cache: 131072 tokens 41.6 / 38.4.  (4 wavefronts to a
-  // tile gain 1 .. 3 %, and lose as much.)
+  // (half of them, say) on.  In us with / without, 28 rows, 10 prefixes in turn, 4 KV heads: D = 128, 16384
+  // tokens, 24 MiB, 15.1 / 15.2; 32768 tokens 18.8 / 20.5; 65536 tokens 25.9 / 29.4; D = 64, 24 MiB 11.9 / 12.1;
+  // 48 MiB 15.2 / 16.4; 96 MiB 22.8 / 24.9, with 63 rows 31.2 / 32.7.  One prefix alone, over and over out of the
+  // last-level cache: D = 128, 65536 tokens 25.4 / 24.8; 131072 tokens 43.4 / 38.9; D = 64, 96 MiB 21.9 / 21.7.
+  // (4 wavefronts to a tile gain 1 .. 3 %, and lose as much.)
   const bool stream = p.row_blocks == 1 && 3ll * s.Hkv * k_pages * kPage * s.D > (40ll << 20);
   const int rc = s.D == 128 ? shared_list<128>(P, p.wr, stream, blocks, st)
                             : shared_list<64>(P, p.wr, stream, blocks, st);

@@ -622,7 +622,7 @@ def check_some(c, some, dtype, pages=None):
 TURNS = [((2, 16, 8, 20003, 0), 256), ((30, 1, 16, 12003, 9), 256),       # a wavefront to a tile
          ((4, 16, 8, 20003, 0), 128), ((8, 8, 8, 16003, 40), 128),        # 2
          ((64, 16, 1, 9003, 33), 64), ((150, 7, 2, 20011, 0), 64),        # 4
-         ((48, 8, 8, 4001, 1000), 64), ((300, 1, 16, 15011, 0), 64)]      # 8: beside tails, a long prefix
+         ((48, 8, 8, 4001, 1000), 64), ((512, 1, 16, 8403, 0), 64)]      # 8: beside tails, a long prefix
 
 
 def turns_of(c, turn, k):
