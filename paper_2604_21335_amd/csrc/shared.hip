@@ -8,15 +8,17 @@
 // Every sequence's own tail goes the same way in workgroups of its own; a second launch merges the
 // partial results of a row.
 //
-// What bounds it (D = 128, half of the value groups kept):
-//   few rows, long prefix: 16 x 28 rows over 32768 tokens 26 us, the bytes of the cache 10.  Of the first
-//     launch's 21, 6 go by before the first product (kernel, masks and offsets, values: a chain of loads),
-//     13 in the loop at half of the matrix units' rate, 2 into writing partial results; the merge takes 5.
-//   many rows: 256 x 28 over 32768 tokens, 181 us; 90 GFLOP of kept values, 180 with the dropped ones, which are
-//     multiplied as zeros, and the second parts of the weights: 1000 TFLOP/s, a library's largest product 1220 ..
-//     1360 on the card.
-//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 .. 32 us, 138 MB at
-//     4.3 .. 4.8 TB/s with the merge's launch, where a copy reaches 5.1.
+// What bounds it (D = 128, half of the value groups kept; counters as shares of the time of the compute units
+// that work; cards differ by 13 %):
+//   few rows, long prefix: 16 x 28 rows over 32768 tokens 26 .. 29.5 us, the bytes of the cache 7.5.  On the slow card
+//     the first launch takes 24.3, the merge 4.8.  A chain of loads (masks and offsets, then values) goes by before
+//     the first product; then matrix units are busy 30 %, vector instructions issue 43 %, shared memory works 21 %.
+//   many rows: 256 x 28 over 32768 tokens, 177 .. 188 us; 90 GFLOP of kept values, 180 with the dropped ones, which
+//     are multiplied as zeros, and the second parts of the weights: 1000 TFLOP/s, a library's largest product 1190 ..
+//     1390.  Matrix units are busy 56 %, vector instructions issue 52 %: the exponentials and the weights' parts
+//     share the wavefronts' issue with the products.  Shared memory works 25 %, without bank conflicts.
+//   long tails: the memory; 64 x 32 heads of 144 + 64 tokens and tails of 0 .. 256 take 29 .. 33 us, 150 MB read in
+//     28.5 us, 5.3 TB/s where a plain read reaches 7.1, and the merge.
 #include "stc_common.hpp"
 #include "stc_kernels.hpp"
 
@@ -86,8 +88,8 @@ __device__ __forceinline__ float over_groups(float x, Op op) {
 }
 
 // Two weights in PARTS bf16 parts, put(part, both as one word); l: their sum.  A part leaves 2^-8 of what it
-// rounds.  The prefix takes two (2^-16, and errors of many weights cancel: float outputs are off by some 10^-6):
-// three would cost 1 .. 18 % there, where the matrix units are what is short.  One would be 20 % faster with many
+// rounds.  The prefix takes two (2^-16, and errors of many weights cancel: float outputs are off by 1 .. 2 10^-6 of
+// their norm): three would cost 0 .. 22 % there, most where rows are many.  One would be 20 % faster with many
 // rows (256 x 28 over 32768 tokens, 181 us -> 145), but puts an error as large as the output's own rounding beside
 // it where the output is bf16: 0.0021 of the output's norm where the rounding alone is 0.0017.  The tails take
 // three (2^-24, a float's own), where the matrix units are not short and a row may have few tokens.

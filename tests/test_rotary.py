@@ -59,7 +59,8 @@ def test_turns_refuse(kw):
     assert e.value.status == stc.STC_ERR_SHAPE
 
 
-@pytest.mark.parametrize("kw", [dict(kind=1, factor=5e-324), dict(kind=2, factor=5e-324), dict(base=1.5, kind=2, factor=1e-302),
+@pytest.mark.parametrize("kw", [dict(kind=1, factor=5e-324), dict(kind=2, factor=5e-324),
+                                dict(base=1.5, kind=2, factor=1e-302),
                                 dict(kind=4, factor=1e-310, original_len=64, slow=1.0, fast=2.0)])
 def test_turns_refuse_frequencies_that_are_not_finite(kw):
     s = stc.stc_rotary_scaling_t(kw["kind"], kw.get("original_len", 0), kw.get("base", 1e4), kw["factor"],
