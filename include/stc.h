@@ -28,6 +28,11 @@
  *                        into tails of different lengths), stc_rotary_turns (frequencies)
  *   one prefix for all   stc_decode_attention_shared (a batch over one compressed prefix, with
  *                        tails of different lengths), stc_shared_workspace_bytes
+ *   drafted tokens       stc_rotary_append_tree (up to 64 tokens of every sequence, a tree, behind
+ *                        its tail), stc_decode_attention_tree (their attention, over one prefix or
+ *                        one for each sequence), stc_tree_workspace_bytes, stc_accept_tail (the
+ *                        accepted ones stay)
+ *   tails of a batch     stc_fork_tail (sequences that continue others' tails, or end)
  *   per-query-head form  stc_select_pages_per_head, stc_decode_attention_per_head,
  *                        stc_union_pages + stc_decode_attention_union (shared K/V reads)
  *   helpers              stc_workspace_bytes, stc_bounds_bytes, stc_status_string, stc_version
@@ -425,6 +430,103 @@ int stc_decode_attention_shared(const stc_shape_t *shape, const void *q, const v
                                 const int32_t *page_idx, int k_pages, const void *K_tail,
                                 const void *V_tail, const int32_t *n_tail, int tail_cap, int out_type,
                                 void *out, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Drafted tokens.  A sequence may have T tokens in flight (1 <= T <= 64), the nodes of a tree, behind its tail:
+ * node t of sequence b has row n_tail[b] + t of the sequence's tails.  What a node sees of the other nodes is a
+ * set of bits: bit u of tree[b][t] (or of tree[t], one tree for the batch) stands for node u, its own bit among
+ * them, so a token in a tree has the bits of its ancestors and its own.  NULL stands for a chain: node t sees nodes
+ * 0 .. t.  n_draft[b] says how many of the T nodes a sequence has (clamped to 0 .. T; NULL: T); bits of others do
+ * not count.  n_tail[b] < 0: b is padding.  Trees, counts and lengths lie on the device, so that a captured graph
+ * can be replayed with others.  A prompt's tokens may come this way too, 64 at a time, as chains that are accepted
+ * whole.
+ */
+
+/*
+ * Positions, keys and values of the nodes, in one launch (arithmetic of stc_rotary).  The tails' lengths stay.
+ *   shape     B, Hq, Hkv, D are used (the rest must be valid)
+ *   q, k_new, v_new  [B, T, Hq, D], [B, T, Hkv, D], [B, T, Hkv, D] bf16, in; a node's heads are contiguous, and
+ *             q_stride (k_stride, v_stride), HOST arrays, hold the strides of b and t in elements: multiples of 8,
+ *             >= 0 (slices of one fused projection's output)
+ *   q_out     [B, T, Hq, D] bf16, out: rows of nodes that a sequence has; may be q where q's strides are T*Hq*D and
+ *             Hq*D
+ *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16: rows n_tail[b] .. n_tail[b] + n_draft[b] - 1 of b are written.
+ *             Where they would pass tail_cap nothing of b is written, and *dev_status becomes 1
+ *   n_tail    [B] int32, in;  n_draft  [B] int32, in, may be NULL
+ *   tree      [B, T] (tree_per_batch 1) or [T] (0) uint64, in, may be NULL; used where pos is NULL
+ *   rot_dim   0 (no rotation; turns may be NULL), 16, 32, .. D;  layout without STC_ROTARY_INVERSE
+ *   pos       [B, T] int32, in: the nodes' positions, or NULL: pos0 + n_tail[b] + the number of nodes u < t that node
+ *             t sees.  pos0 + tail_cap - 1 must not pass 2^31 - 1
+ *   dev_status int32 on the device, out, may be NULL; the caller zeroes it
+ */
+int stc_rotary_append_tree(const stc_shape_t *shape, int T, const void *q, const int64_t *q_stride,
+                           const void *k_new, const int64_t *k_stride, const void *v_new,
+                           const int64_t *v_stride, void *q_out, void *K_tail, void *V_tail,
+                           const int32_t *n_tail, const int32_t *n_draft, int tail_cap, const uint64_t *tree,
+                           int tree_per_batch, int rot_dim, int layout, const double *turns, float amplitude,
+                           const int32_t *pos, int32_t pos0, int32_t *dev_status, void *stream);
+
+/*
+ * Decode attention of the nodes: every node's query heads attend the tokens of the listed pages of the prefix, rows
+ * 0 .. n_tail[b]-1 of the sequence's tails, and rows n_tail[b] + u for the nodes u that it sees (that it has, and
+ * that lie below tail_cap), under one softmax; everything else as stc_decode_attention_shared.  With T = 1 and no
+ * tree it is the step of one token whose row stands behind the tail.
+ *   shape    B sequences; Hq, Hkv, D of the model; N, G, N_cap, v_cap_groups of a prefix
+ *   n_prefix 1: all sequences continue one prefix, arrays of a cache with B = 1; B: every sequence its own
+ *   q        [B, T, Hq, D] bf16, in
+ *   K, vpacked, mask, tok_off  [n_prefix, Hkv, ...], in: caches as stc_route_and_pack_values leaves them; their
+ *            sizes are not limited to 4 GiB
+ *   page_idx [n_prefix, Hkv, k_pages] int32, in, or NULL, as for stc_decode_attention_shared
+ *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16, in;  tail_cap >= 1
+ *   n_tail   [B] int32, in (counted as tail_cap if larger);  n_draft  [B] int32, in, may be NULL
+ *   tree     [B, T] (tree_per_batch 1) or [T] (0) uint64, in, may be NULL
+ *   out      [B, T, Hq, D], out, float or bf16; rows of padding and of nodes that a sequence does not have are left
+ *            as they are; a query without any token gets zeros
+ *   ws       stc_tree_workspace_bytes(...) bytes; calls whose work overlaps in time need one each
+ * Magnitudes count as for stc_decode_attention_shared.  Keys and values of a node that are infinite or NaN reach the
+ * queries that see it and no others.  The results depend on the sizes, not on other sequences' lengths or trees.
+ */
+size_t stc_tree_workspace_bytes(const stc_shape_t *shape, int T, int n_prefix, int k_pages, int tail_cap);
+int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, const void *q, const void *K,
+                              const void *vpacked, const uint16_t *mask, const uint32_t *tok_off,
+                              const int32_t *page_idx, int k_pages, const void *K_tail, const void *V_tail,
+                              const int32_t *n_tail, const int32_t *n_draft, int tail_cap, const uint64_t *tree,
+                              int tree_per_batch, int out_type, void *out, void *ws, size_t ws_bytes,
+                              void *stream);
+
+/*
+ * Accepted nodes stay: of the T rows behind the tail those whose bits are set in keep[b] move together, in order,
+ * in place, and the tail grows by their number, in all layers at once.  (An accepted path is the set of its last
+ * node: tree[b][last].)  Bits at and above T, and of rows at and above tail_cap, do not count.  The other rows are
+ * left as they are, and as what they are: behind the tail.
+ *   shape     B, Hkv, D are used (the rest must be valid)
+ *   n_layers  1 .. 1024; the arrays below are HOST arrays of n_layers device pointers
+ *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16 each, in/out; no two may overlap
+ *   n_tail    [B] int32 each, in (negative: padding, left alone); layers may share one where n_out is another
+ *   n_out     [B] int32 each, out: the new lengths; n_out[i] may be n_tail[i] itself, but must not overlap another
+ *             layer's n_tail or n_out
+ *   keep      [B] uint64, in, the same for all layers
+ */
+int stc_accept_tail(const stc_shape_t *shape, int T, int n_layers, void *const *K_tail, void *const *V_tail,
+                    const int32_t *const *n_tail, int32_t *const *n_out, int tail_cap, const uint64_t *keep,
+                    void *stream);
+
+/*
+ * Sequences that go on with others' tails (beams, samples of one answer, another try from an earlier token), in place
+ * and in all layers at once.  src is any map: sequences may change places or all follow one.
+ *   shape, n_layers, K_tail, V_tail, n_tail, n_out  as for stc_accept_tail; B <= 4096
+ *   src       [B] int32, in: sequence b continues with the rows and the length that src[b] had before the call.
+ *             src[b] = b: it stays; STC_TAIL_FREED: it becomes padding (length -1); STC_TAIL_EMPTY: it starts anew
+ *             (length 0).  Other values: it stays, and *dev_status becomes 1
+ *   n_keep    [B] int32, in, may be NULL: b continues with the first n_keep[b] of those rows at most (negative: none).
+ *             src and n_keep must not overlap an n_out
+ *   dev_status int32 on the device, out, may be NULL; the caller zeroes it
+ * A sequence that follows padding becomes padding.  Rows at and behind a sequence's new length are left as they are.
+ */
+enum { STC_TAIL_FREED = -1, STC_TAIL_EMPTY = -2 };
+int stc_fork_tail(const stc_shape_t *shape, int n_layers, void *const *K_tail, void *const *V_tail,
+                  const int32_t *const *n_tail, int32_t *const *n_out, int tail_cap, const int32_t *src,
+                  const int32_t *n_keep, int32_t *dev_status, void *stream);
 
 /*
  * Per-query-head page selection and attention: the other reading of Quest under grouped-query

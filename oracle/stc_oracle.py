@@ -513,3 +513,89 @@ def shared_attention_all(q_bits, K_bits, V_bits, mask, page_idx, G, K_tail, V_ta
                 w /= w.sum()
                 out[b, j], size[b, j] = w @ Vb, w @ np.abs(Vb)
     return out, size, top
+
+
+def sees(tree, T, n_draft):
+    """What the T nodes of one sequence see of each other, [T, T] bool: bit u of tree[t], or a chain; of
+    the n_draft nodes that are there (None: T)."""
+    nodes = T if n_draft is None else min(max(int(n_draft), 0), T)
+    out = np.zeros((T, T), dtype=bool)
+    for t in range(T):
+        for u in range(nodes):
+            out[t, u] = u <= t if tree is None else int(tree[t]) >> u & 1
+    return out, nodes
+
+
+def tree_attention_all(q_bits, K_bits, V_bits, mask, page_idx, G, K_tail, V_tail, n_tail, tree=None,
+                       n_draft=None, P=16):
+    """Nodes of trees over compressed prefixes.  q_bits[B, T, Hq, D]; K_bits, V_bits [n, Hkv, N, D]
+    (dense values), mask[n, Hkv, N] of n = 1 prefix for all or n = B; page_idx[n, Hkv, k] (entries outside
+    the prefix are skipped) or None: every page; K_tail, V_tail [B, Hkv, cap, D]: sequence b's tail of
+    n_tail[b] tokens (at most cap), then its nodes; tree[B, T] bits or None.  -> (out, size [B, T, Hq, D],
+    top, on[B, T]) as shared_attention_all; on: the nodes that are there."""
+    B, T, Hq, D = q_bits.shape
+    n_prefix, Hkv, N, _ = K_bits.shape
+    R, cap = Hq // Hkv, K_tail.shape[2]
+    out, size, top = np.zeros(q_bits.shape), np.zeros(q_bits.shape), 0.0
+    on = np.zeros((B, T), dtype=bool)
+    for b in range(B):
+        if n_tail[b] < 0:
+            continue
+        p = b if n_prefix > 1 else 0
+        see, nodes = sees(None if tree is None else tree[b], T, None if n_draft is None else n_draft[b])
+        n0 = min(int(n_tail[b]), cap)
+        n = min(n0 + nodes, cap)
+        on[b, :nodes] = True
+        visible = np.ones((T, n), dtype=bool)
+        visible[:, n0:] = see[:, :n - n0]
+        for h in range(Hkv):
+            listed = np.zeros(N, dtype=bool)
+            for page in range((N + P - 1) // P) if page_idx is None else page_idx[p, h]:
+                if 0 <= page < (N + P - 1) // P:
+                    listed[page * P:(page + 1) * P] = True
+            keep = (np.asarray(mask[p, h][listed]).astype(np.int64)[:, None] >> np.arange(G)) & 1
+            K = bf16_to_f32(np.concatenate([K_bits[p, h][listed], K_tail[b, h, :n]])).astype(np.float64)
+            V = np.concatenate([
+                bf16_to_f32(V_bits[p, h][listed]).astype(np.float64) * np.repeat(keep, D // G, axis=1),
+                bf16_to_f32(V_tail[b, h, :n]).astype(np.float64)])
+            for t in range(nodes):
+                at = np.concatenate([np.ones(int(listed.sum()), dtype=bool), visible[t]])
+                if not at.any():
+                    continue
+                q = bf16_to_f32(q_bits[b, t, h * R:(h + 1) * R]).astype(np.float64)
+                s = q @ K[at].T / math.sqrt(D)
+                top = max(top, float((np.abs(q) @ np.abs(K[at]).T).max() / math.sqrt(D)))
+                w = np.exp(s - s.max(axis=1, keepdims=True))
+                w /= w.sum(axis=1, keepdims=True)
+                out[b, t, h * R:(h + 1) * R] = w @ V[at]
+                size[b, t, h * R:(h + 1) * R] = w @ np.abs(V[at])
+    return out, size, top, on
+
+
+def accept(rows, n_tail, T, keep):
+    """rows[H, cap, D] of one sequence -> (rows, new length): of the T rows behind n_tail those whose bit
+    keep has, in order, right behind it."""
+    n_tail = int(n_tail)
+    out, at = rows.copy(), n_tail
+    if n_tail < 0:
+        return out, n_tail
+    for u in range(T):
+        if int(keep) >> u & 1 and n_tail + u < rows.shape[1]:
+            out[:, at] = rows[:, n_tail + u]
+            at += 1
+    return out, at
+
+
+def fork(rows, n_tail, src, n_keep=None):
+    """rows[B, H, cap, D], n_tail[B], src[B] (-1: ends, -2: starts anew) -> (rows, lengths)."""
+    out, n = rows.copy(), np.array(n_tail)
+    for b, s in enumerate(src):
+        if s in (-1, -2):
+            n[b] = -1 if s == -1 else 0
+        elif 0 <= s < len(src):
+            n[b] = n_tail[s]
+            if n_keep is not None and n[b] >= 0:
+                n[b] = min(n[b], max(n_keep[b], 0))
+            m = max(min(n[b], rows.shape[2]), 0)
+            out[b, :, :m] = rows[s, :, :m]
+    return out, n

@@ -26,6 +26,7 @@ STC_OUT_F32, STC_OUT_BF16 = 0, 1
 STC_ROTARY_HALVES, STC_ROTARY_INTERLEAVED, STC_ROTARY_INVERSE = 0, 1, 0x100
 STC_ROTARY_SCALE_NONE, STC_ROTARY_SCALE_LINEAR, STC_ROTARY_SCALE_BASE = 0, 1, 2
 STC_ROTARY_SCALE_CHANNELS, STC_ROTARY_SCALE_WAVELENGTHS = 3, 4
+STC_TAIL_FREED, STC_TAIL_EMPTY = -1, -2     # in the map of stc_fork_tail
 
 EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bounds_bytes",
            "stc_build_page_bounds",
@@ -34,7 +35,9 @@ EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bound
            "stc_union_pages", "stc_decode_attention_union", "stc_flush_tail",
            "stc_compact_tokens", "stc_decode_step", "stc_decode_step_tail",
            "stc_decode_step_static", "stc_rotary_turns", "stc_rotary", "stc_rotary_append",
-           "stc_shared_workspace_bytes", "stc_decode_attention_shared"]
+           "stc_shared_workspace_bytes", "stc_decode_attention_shared",
+           "stc_rotary_append_tree", "stc_tree_workspace_bytes", "stc_decode_attention_tree",
+           "stc_accept_tail", "stc_fork_tail"]
 
 
 class StcError(RuntimeError):
@@ -140,6 +143,19 @@ def load_library():
     lib.stc_decode_attention_shared.restype = ctypes.c_int
     lib.stc_decode_attention_shared.argtypes = [shp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp, vp,
                                                 ctypes.c_int, ctypes.c_int, vp, vp, sz, vp]
+    ci, ptrs = ctypes.c_int, ctypes.POINTER(vp)
+    lib.stc_rotary_append_tree.restype = ci
+    lib.stc_rotary_append_tree.argtypes = [shp, ci, vp, strides, vp, strides, vp, strides, vp, vp, vp, vp,
+                                           vp, ci, vp, ci, ci, ci, vp, f32, vp, i32, vp, vp]
+    lib.stc_tree_workspace_bytes.restype = sz
+    lib.stc_tree_workspace_bytes.argtypes = [shp, ci, ci, ci, ci]
+    lib.stc_decode_attention_tree.restype = ci
+    lib.stc_decode_attention_tree.argtypes = [shp, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, ci,
+                                              vp, ci, ci, vp, vp, sz, vp]
+    lib.stc_accept_tail.restype = ci
+    lib.stc_accept_tail.argtypes = [shp, ci, ci, ptrs, ptrs, ptrs, ptrs, ci, vp, vp]
+    lib.stc_fork_tail.restype = ci
+    lib.stc_fork_tail.argtypes = [shp, ci, ptrs, ptrs, ptrs, ptrs, ci, vp, vp, vp, vp]
     lib.stc_compact_tokens.restype = ctypes.c_int
     lib.stc_compact_tokens.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     _lib = lib
@@ -336,6 +352,64 @@ def stc_decode_attention_shared(shape, q, K, vpacked, mask, tok_off, page_idx, k
                                                         ws)
 
 
+def stc_rotary_append_tree(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail, tail_cap, turns, rot_dim,
+                           layout, tree=None, n_draft=None, amplitude=1.0, pos=None, pos0=0,
+                           dev_status=None):
+    """T drafted tokens of every sequence, q [B, T, Hq, D], k_new, v_new [B, T, Hkv, D] (slices of one
+    projection's output will do): rotated q to q_out, rotated k_new and v_new to rows n_tail[b] .. of sequence
+    b's tails, whose lengths stay.  tree [T] or [B, T] int64: the nodes that a node sees, as bits; None: a chain.
+    n_draft [B] int32: nodes that a sequence has; None: T."""
+    (_native or _load_native()).rotary_append_tree(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail,
+                                                   tail_cap, turns, rot_dim, layout, tree, n_draft, amplitude,
+                                                   pos, pos0, dev_status)
+
+
+def stc_tree_workspace_bytes(shape, T, k_pages, tail_cap, n_prefix=1):
+    return int(load_library().stc_tree_workspace_bytes(ctypes.byref(shape), T, n_prefix, k_pages, tail_cap))
+
+
+def stc_decode_attention_tree(shape, q, K, vpacked, mask, tok_off, page_idx, k_pages, K_tail, V_tail, n_tail,
+                              tail_cap, out, ws, tree=None, n_draft=None, n_prefix=1):
+    """The nodes' queries q [B, T, Hq, D] over the listed pages of a prefix (n_prefix 1: the batch's; B: one for
+    each sequence), the sequence's tail and the nodes that they see; out [B, T, Hq, D] float32 or bfloat16."""
+    (_native or _load_native()).decode_attention_tree(shape, n_prefix, q.shape[1], q, K, vpacked, mask, tok_off,
+                                                      page_idx, k_pages, K_tail, V_tail, n_tail, tail_cap, tree,
+                                                      n_draft, out, ws)
+
+
+def stc_accept_tail(shape, T, K_tails, V_tails, n_tails, tail_cap, keep, n_outs=None):
+    """Of the T nodes behind sequence b's tail, those whose bits keep[b] (int64) has move together, and the tail
+    grows by them, in all layers: K_tails, V_tails, n_tails are lists of the layers' tensors.  n_outs: where the new
+    lengths go; None: n_tails."""
+    (_native or _load_native()).accept_tail(shape, T, tail_cap, K_tails, V_tails, n_tails,
+                                            n_tails if n_outs is None else n_outs, keep)
+
+
+def stc_fork_tail(shape, K_tails, V_tails, n_tails, tail_cap, src, n_keep=None, n_outs=None, dev_status=None):
+    """Sequence b goes on with the tail of src[b] (int32; STC_TAIL_FREED: ends, STC_TAIL_EMPTY: starts anew), its
+    first n_keep[b] tokens where given, in all layers: lists of tensors as for stc_accept_tail."""
+    (_native or _load_native()).fork_tail(shape, tail_cap, K_tails, V_tails, n_tails,
+                                          n_tails if n_outs is None else n_outs, src, n_keep, dev_status)
+
+
+def tree_from_parents(parents, device="cuda:0"):
+    """Bits of the nodes that each node of a tree of drafted tokens sees, its ancestors and itself: parents is a
+    list of T numbers (or B such lists), the place of a node's parent, smaller than its own, or -1 for nodes that
+    follow the sequence's last token.  -> int64 tensor [T] (or [B, T]), the `tree` of the calls below."""
+    many = len(parents) > 0 and hasattr(parents[0], "__len__")
+    out = []
+    for one in (parents if many else [parents]):
+        if not 1 <= len(one) <= 64:
+            raise ValueError("a tree has 1 to 64 nodes")
+        seen = []
+        for t, p in enumerate(one):
+            if not -1 <= p < t:
+                raise ValueError("a node's parent stands in front of it")
+            seen.append((seen[int(p)] if p >= 0 else 0) | 1 << t)
+        out.append([x - (1 << 64) if x >> 63 else x for x in seen])
+    return torch.tensor(out if many else out[0], dtype=torch.int64, device=device)
+
+
 class Rotary:
     """A model's rotary positions: the frequencies on the device and how they are applied."""
 
@@ -522,11 +596,13 @@ class SharedPrefix:
     answers the query of the step before once more.  The lengths are not known to the host, so nothing
     is raised: who does not stop a sequence in time looks at dev_status, which stays 1 until cleared."""
 
-    def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32, pos0=None):
+    n_prefix = 1        # prefixes of the batch
+
+    def __init__(self, prefix, B, tail_cap, rotary=None, out_dtype=torch.float32, pos0=None, nodes=()):
         """rotary: positions for the queries and keys given to append().  pos0: position of a tail's first
         token; None: the one behind the prefix's last, which the prefix knows unless it was built from
-        given positions."""
-        if prefix.B != 1:
+        given positions.  nodes: the numbers of nodes that drafts have (one, or several in a tuple)."""
+        if prefix.B != self.n_prefix:
             raise ValueError("the prefix is a cache of one batch element")
         self.prefix, self.B, self.tail_cap, self.rotary = prefix, B, tail_cap, rotary
         self.pos0 = pos0
@@ -540,26 +616,39 @@ class SharedPrefix:
         self.q = torch.zeros(B, p.Hq, p.D, dtype=torch.bfloat16, device=dev)
         self.out = torch.zeros(B, p.Hq, p.D, dtype=out_dtype, device=dev)
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.nodes = (nodes,) if isinstance(nodes, int) else tuple(nodes)
+        most = max(self.nodes, default=0)
+        self._q_tree = torch.zeros(B * most * p.Hq * p.D, dtype=torch.bfloat16, device=dev)
+        self._out_tree = torch.zeros(B * most * p.Hq * p.D, dtype=out_dtype, device=dev)
+        self._same = torch.arange(B, dtype=torch.int32, device=dev)
         # the workspace covers every choice of pages
-        need = max(stc_shared_workspace_bytes(self.shape, k, tail_cap) for k in range(1, p.NP + 1))
+        need = max(self._need(k) for k in range(1, p.NP + 1))
         self._ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+
+    def _need(self, k):
+        return max([stc_shared_workspace_bytes(self.shape, k, self.tail_cap)] +
+                   [stc_tree_workspace_bytes(self.shape, T, k, self.tail_cap) for T in self.nodes])
 
     def _whole(self):
         if self.prefix.n_tail or self.prefix.N != self.N:
             raise ValueError("the prefix has a tail of its own or has grown")
 
+    def _first(self, pos):
+        """Position of a tail's first token, for calls that are not given positions."""
+        self._whole()
+        pos0 = self.prefix.next_pos if self.pos0 is None else self.pos0
+        if pos0 is None:
+            if self.rotary and pos is None:
+                raise ValueError("the prefix was built from given positions: pos0 or pos has to say where "
+                                 "its sequences go on")
+            pos0 = 0
+        return pos0
+
     def append(self, q, k_new, v_new, pos=None):
         """The new token of every sequence: q [B, Hq, D], k_new, v_new [B, Hkv, D] (without positions
         where rotary is given).  Key and value go to the tails; returns the queries for attend().
         pos [B] int32: the tokens' positions; None: pos0 + n_tail."""
-        self._whole()
-        r = self.rotary
-        pos0 = self.prefix.next_pos if self.pos0 is None else self.pos0
-        if pos0 is None:
-            if r and pos is None:
-                raise ValueError("the prefix was built from given positions: pos0 or pos has to say where "
-                                 "its sequences go on")
-            pos0 = 0
+        pos0, r = self._first(pos), self.rotary
         stc_rotary_append(self.shape, q, k_new, v_new, self.q, self.K_tail, self.V_tail, self.n_tail,
                           self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
                           r.layout if r else STC_ROTARY_HALVES, amplitude=r.amplitude if r else 1.0,
@@ -578,3 +667,79 @@ class SharedPrefix:
 
     def step(self, q, k_new, v_new, page_idx=None, pos=None):
         return self.attend(self.append(q, k_new, v_new, pos), page_idx)
+
+    # Drafted tokens, the nodes of a tree behind each tail: draft, attend_tree (or step_tree for both), and
+    # accept for those that stay.  tree, n_draft as in stc_rotary_append_tree.
+    def _tree_rows(self, buf, T):
+        if T not in self.nodes:
+            raise ValueError("drafts have %s nodes, not %d" % (list(self.nodes), T))
+        return buf[:self.B * T * self.prefix.Hq * self.prefix.D].view(self.B, T, self.prefix.Hq, self.prefix.D)
+
+    def draft(self, q, k_new, v_new, tree=None, n_draft=None, pos=None):
+        """The nodes of every sequence: q [B, T, Hq, D], k_new, v_new [B, T, Hkv, D].  Keys and values go behind
+        the tails, whose lengths stay; returns the queries for attend_tree().  Where a sequence has no room for
+        its nodes, nothing of it is written and dev_status becomes 1."""
+        pos0, r, out = self._first(pos), self.rotary, self._tree_rows(self._q_tree, q.shape[1])
+        stc_rotary_append_tree(self.shape, q, k_new, v_new, out, self.K_tail, self.V_tail, self.n_tail,
+                               self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
+                               r.layout if r else STC_ROTARY_HALVES, tree=tree, n_draft=n_draft,
+                               amplitude=r.amplitude if r else 1.0, pos=pos, pos0=pos0,
+                               dev_status=self.dev_status)
+        return out
+
+    def attend_tree(self, q, tree=None, n_draft=None, page_idx=None):
+        """page_idx as in attend().  Returns [B, T, Hq, D]; rows of nodes that are not there are what they were."""
+        return self._attend_tree(q, self._tree_rows(self._out_tree, q.shape[1]), tree, n_draft, page_idx)
+
+    def _attend_tree(self, q, out, tree, n_draft, page_idx):
+        self._whole()
+        p = self.prefix
+        k = p.NP if page_idx is None else page_idx.shape[-1]
+        stc_decode_attention_tree(self.shape, q, p.K, p.vpacked, p.mask, p.tok_off, page_idx, k, self.K_tail,
+                                  self.V_tail, self.n_tail, self.tail_cap, out, self._ws, tree=tree,
+                                  n_draft=n_draft, n_prefix=self.n_prefix)
+        return out
+
+    def step_tree(self, q, k_new, v_new, tree=None, n_draft=None, page_idx=None, pos=None):
+        return self.attend_tree(self.draft(q, k_new, v_new, tree, n_draft, pos), tree, n_draft, page_idx)
+
+    def accept(self, keep, T, layers=()):
+        """keep [B] int64: bits of the nodes (of T) that stay, in order, behind the tails, which grow by them.
+        layers: the objects of the model's other layers, for the same in all of them."""
+        every = (self,) + tuple(layers)
+        stc_accept_tail(self.shape, T, [x.K_tail for x in every], [x.V_tail for x in every],
+                        [x.n_tail for x in every], self.tail_cap, keep)
+
+    def fork(self, src=None, n_keep=None, layers=()):
+        """src [B] int32: sequence b goes on with the tail of src[b] (STC_TAIL_FREED: it ends, STC_TAIL_EMPTY: it
+        starts anew; None: with its own), the first n_keep[b] tokens of it where given.  layers as in accept()."""
+        every = (self,) + tuple(layers)
+        stc_fork_tail(self.shape, [x.K_tail for x in every], [x.V_tail for x in every],
+                      [x.n_tail for x in every], self.tail_cap, self._same if src is None else src,
+                      n_keep=n_keep, dev_status=self.dev_status)
+
+
+class OwnPrefixes(SharedPrefix):
+    """As SharedPrefix, for B sequences that continue a prefix of their own each: `prefix` is a RoutedCache of B
+    elements, and page lists have a dimension for them, [B, Hkv, k] (RoutedCache.page_idx).  Sequences do not take
+    over others' tails, which belong to other prefixes: fork() only shortens them (n_keep)."""
+
+    def __init__(self, prefix, tail_cap, rotary=None, out_dtype=torch.float32, pos0=None, nodes=()):
+        self.n_prefix = prefix.B
+        self._blind = torch.zeros(1, dtype=torch.int64, device=prefix.device)
+        super().__init__(prefix, prefix.B, tail_cap, rotary, out_dtype, pos0, nodes)
+
+    def _need(self, k):
+        return max(stc_tree_workspace_bytes(self.shape, T, k, self.tail_cap, self.n_prefix)
+                   for T in (1,) + self.nodes)
+
+    def attend(self, q, page_idx=None):
+        # the token was appended: a query that stands behind the tail and sees nothing but it
+        one = (self.B, 1, self.prefix.Hq, self.prefix.D)
+        self._attend_tree(q.view(one), self.out.view(one), self._blind, None, page_idx)
+        return self.out
+
+    def fork(self, src=None, n_keep=None, layers=()):
+        if src is not None:
+            raise ValueError("sequences with prefixes of their own go on with their own tails")
+        super().fork(None, n_keep, layers)

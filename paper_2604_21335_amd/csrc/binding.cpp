@@ -116,6 +116,29 @@ class Args {
     return r;
   }
 
+  // The next argument stands for the number of layers' tensors: a list or tuple of them, of at least one.
+  struct Many {
+    static constexpr int kMost = 1024;
+    void* p[kMost];
+    int n;
+  };
+  template <class... T>
+  void many(Many& m, const char* name, int64_t numel, T... types) {
+    PyObject* o = next();
+    if (!PyList_Check(o) && !PyTuple_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "%s must be a list or tuple of tensors", name);
+      throw PythonError();
+    }
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    need(n >= 1 && n <= Many::kMost, name, "must have 1 to 1024 tensors");
+    m.n = (int)n;
+    PyObject* const* const args = args_;
+    const Py_ssize_t at = at_;
+    args_ = PySequence_Fast_ITEMS(o), at_ = 0;
+    for (Py_ssize_t i = 0; i < n; ++i) m.p[i] = sized(name, numel, types...);
+    args_ = args, at_ = at;
+  }
+
   float real() {
     const double v = PyFloat_AsDouble(next());
     if (v == -1.0 && PyErr_Occurred()) throw PythonError();
@@ -355,6 +378,88 @@ STC_PY(decode_attention_shared, 14,
   auto ws = a.ws(); auto nws = a.bytes(); auto st = a.stream();
   return [=] { return stc_decode_attention_shared(&s, q, K, v, mask, off, idx, k, Kt, Vt, n, cap, type, out, ws, nws, st); };)
 
+// Sets of visible nodes: [B, T], or [T] for all sequences.
+struct Tree {
+  const uint64_t* p;
+  int per_batch;
+};
+static Tree tree_of(Args& a, int32_t B, int64_t T) {
+  const auto p = (const uint64_t*)a.tensor("tree", at::kLong, at::kUInt64);
+  const int64_t n = a.bytes() / 8;
+  a.need(!p || n == T || n == (int64_t)B * T, "tree", "must be [T] or [B, T]");
+  return {p, p && n != T};
+}
+
+STC_PY(rotary_append_tree, 18,
+  auto s = *a.shape(); a.one_device();
+  auto q = a.rows("q", 4); auto k = a.rows("k_new", 4); auto v = a.rows("v_new", 4);
+  const int64_t T = q.size[1];
+  const auto heads = [&](const Args::Rows& r, const char* name, int32_t H) {
+    a.need(r.size[0] == s.B && r.size[1] == T && r.size[2] == H && r.size[3] == s.D, name, "has another shape");
+    a.need(H == 1 || r.stride[2] == s.D, name, "must have contiguous heads");
+  };
+  heads(q, "q", s.Hq); heads(k, "k_new", s.Hkv); heads(v, "v_new", s.Hkv);
+  const int64_t streams = (int64_t)s.B * s.Hkv * s.D;
+  auto qo = a.sized("q_out", (int64_t)s.B * T * s.Hq * s.D, kBf16);
+  auto Kt = a.bf16("K_tail"); auto nk = a.bytes(); auto Vt = a.bf16("V_tail"); auto nv = a.bytes();
+  auto n = (int32_t*)a.sized("n_tail", s.B, at::kInt); auto cap = a.integer();
+  a.need(nk == (size_t)streams * cap * 2 && nv == nk, "K_tail, V_tail", "must be [B, Hkv, tail_cap, D]");
+  auto turns = (double*)a.tensor("turns", kF64); auto nturns = a.bytes() / 8; auto rot = a.integer();
+  a.need(!turns || (int64_t)nturns * 2 == rot, "turns", "must have rot_dim/2 elements");
+  auto layout = a.integer(); auto tree = tree_of(a, s.B, T);
+  auto nd = (int32_t*)a.sized("n_draft", s.B, at::kInt); auto amp = a.real();
+  auto pos = (int32_t*)a.sized("pos", s.B * T, at::kInt); auto pos0 = a.integer();
+  auto status = (int32_t*)a.sized("dev_status", 1, at::kInt); auto st = a.stream();
+  // strides of dimensions of one element: as if rows followed each other
+  if (T == 1) q.stride[1] = (int64_t)s.Hq * s.D;
+  if (s.B == 1) q.stride[0] = T * s.Hq * s.D;
+  return [=] { return stc_rotary_append_tree(&s, (int)T, q.p, q.stride, k.p, k.stride, v.p, v.stride, qo, Kt, Vt, n, nd, cap, tree.p, tree.per_batch, rot, layout, turns, amp, pos, pos0, status, st); };)
+
+STC_PY(decode_attention_tree, 18,
+  auto s = *a.shape(); a.one_device(); auto P = a.integer(); auto T = a.integer();
+  const int64_t Nc = s.N_cap ? s.N_cap : s.N; const int64_t gd = s.G > 0 ? s.D / s.G : 0;
+  const int64_t n_q = (int64_t)s.B * T * s.Hq * s.D; const int64_t heads = (int64_t)P * s.Hkv;
+  a.need(T >= 1 && T <= 64, "q", "must have 1 to 64 nodes");
+  a.need(P == 1 || P == s.B, "n_prefix", "must be 1 or B");
+  auto q = a.sized("q", n_q, kBf16); auto K = a.sized("K", heads * Nc * s.D, kBf16);
+  auto v = a.sized("vpacked", heads * s.v_cap_groups * gd, kBf16);
+  auto mask = (uint16_t*)a.sized("mask", heads * Nc, at::kShort, at::kUInt16);
+  auto off = (uint32_t*)a.sized("tok_off", heads * (Nc + 1), at::kInt, at::kUInt32);
+  auto idx = a.i32("page_idx"); auto nidx = a.bytes() / 4; auto k = a.integer();
+  a.need(!idx || (int64_t)nidx == heads * k, "page_idx", "must be [n_prefix, Hkv, k_pages]");
+  auto Kt = a.bf16("K_tail"); auto nk = a.bytes(); auto Vt = a.bf16("V_tail"); auto nv = a.bytes();
+  auto n = (int32_t*)a.sized("n_tail", s.B, at::kInt); auto cap = a.integer();
+  a.need(nk == (size_t)s.B * s.Hkv * cap * s.D * 2 && nv == nk, "K_tail, V_tail", "must be [B, Hkv, tail_cap, D]");
+  auto tree = tree_of(a, s.B, T); auto nd = (int32_t*)a.sized("n_draft", s.B, at::kInt);
+  auto out = a.sized("out", n_q, kF32, kBf16);
+  auto type = out && a.bytes() == (size_t)n_q * 2 ? STC_OUT_BF16 : STC_OUT_F32;
+  auto ws = a.ws(); auto nws = a.bytes(); auto st = a.stream();
+  return [=] { return stc_decode_attention_tree(&s, T, P, q, K, v, mask, off, idx, k, Kt, Vt, n, nd, cap, tree.p, tree.per_batch, type, out, ws, nws, st); };)
+
+// The tails of all layers: K_tails, V_tails, n_tails, n_outs (None: the lengths advance in place)
+struct LayerTails {
+  Args::Many K, V, n, out;
+};
+static void layer_tails(Args& a, LayerTails& t, const stc_shape_t& s, int cap) {
+  const int64_t rows = (int64_t)s.B * s.Hkv * cap * s.D;
+  a.many(t.K, "K_tails", rows, kBf16); a.many(t.V, "V_tails", rows, kBf16);
+  a.many(t.n, "n_tails", s.B, at::kInt); a.many(t.out, "n_outs", s.B, at::kInt);
+  a.need(t.V.n == t.K.n && t.n.n == t.K.n && t.out.n == t.K.n, "K_tails, V_tails, n_tails, n_outs", "must be as many");
+}
+
+STC_PY(accept_tail, 8,
+  auto s = *a.shape(); a.one_device(); auto T = a.integer(); auto cap = a.integer();
+  LayerTails t; layer_tails(a, t, s, cap);
+  auto keep = (const uint64_t*)a.sized("keep", s.B, at::kLong, at::kUInt64); auto st = a.stream();
+  return [=] { return stc_accept_tail(&s, T, t.K.n, t.K.p, t.V.p, (const int32_t* const*)t.n.p, (int32_t* const*)t.out.p, cap, keep, st); };)
+
+STC_PY(fork_tail, 9,
+  auto s = *a.shape(); a.one_device(); auto cap = a.integer();
+  LayerTails t; layer_tails(a, t, s, cap);
+  auto src = (const int32_t*)a.sized("src", s.B, at::kInt); auto keep = (const int32_t*)a.sized("n_keep", s.B, at::kInt);
+  auto status = (int32_t*)a.sized("dev_status", 1, at::kInt); auto st = a.stream();
+  return [=] { return stc_fork_tail(&s, t.K.n, t.K.p, t.V.p, (const int32_t* const*)t.n.p, (int32_t* const*)t.out.p, cap, src, keep, status, st); };)
+
 PyMethodDef methods[] = {
 #define STC_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
     STC_METHOD(build_page_bounds), STC_METHOD(route_and_pack_values), STC_METHOD(select_pages),
@@ -364,6 +469,8 @@ PyMethodDef methods[] = {
     STC_METHOD(decode_step_static), STC_METHOD(decode_step_tail), STC_METHOD(flush_tail),
     STC_METHOD(append_tail), STC_METHOD(router_logits), STC_METHOD(compact_tokens),
     STC_METHOD(rotary), STC_METHOD(rotary_append), STC_METHOD(decode_attention_shared),
+    STC_METHOD(rotary_append_tree), STC_METHOD(decode_attention_tree), STC_METHOD(accept_tail),
+    STC_METHOD(fork_tail),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

@@ -80,6 +80,10 @@ struct Rows {
   int64_t b, h, n;  // strides in 16-byte pieces
 };
 
+struct NodeStrides {
+  int64_t b, t;  // in 16-byte pieces
+};
+
 // A thread takes one slot of a row.  Neighbouring lanes take the slots of a row, then the rows that lie next
 // to each other in x (heads of a token, or tokens of a head).  Bound by memory: 16 + 16 bytes in and out
 // for 8 angles, a third of whose arithmetic would fit behind them.  (Four heads a thread, which share their
@@ -162,6 +166,46 @@ __global__ __launch_bounds__(1024) void rotary_append_kernel(
   }
 }
 
+// The nodes of a tree of drafted tokens of every sequence: as above, into the rows behind the tail, whose length
+// stays.  A node stands as many positions behind the tail as it has ancestors.  A thread per slot; sequences along y.
+template <int D>
+__global__ __launch_bounds__(256) void rotary_append_tree_kernel(
+    const u32x4* q, const u32x4* __restrict__ k_new, const u32x4* __restrict__ v_new,
+    const int32_t* __restrict__ n_tail, const int32_t* __restrict__ n_draft, const uint64_t* __restrict__ tree,
+    u32x4* q_out, u32x4* __restrict__ K_tail, u32x4* __restrict__ V_tail, const double* __restrict__ turns,
+    const int32_t* __restrict__ pos, int pos0, int T, int tree_step, int tail_cap, int Hq, int Hkv, int rot_dim,
+    float amplitude, int interleaved, NodeStrides qs, NodeStrides ks, NodeStrides vs, int32_t* dev_status) {
+  constexpr int SLOTS = D / 16, PPR = D / 8;
+  const int b = blockIdx.y, n = n_tail[b], nodes = n_draft ? max(0, min(n_draft[b], T)) : T;
+  if (n < 0) return;
+  if (nodes > tail_cap - n) {  // no room for all of them: none is written
+    if (nodes > 0 && dev_status && blockIdx.x == 0 && threadIdx.x == 0) *dev_status = 1;
+    return;
+  }
+  const int slots = (Hq + 2 * Hkv) * SLOTS, i = blockIdx.x * 256 + threadIdx.x;
+  const int t = i / slots, slot = i % SLOTS, row = i % slots / SLOTS;
+  if (t >= nodes) return;
+  const bool is_q = row < Hq, is_v = row >= Hq + Hkv;
+  const int h = is_q ? row : is_v ? row - Hq - Hkv : row - Hq;
+  const u32x4* src = is_q ? q + b * qs.b + t * qs.t : is_v ? v_new + b * vs.b + t * vs.t : k_new + b * ks.b + t * ks.t;
+  const Slot sl = slot_of(slot, is_v ? 0 : rot_dim, interleaved);
+  u32x4 u = src[h * PPR + sl.first], w = src[h * PPR + sl.second];
+  if (sl.rotated) {
+    int p;
+    if (pos) {
+      p = pos[(size_t)b * T + t];
+    } else {
+      const uint64_t front = (1ull << t) - 1;
+      p = pos0 + n + __builtin_popcountll(tree ? tree[(size_t)b * tree_step + t] & front : front);
+    }
+    rotate(u, w, angles_of(turns, slot, p, amplitude, false), interleaved);
+  }
+  u32x4* dst = is_q ? q_out + (((size_t)b * T + t) * Hq + h) * PPR
+                    : (is_v ? V_tail : K_tail) + (((size_t)b * Hkv + h) * tail_cap + n + t) * PPR;
+  dst[sl.first] = u;
+  dst[sl.second] = w;
+}
+
 }  // namespace
 
 void rotary_turns(int rot_dim, const stc_rotary_scaling_t& s, double* turns) {
@@ -225,6 +269,27 @@ int launch_rotary_append(const stc_shape_t& s, const void* q, int64_t q_stride, 
       (const u32x4*)q, (const u32x4*)k_new, (const u32x4*)v_new, n_tail, (u32x4*)q_out,            \
       (u32x4*)K_tail, (u32x4*)V_tail, turns, pos, pos0, tail_cap, s.Hq, s.Hkv, rot_dim, amplitude, \
       layout == STC_ROTARY_INTERLEAVED, q_stride / 8, k_stride / 8, v_stride / 8, n_out, dev_status)
+  if (s.D == 128) STC_APPEND(128);
+  else STC_APPEND(64);
+#undef STC_APPEND
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+int launch_rotary_append_tree(const stc_shape_t& s, int T, const void* q, const int64_t* q_stride,
+                              const void* k_new, const int64_t* k_stride, const void* v_new,
+                              const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
+                              const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
+                              bool tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
+                              const int32_t* pos, int pos0, int32_t* dev_status, hipStream_t st) {
+  const auto strides = [](const int64_t* x) { return NodeStrides{x[0] / 8, x[1] / 8}; };
+  const long long slots = (long long)T * (s.Hq + 2 * s.Hkv) * (s.D / 16);
+  const dim3 grid((unsigned)((slots + 255) / 256), s.B);
+#define STC_APPEND(DD)                                                                                   \
+  rotary_append_tree_kernel<DD><<<grid, 256, 0, st>>>(                                                   \
+      (const u32x4*)q, (const u32x4*)k_new, (const u32x4*)v_new, n_tail, n_draft, tree, (u32x4*)q_out,   \
+      (u32x4*)K_tail, (u32x4*)V_tail, turns, pos, pos0, T, tree_per_batch ? T : 0, tail_cap, s.Hq, s.Hkv, \
+      rot_dim, amplitude, layout == STC_ROTARY_INTERLEAVED, strides(q_stride), strides(k_stride),        \
+      strides(v_stride), dev_status)
   if (s.D == 128) STC_APPEND(128);
   else STC_APPEND(64);
 #undef STC_APPEND

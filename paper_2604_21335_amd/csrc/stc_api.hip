@@ -574,6 +574,147 @@ int stc_rotary_append(const stc_shape_t* shape, const void* q, int64_t q_stride,
              : STC_OK;
 }
 
+namespace {
+constexpr int kMostNodes = 64, kMostLayers = 1024;
+
+bool tree_ok(const stc_shape_t* s, int T, int n_prefix, int k_pages, int tail_cap) {
+  return shared_ok(s, k_pages, tail_cap) && tail_cap >= 1 && T >= 1 && T <= kMostNodes &&
+         (n_prefix == 1 || n_prefix == s->B);
+}
+
+// Sorts the places of n arrays of so many bytes; whether no two of them overlap.
+bool apart(uintptr_t* at, int n, size_t bytes) {
+  std::sort(at, at + n);
+  for (int i = 1; i < n; ++i)
+    if (at[i] - at[i - 1] < bytes) return false;
+  return true;
+}
+
+// Whether an array of so many bytes overlaps one of the n sorted ones, other than `own`, which it may be itself.
+bool overlaps(const void* p, size_t bytes, const uintptr_t* at, int n, const void* own = nullptr) {
+  const uintptr_t x = (uintptr_t)p;
+  for (const uintptr_t* w = std::lower_bound(at, at + n, x < bytes ? 0 : x - bytes + 1);
+       w != at + n && *w < x + bytes; ++w)
+    if (*w != (uintptr_t)own || *w != x) return true;
+  return false;
+}
+
+// The tails of all layers and their lengths: all there and aligned, and what is written apart from what else is
+// read or written.  `also`: two more arrays of B numbers that are read, or NULL.
+int layers_status(const stc_shape_t* s, int n_layers, void* const* K, void* const* V, const int32_t* const* n,
+                  int32_t* const* out, int tail_cap, const int32_t* also, const int32_t* also2) {
+  uintptr_t tails[2 * kMostLayers], written[kMostLayers];
+  for (int i = 0; i < n_layers; ++i) {
+    if (!K[i] || !V[i] || !n[i] || !out[i]) return STC_ERR_NULL;
+    if (!aligned16(K[i]) || !aligned16(V[i]) || ((uintptr_t)n[i] & 3) || ((uintptr_t)out[i] & 3))
+      return STC_ERR_ALIGN;
+    tails[2 * i] = (uintptr_t)K[i], tails[2 * i + 1] = (uintptr_t)V[i], written[i] = (uintptr_t)out[i];
+  }
+  const size_t lengths = (size_t)s->B * 4;
+  if (!apart(tails, 2 * n_layers, (size_t)s->B * s->Hkv * tail_cap * s->D * 2) ||
+      !apart(written, n_layers, lengths))
+    return STC_ERR_SHAPE;
+  for (int i = 0; i < n_layers; ++i)
+    if (overlaps(n[i], lengths, written, n_layers, out[i])) return STC_ERR_SHAPE;
+  if ((also && overlaps(also, lengths, written, n_layers)) || (also2 && overlaps(also2, lengths, written, n_layers)))
+    return STC_ERR_SHAPE;
+  return STC_OK;
+}
+}  // namespace
+
+int stc_rotary_append_tree(const stc_shape_t* shape, int T, const void* q, const int64_t* q_stride,
+                           const void* k_new, const int64_t* k_stride, const void* v_new,
+                           const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
+                           const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
+                           int tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
+                           const int32_t* pos, int32_t pos0, int32_t* dev_status, void* stream) {
+  if (!shape || !q || !q_stride || !k_new || !k_stride || !v_new || !v_stride || !q_out || !K_tail || !V_tail ||
+      !n_tail)
+    return STC_ERR_NULL;
+  if (rot_dim != 0 && !turns) return STC_ERR_NULL;
+  if (!shape_ok(shape) || T < 1 || T > kMostNodes || tail_cap < 1 || tail_cap > (1 << 30) ||
+      (tree_per_batch != 0 && tree_per_batch != 1) || (rot_dim != 0 && !rot_dim_ok(rot_dim, shape->D)) ||
+      (layout != STC_ROTARY_HALVES && layout != STC_ROTARY_INTERLEAVED) || !isfinite(amplitude))
+    return STC_ERR_SHAPE;
+  if ((long long)T * (shape->Hq + 2ll * shape->Hkv) * (shape->D / 16) > INT32_MAX - 256) return STC_ERR_SHAPE;
+  if (!pos && (long long)pos0 + tail_cap - 1 > INT32_MAX) return STC_ERR_SHAPE;
+  // in place only where every row stays where it is
+  const int64_t row = (int64_t)shape->Hq * shape->D;
+  if (q_out == q && ((shape->B > 1 && q_stride[0] != T * row) || (T > 1 && q_stride[1] != row))) return STC_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(K_tail) ||
+      !aligned16(V_tail) || (turns && !aligned16(turns)) || ((uintptr_t)n_tail & 3) || ((uintptr_t)n_draft & 3) ||
+      ((uintptr_t)pos & 3) || ((uintptr_t)tree & 7) || ((uintptr_t)dev_status & 3))
+    return STC_ERR_ALIGN;
+  for (int i = 0; i < 2; ++i)
+    if (!stride_ok(q_stride[i]) || !stride_ok(k_stride[i]) || !stride_ok(v_stride[i])) return STC_ERR_ALIGN;
+  return stc::launch_rotary_append_tree(*shape, T, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, K_tail,
+                                        V_tail, n_tail, n_draft, tail_cap, tree, tree_per_batch != 0, rot_dim,
+                                        layout, turns, amplitude, pos, pos0, dev_status, (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
+size_t stc_tree_workspace_bytes(const stc_shape_t* shape, int T, int n_prefix, int k_pages, int tail_cap) {
+  if (!shape || !tree_ok(shape, T, n_prefix, k_pages, tail_cap)) return 0;
+  return stc::tree_ws_bytes(*shape, T, n_prefix, k_pages, tail_cap);
+}
+
+int stc_decode_attention_tree(const stc_shape_t* shape, int T, int n_prefix, const void* q, const void* K,
+                              const void* vpacked, const uint16_t* mask, const uint32_t* tok_off,
+                              const int32_t* page_idx, int k_pages, const void* K_tail, const void* V_tail,
+                              const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
+                              int tree_per_batch, int out_type, void* out, void* ws, size_t ws_bytes,
+                              void* stream) {
+  if (!shape || !q || !K || !vpacked || !mask || !tok_off || !K_tail || !V_tail || !n_tail || !out)
+    return STC_ERR_NULL;
+  if (!tree_ok(shape, T, n_prefix, k_pages, tail_cap) || (tree_per_batch != 0 && tree_per_batch != 1) ||
+      (out_type != STC_OUT_F32 && out_type != STC_OUT_BF16))
+    return STC_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(K) || !aligned16(vpacked) || !aligned16(mask) || !aligned16(tok_off) ||
+      (page_idx && !aligned16(page_idx)) || !aligned16(K_tail) || !aligned16(V_tail) || !aligned16(out) ||
+      ((uintptr_t)n_tail & 3) || ((uintptr_t)n_draft & 3) || ((uintptr_t)tree & 7))
+    return STC_ERR_ALIGN;
+  const size_t need = stc::tree_ws_bytes(*shape, T, n_prefix, k_pages, tail_cap);
+  if (!ws || ws_bytes < need || !aligned16(ws)) return STC_ERR_WORKSPACE;
+  return stc::launch_tree(*shape, T, n_prefix, q, K, vpacked, mask, tok_off, page_idx, k_pages, K_tail, V_tail,
+                          n_tail, n_draft, tail_cap, tree, tree_per_batch != 0, out_type == STC_OUT_BF16, out, ws,
+                          (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
+int stc_accept_tail(const stc_shape_t* shape, int T, int n_layers, void* const* K_tail, void* const* V_tail,
+                    const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
+                    void* stream) {
+  if (!shape || !K_tail || !V_tail || !n_tail || !n_out || !keep) return STC_ERR_NULL;
+  if (!shape_ok(shape) || T < 1 || T > kMostNodes || n_layers < 1 || n_layers > kMostLayers || tail_cap < 1 ||
+      tail_cap > (1 << 30))
+    return STC_ERR_SHAPE;
+  if ((uintptr_t)keep & 7) return STC_ERR_ALIGN;
+  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, nullptr, nullptr);
+  if (status != STC_OK) return status;
+  return stc::launch_accept_tail(*shape, T, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep,
+                                 (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
+int stc_fork_tail(const stc_shape_t* shape, int n_layers, void* const* K_tail, void* const* V_tail,
+                  const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const int32_t* src,
+                  const int32_t* n_keep, int32_t* dev_status, void* stream) {
+  if (!shape || !K_tail || !V_tail || !n_tail || !n_out || !src) return STC_ERR_NULL;
+  if (!shape_ok(shape) || shape->B > stc::kForkMost || n_layers < 1 || n_layers > kMostLayers || tail_cap < 1 ||
+      tail_cap > (1 << 30))
+    return STC_ERR_SHAPE;
+  if (((uintptr_t)src & 3) || ((uintptr_t)n_keep & 3) || ((uintptr_t)dev_status & 3)) return STC_ERR_ALIGN;
+  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, src, n_keep);
+  if (status != STC_OK) return status;
+  return stc::launch_fork_tail(*shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, src, n_keep, dev_status,
+                               (hipStream_t)stream)
+             ? STC_ERR_LAUNCH
+             : STC_OK;
+}
+
 int stc_compact_tokens(const void* src, const int32_t* token_idx, void* dst, int32_t B,
                        int32_t Hkv, int32_t N_src, int32_t n_keep, int32_t D,
                        int32_t* dev_status, void* stream) {
