@@ -484,7 +484,8 @@ int stc_rotary_append_tree(const stc_shape_t *shape, int T, const void *q, const
  *            as they are; a query without any token gets zeros
  *   ws       stc_tree_workspace_bytes(...) bytes; calls whose work overlaps in time need one each
  * Magnitudes count as for stc_decode_attention_shared.  Keys and values of a node that are infinite or NaN reach the
- * queries that see it and no others.  The results depend on the sizes, not on other sequences' lengths or trees.
+ * queries that see it and no others.  Where the sums of a query are cut depends on the lengths and nodes of the whole
+ * batch: other sequences change its results by roundings, and by nothing else.
  */
 size_t stc_tree_workspace_bytes(const stc_shape_t *shape, int T, int n_prefix, int k_pages, int tail_cap);
 int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, const void *q, const void *K,

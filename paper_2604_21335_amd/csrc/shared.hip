@@ -225,7 +225,7 @@ constexpr int shared_lds() {
 
 template <int D, int WR, bool LIST, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void shared_kernel(SharedParams P) {
-  extern __shared__ __align__(16) unsigned char lds[];
+  extern __shared__ __align__(256) unsigned char lds[];
   if ((int)blockIdx.x < P.tail_blocks) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     tails<D>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE,
@@ -262,7 +262,11 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams P) {
   const int row = merge_row_of<WPR>();
   const int b = row / P.Hq;
   const int n = row < P.B * P.Hq ? (P.n_tail ? P.n_tail[b] : 0) : -1;
-  merge_row<D, WPR>(P, row, (long long)P.B * P.Hq, n);
+  const int per = kTailTile * P.tail_tiles;
+  const int nt = P.tail_cap && n > 0 ? (min(n, P.tail_cap) + per - 1) / per : 0;
+  const long long p0 = (long long)row * P.splits;
+  const long long t0 = (long long)P.B * P.Hq * P.splits + (long long)row * P.tail_splits - P.splits;
+  merge_row<D, WPR>(P, row, n < 0 ? -1 : P.splits + nt, [&](int i) { return (i < P.splits ? p0 : t0) + i; });
 }
 
 struct SharedPlan {

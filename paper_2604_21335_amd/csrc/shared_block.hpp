@@ -160,7 +160,7 @@ constexpr int kPast = 2;                    // non-temporal: past the caches
 // Tiles [tile0, tile1) of the prefix for the query rows q_row(0 ..) of one KV head; tile t of key group
 // g is tile t * WK + g.  The groups' results are merged; the partial result of row r goes to index(r)
 // (negative: nowhere).
-template <int D, int WR, int T, int STAGES, bool LIST, bool STREAM, class Row, class Index>
+template <int D, int WR, int T, int STAGES, bool LIST, bool STREAM, int PARTS = kParts, class Row, class Index>
 __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds, int kvh, int tile0,
                                        int tile1, Row q_row, Index index) {
   using C = Cfg<D, WR, T, STAGES>;
@@ -287,17 +287,20 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     }
   };
 
-  // Addresses in shared memory, where this thread's pieces go: of one stage at a time
+  // Addresses in shared memory, where this thread's pieces go: of one stage at a time.  Row i * RPI + .. has its piece
+  // shifted by the row's low bits; those that i changes are bits of the address as well (tiles lie at multiples of 256)
   const uint32_t mine = lds_address(lds) + grp * STAGES * C::STAGE;
-  uint32_t pk[C::NI], pv[C::NI];
+  uint32_t pk[1] = {mine + k_at<D>(row0 + row_in, piece)}, pv[1] = {mine + C::TILE + v_at<D>(row0 + row_in, piece)};
+  constexpr uint32_t K_BITS = C::RPI & (C::CH - 1), V_BITS = D == 128 ? (C::RPI & 4) >> 1 : 0;
+  static_assert(C::RPI % 4 == 0 && (D == 128 || C::RPI % 8 == 0) && (STAGES == 1 || C::RPI % 16 == 0), "");
+  auto put = [&](uint32_t at, uint32_t bits, const Data& x) {
 #pragma unroll
-  for (int i = 0; i < C::NI; ++i) {
-    const uint32_t row = i * C::RPI + row0 + row_in;
-    pk[i] = mine + k_at<D>(row, piece), pv[i] = mine + C::TILE + v_at<D>(row, piece);
-  }
-  auto put = [&](const uint32_t (&at)[C::NI], const Data& x) {
+    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>((at ^ (i * bits & (C::CH - 1)) << 4) + i * C::RPI * C::RB) = x[i];
+  };
+  auto put_keys = [&](const Data& x) { put(pk[0], K_BITS, x); };
+  auto put_values = [&](const Data& x) {
 #pragma unroll
-    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>(at[i]) = x[i];
+    for (int i = 0; i < C::NI; ++i) *lds_at<u32x4>((pv[0] ^ (i % 2 * V_BITS) << 4) + i * C::RPI * C::RB) = x[i];
   };
   // on to the next stage of a ring: from stage `at`
   auto advance = [&](auto& a, int at) {
@@ -374,7 +377,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
   auto block = [&](auto NEXT, f32x16& S, int sub, int sub1, int sub2, const Tile& x1, auto between) {
     constexpr int QK = D / 16, HALF = D / 32;  // products of the logits; of the values, per half
     constexpr int STEPS = 2 * QK;
-    u32x4 p[kParts][2];
+    u32x4 p[PARTS][2];
     f32x16 N = {};
     auto read = [&](auto s) {  // the operand of product s
       if constexpr (s < QK) {
@@ -395,7 +398,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     static_for<0, STEPS>([&](auto s) {
       static_for<0, 8>([&](auto j) {
         if constexpr (pair_at(j) + 1 == s)
-          split<kParts>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
+          split<PARTS>(w[j][0], w[j][1], l, [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
       });
       if constexpr (NEXT || s >= QK) read(IC<s + 3>{});
       if constexpr (s < QK) {
@@ -403,7 +406,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
       } else {
         constexpr int v = s - QK;
 #pragma unroll
-        for (int k = kParts - 1; k >= 0; --k)
+        for (int k = PARTS - 1; k >= 0; --k)
           O[v % HALF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
               ring[s % 4], __builtin_bit_cast(bf16x8, p[k][v / HALF]), O[v % HALF], 0, 0, 0);
         if constexpr (v == HALF) made_by_now(l);
@@ -471,7 +474,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     int put_stage = 0, key_stage = 0, value_stage = 0;
     auto on = [](int& s) { s = s == STAGES - 1 ? 0 : s + 1; };
     static_for<0, A>([&](auto i) {
-      put(pk, k0[i]), put(pv, v0[i]);
+      put_keys(k0[i]), put_values(v0[i]);
       advance(pk, put_stage), advance(pv, put_stage), on(put_stage);
     });
     __syncthreads();
@@ -479,9 +482,9 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     static_for<0, 3>([&](auto s) { read_key(s, 1); });
     for (int t = tile0; t < tile1; ++t) {
       auto store = [&](auto s) {
-        if constexpr (s == 0) put(pk, kr);
+        if constexpr (s == 0) put_keys(kr);
         if constexpr (s == 1) put_meta(meta), meta = ask_meta(tile(t, IC<A + 2>{}));
-        if constexpr (s == 2) put(pv, vr);
+        if constexpr (s == 2) put_values(vr);
         if constexpr (s == 3) wave_lds_sync(), get_meta(e);
         if constexpr (s == 4) advance(pk, put_stage), advance(pv, put_stage), on(put_stage);
       };
@@ -518,7 +521,7 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
     get_meta(e);
     ask_values(e, vr);
     for (int t = tile0; t < tile1; ++t) {
-      put(pk, kr), put(pv, vr);
+      put_keys(kr), put_values(vr);
       put_meta(m1);
       const Tile here = x0;
       x0 = x1, x1 = x2, x2 = look(tile_of(t + 3));
@@ -586,17 +589,13 @@ __device__ __forceinline__ void attend(const SharedParams& P, unsigned char* lds
 // Merges the partial results of a row in a fixed order: the prefix's splits, then those of the tail that
 // hold tokens.  WPR wavefronts per row; D/4 lanes take four channels each of a partial result, 16 bytes
 // a lane, and the groups of so many lanes share the partial results out.
-// `row` of `rows`; n: the row's tail tokens, negative where it is padding.
-template <int D, int WPR>
-__device__ __forceinline__ void merge_row(const SharedParams& P, int row, long long rows, int n) {
+// total: partial results of the row, place(i) where they are; negative for padding.
+template <int D, int WPR, class Place>
+__device__ __forceinline__ void merge_row(const SharedParams& P, int row, int total, Place place) {
   constexpr int L = D / 4, GPW = 64 / L, GROUPS = GPW * WPR, AHEAD = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (WPR == 1 && n < 0) return;  // padding: its rows of the output stay as they are
-  const int per = kTailTile * P.tail_tiles;
-  const int nt = P.tail_cap && n > 0 ? (min(n, P.tail_cap) + per - 1) / per : 0;
-  const long long p0 = (long long)row * P.splits;
-  const long long t0 = rows * P.splits + (long long)row * P.tail_splits - P.splits;
-  const int total = n < 0 ? 0 : P.splits + nt;
+  const bool padding = total < 0;
+  if (WPR == 1 && padding) return;  // its rows of the output stay as they are
   const f32x4* acc = (const f32x4*)P.acc;
   const f32x2* ml = (const f32x2*)P.ml;
   const int group = (WPR > 1 ? wave % WPR : 0) * GPW + lane / L, quad = lane % L;
@@ -608,7 +607,7 @@ __device__ __forceinline__ void merge_row(const SharedParams& P, int row, long l
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const int i = i0 + k * GROUPS;
-      const long long at = (i < P.splits ? p0 : t0) + i;
+      const long long at = place(i);
       e[k] = f32x2{kNone, 0.0f}, x[k] = f32x4{0, 0, 0, 0};
       if (i < total) e[k] = ml[at], x[k] = acc[at * L + quad];
     }
@@ -647,7 +646,7 @@ __device__ __forceinline__ void merge_row(const SharedParams& P, int row, long l
     if (lane < L) s_o[wave][lane] = o;
     if (lane == 0) s_e[wave] = f32x2{top, sum};
     __syncthreads();
-    if (wave % WPR != 0 || n < 0) return;
+    if (wave % WPR != 0 || padding) return;
 #pragma unroll
     for (int w = 1; w < WPR; ++w) join(s_e[wave + w][0], s_e[wave + w][1], s_o[wave + w][quad]);
   }

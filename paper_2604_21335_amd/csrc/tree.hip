@@ -15,10 +15,28 @@ using namespace shared;
 struct TreeParams : SharedParams {
   const int32_t* n_draft;
   const uint64_t* tree;
+  int32_t* where;         // compact: splits, row blocks, then where a sequence's nodes begin among all
+  int2* shares;           // of the tails, by block of rows: the first one that works on it, and how many follow
   int T, tree_step;       // nodes of a sequence; sets from one sequence to the next (0: one for all)
   int streams, rows;      // KV heads of all prefixes, query rows of each
   int prefix_seqs;        // sequences of a prefix
+  int items, tiles;       // row blocks of all splits that the launch has room for; tiles of a prefix
+  int compact;            // only nodes that are there are rows
+  uint32_t item_cost;     // time of a row block of a split, in tiles of the tails
+  int tail_rb;            // row blocks of a sequence and KV head, at most
+  long long first_at, next_at;  // places of the tails' partial results: of fragments that begin a tail, of others
 };
+
+// Splits of a prefix where `items` row blocks of splits may work at a time on so many row blocks of all prefixes.
+struct Splits {
+  int n, tiles;
+};
+__host__ __device__ inline Splits splits_of(long long items, long long blocks, int tiles) {
+  long long n = items / blocks;
+  n = n < 1 ? 1 : n > tiles ? tiles : n;
+  const int each = (int)((tiles + n - 1) / n);
+  return {(tiles + each - 1) / each, each};
+}
 
 // What sequence b has: tokens in front of the nodes, with the nodes, and nodes.  Padding has none.
 struct Held {
@@ -31,189 +49,153 @@ __device__ __forceinline__ Held held(const TreeParams& P, int b) {
   return {first, min(first + nodes, P.tail_cap), nodes};
 }
 
-// Weights of a wavefront's rows that are not finite in bf16, as sign, exponent and fraction lie.
-__device__ __forceinline__ bool endless(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
+// The tails and nodes as a row of tiles: of all sequences, their KV heads, blocks of 32 query rows (node by node, R rows
+// each), tiles of 32 tokens.
+struct Run {
+  uint32_t tiles, blocks;  // of a sequence: of a KV head's block, of a KV head
+};
+__device__ __forceinline__ Run run_of(const TreeParams& P, const Held& h) {
+  return {(uint32_t)(h.n + kTailTile - 1) / kTailTile, (uint32_t)(h.nodes * P.R + kRows - 1) / kRows};
+}
+__device__ __forceinline__ uint32_t tiles_of(const TreeParams& P, const Held& h) {
+  const Run r = run_of(P, h);
+  return r.tiles * r.blocks * P.Hkv;
+}
 
-// The tails and the nodes.  A wavefront takes blocks of 32 query rows (node by node, R rows each) over pieces of
-// P.tail_tiles tiles of 32 tokens, one after the other, with the next tile on its way while one is worked on.  The
-// blocks that hold nodes, in order of sequence, KV head, piece and row, are shared out evenly over the nw wavefronts,
-// which add up the lengths for it; where a piece begins depends on the sizes alone.
-template <int D>
-__device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds, int w, int nw) {
-  using C = Cfg<D, 1, kTailTile, 1>;
-  constexpr int RB = C::RB, NI = C::NI;
-  const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
-  const int per = kTailTile * P.tail_tiles;  // tokens of a piece
-  auto pieces_of = [&](int n) { return (uint32_t)(n + per - 1) / (uint32_t)per; };
-  auto blocks_of = [&](int nodes) { return (uint32_t)(nodes * P.R + kRows - 1) / kRows; };
-  auto units_of = [&](const Held& h) { return h.nodes > 0 ? pieces_of(h.n) * blocks_of(h.nodes) : 0u; };
-  auto of_lane = [&](int base) { return base + lane < P.B ? held(P, base + lane) : Held{0, 0, 0}; };
-  uint32_t total = 0;
-  for (int base = 0; base < P.B; base += 64) total += wave_reduce(units_of(of_lane(base)), OpAdd{}, 0u);
-  const uint64_t all = (uint64_t)total * P.Hkv;
-  uint32_t at = (uint32_t)(all * w / nw);
-  const uint32_t end = (uint32_t)(all * (w + 1) / nw);
-  if (at >= end) return;
-
-  // The sequence that block `at` belongs to, found again among the lengths (which a caller must not change
-  // meanwhile; if it does, the search still ends, and the results are meaningless).
-  int base = 0, b = P.B;
-  Held lens = of_lane(0), h{0, 0, 0};
-  uint32_t seen = 0, in_b = 0;  // blocks in front of sequence b; of sequence b, all KV heads
-  auto lane_held = [&](int j) {
-    return Held{__builtin_amdgcn_readlane(lens.n0, j), __builtin_amdgcn_readlane(lens.n, j),
-                __builtin_amdgcn_readlane(lens.nodes, j)};
-  };
-  for (; base < P.B; base += 64, lens = of_lane(base)) {
-    const uint32_t mine = units_of(lens), incl = wave_scan(mine, OpAdd{}, 0u);
-    const uint64_t past = __builtin_amdgcn_ballot_w64((seen + incl) * (uint64_t)P.Hkv > at);
-    if (past) {
-      const int j = __builtin_ctzll(past);
-      b = base + j;
-      h = lane_held(j);
-      in_b = units_of(h) * P.Hkv;
-      seen = (seen + __builtin_amdgcn_readlane(incl, j)) * P.Hkv - in_b;
-      break;
+// How the tiles are shared out: share s, of one wavefront, begins at begin(s), and none is empty.  Workgroups in front of
+// `more` had a row block of a prefix more than those behind, whose wavefronts take tiles for its time first; where that
+// is (nearly) all of them, only they have shares.  A share has kGrain tiles at least (but the only one), so that few tiles do
+// not become as many partial results.  In whole numbers, since both launches have to find the same.
+constexpr uint32_t kGrain = 2;
+struct Shares {
+  uint32_t all, each, odd;         // tiles; tiles of a share, and what is left over all of them
+  int from, waves, count, more;    // wavefronts that have shares: from the first on, so many; shares
+  uint32_t lead;                   // tiles of a workgroup behind `more` first
+  __device__ __forceinline__ Shares(uint32_t all, int groups, int more, uint32_t item_cost)
+      : all(all), more(more), lead(0) {
+    const uint32_t total = groups * kWaves, fewer = groups - more;
+    if (fewer > 0 && all / fewer < item_cost + kGrain * total / fewer) {
+      from = more * kWaves, waves = fewer * kWaves;
+    } else {
+      from = 0, waves = total;
+      if (fewer > 0) lead = item_cost;
     }
-    seen += __builtin_amdgcn_readlane(incl, 63);
+    const uint32_t rest = all - lead * fewer;
+    count = max(min((int)min(rest / kGrain, 1u << 20), waves), 1);
+    each = rest / count, odd = rest % count;
   }
-  if (b >= P.B) return;
-  int kvh, piece, rb, t, t_end;
-  auto open = [&] {  // the place of block `at` in sequence b
-    const uint32_t nb = blocks_of(h.nodes), each = pieces_of(h.n) * nb, i = at - seen, j = i % each;
-    kvh = i / each, piece = j / nb, rb = j % nb;
-    t = piece * P.tail_tiles;
-    t_end = min((h.n + kTailTile - 1) / kTailTile, t + P.tail_tiles);
-  };
-  open();
+  __device__ __forceinline__ uint32_t begin(int s) const {
+    const int g = s / kWaves;  // (with a lead every wavefront has a share)
+    uint32_t x = each * s + odd * s / count;
+    if (lead && g >= more) x += lead * (g - more) + lead * (s % kWaves) / kWaves;
+    return s >= count ? all : x;
+  }
+  // The share of wavefront w, -1 if it has none: share s is that of wavefront from + s * waves / count
+  __device__ __forceinline__ int of_wave(int w) const {
+    const int i = w - from;
+    if (i < 0 || i >= waves) return -1;
+    const int s = (i * count + waves - 1) / waves;
+    return s < count && s * waves / count == i ? s : -1;
+  }
+  __device__ __forceinline__ int of_tile(uint32_t tile) const {  // tile < all
+    const float of_share = each + (float)odd / count, bend = lead ? of_share * (more * kWaves) : (float)all;
+    const float x = tile < bend ? tile / of_share
+                                : more * kWaves + (tile - bend) / (of_share + (float)lead / kWaves);
+    int s = min((int)x, count - 1);  // about
+    while (s > 0 && begin(s) > tile) --s;
+    while (begin(s + 1) <= tile) ++s;
+    return s;
+  }
+};
+__device__ __forceinline__ int groups_with_more(int items, int groups) {
+  const int each = (items + kXcds - 1) / kXcds, per = groups / kXcds, turns = (each + per - 1) / per;
+  return turns ? kXcds * (each - (turns - 1) * per) : 0;
+}
 
-  u32x4 kr[NI], vr[NI];
-  auto tile_at = [&] { return ((size_t)b * P.Hkv + kvh) * P.tail_cap + (size_t)t * kTailTile; };
-  auto ask = [&] {
-    const size_t row = tile_at();
-    const int bytes = min(kTailTile, h.n - t * kTailTile) * RB;
-    const Rsrc rk = rsrc(P.Kt + row * RB, bytes), rv = rsrc(P.Vt + row * RB, bytes);
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, i * 1024 + lane * 16, 0, 0);
-      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, i * 1024 + lane * 16, 0, 0);
-    }
-  };
-  // Query row c of the block: its place in the output, the nodes that it sees, its operand of S^T
+// 16 (or 4, or 2) bytes a lane from the buffer, `at` bytes behind its base, to shared memory: lane after lane from `to` on.
+// What lies behind the buffer's end comes as zeros.  Written out, and waited for by number (they end in order, and with
+// them whatever else was asked for), since the compiler would wait for all of them in front of any read of shared memory.
+// (The buffer's base is the wavefront's, whatever the compiler made of it.)
+__device__ __forceinline__ Rsrc buffer(const void* base, uint32_t bytes) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  return rsrc((const void*)(uintptr_t)u, bytes);
+}
+template <int PAST>
+__device__ __forceinline__ void fetch16(Rsrc r, uint32_t at, uint32_t to) {
+  if constexpr (PAST)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(at), "s"(r)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
+                 : "memory");
+}
+__device__ __forceinline__ void fetch4(Rsrc r, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
+               : "memory");
+}
+__device__ __forceinline__ void fetch2(Rsrc r, uint32_t at, uint32_t to) {  // (four bytes there, the upper two zero)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ushort %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void fetched() {  // all but the last N
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void have_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A wavefront's 32 query rows, a lane's row c = lane % 32, and its tile of 32 tokens: keys, then values, in shared memory.
+// The tile's keys are free for the next ones behind the logits, its values behind the products, so one place is enough:
+// while one of the two is worked on, the other is on its way.
+template <int D>
+struct Rows32 {
+  static constexpr int RB = 2 * D, CH = D / 8, RPW = 64 / CH, NI = kTailTile / RPW;  // loads for keys, or values
+  static constexpr int TILE = kTailTile * RB;
   bf16x8 qf[D / 16];
-  uint64_t vis;
-  long long row_at;
-  auto ask_q = [&] {
-    const int r = rb * kRows + c, node = r / P.R;
-    const bool on = node < h.nodes;
-    row_at = on ? ((long long)b * P.T + node) * P.Hq + kvh * P.R + r % P.R : -1;
-    vis = 0;
-    if (on) vis = P.tree ? P.tree[(size_t)b * P.tree_step + node] : (2ull << node) - 1;
-    vis &= ~0ull >> (64 - h.nodes);
-    const uint16_t* qr = P.q + (on ? row_at * D : 0);
+  f32x16 O[D / 32];
+  float m, l, scale;
+  uint32_t keys, values;    // where the tile lies
+  uint32_t ka, va;          // where this lane reads its first operands
+  uint32_t k_from, v_from;  // what this lane fetches first: bytes behind the tile's base
+
+  __device__ __forceinline__ explicit Rows32(unsigned char* lds) {
+    const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5, j16 = lane & 15;
+    scale = kLog2e / sqrtf((float)D);
+    keys = __builtin_amdgcn_readfirstlane(lds_address(lds)), values = keys + TILE;
+    ka = keys + k_at<D>(c, half);
+    va = values + v_at<D>(4 * half + (j16 >> 2), ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1)) + 8 * (j16 & 1);
+    k_from = k_at<D>(lane / CH, lane % CH), v_from = v_at<D>(lane / CH, lane % CH);
+  }
+  // Fetch i brings rows i * RPW ..; a row's low bits shift its pieces, so those that i changes are bits of the address
+  static __device__ __forceinline__ uint32_t k_bits(int i) { return D == 128 ? (i & 3) << 6 : 0; }
+  static __device__ __forceinline__ uint32_t v_bits(int i) { return D == 128 ? (i & 1) << 5 : 0; }
+
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) O[i][j] = 0.0f;
+    m = kNone, l = 0.0f;
+  }
+  __device__ __forceinline__ void ask_queries(const uint16_t* q, bool on) {
+    const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       u32x4 x = {0, 0, 0, 0};
-      if (on) x = *(const u32x4*)(qr + 16 * s + 8 * half);
+      if (on) x = *(const u32x4*)(q + 16 * s + 8 * half);
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
-  };
-  ask();
-  ask_q();
-
-  // Addresses in shared memory: as in attend()
-  const uint32_t mine = lds_address(lds);
-  const uint32_t row_in = lane / C::CH, col = lane % C::CH;
-  uint32_t ka[D / 16], va[D / 32];
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) ka[s] = mine + k_at<D>(c, 2 * s + half);
-  const int j16 = lane & 15;
-#pragma unroll
-  for (int cb = 0; cb < D / 32; ++cb)
-    va[cb] = mine + C::TILE + v_at<D>(4 * half + (j16 >> 2), cb * 4 + ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1)) +
-             8 * (j16 & 1);
-
-  f32x16 O[D / 32];
-  float m, l;
-  const float scale = kLog2e / sqrtf((float)D);
-  bool more = true, first = true;
-  while (more) {
-    if (first) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) O[i][j] = 0.0f;
-      m = kNone, l = 0.0f;
-    }
-    const int tok0 = t * kTailTile, rows = h.n - tok0;
-    const int node0 = h.n0 - tok0;  // row of the tile where the nodes begin
-    const bool ragged = node0 < kTailTile || rows < kTailTile;
-    // A weight of zero times an infinity or NaN is NaN, and a row must not get that from a node that it does not
-    // see: such values count as zero in the products, and rows that see them take them in afterwards.
-    const size_t v_tile = tile_at();
-    bool bad = false;
-    if (node0 < kTailTile) {
-      bool any = false;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          any |= i * C::RPW + (int)row_in >= node0 && (endless(vr[i][k]) || endless(vr[i][k] >> 16));
-      bad = __builtin_amdgcn_ballot_w64(any) != 0;
-      if (bad) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-          if (i * C::RPW + (int)row_in >= node0)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              vr[i][k] &= (endless(vr[i][k]) ? 0u : 0xffffu) | (endless(vr[i][k] >> 16) ? 0u : 0xffff0000u);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const uint32_t row = i * C::RPW + row_in;
-      *lds_at<u32x4>(mine + k_at<D>(row, col)) = kr[i];
-      *lds_at<u32x4>(mine + C::TILE + v_at<D>(row, col)) = vr[i];
-    }
-    // Rows of the tile that this query row attends
-    uint32_t see = ~0u;
-    if (node0 <= 0) see = (uint32_t)(vis >> min(-node0, 63));
-    else if (node0 < kTailTile) see = (uint32_t)(vis << node0) | ((1u << node0) - 1u);
-    if (rows < kTailTile) see &= (1u << rows) - 1u;
-    // this block's place, then the next one's
-    const bool last = t + 1 == t_end;
-    const long long index = row_at < 0 ? -1
-                                       : (long long)P.B * P.T * P.Hq * P.splits + row_at * P.tail_splits + piece;
-    if (!last) {
-      ++t;
-    } else if (++at < end) {
-      if (at - seen >= in_b) {  // the next sequence with nodes
-        seen += in_b;
-        in_b = 0;
-        while (in_b == 0 && ++b < P.B) {
-          if (b == base + 64) base += 64, lens = of_lane(base);
-          h = lane_held(b - base);
-          in_b = units_of(h) * P.Hkv;
-        }
-      }
-      more = in_b > 0;
-      if (more) open();
-    } else {
-      more = false;
-    }
-    if (more) ask();
-    wave_lds_sync();
-
+  }
+  // S^T: register 4 a + i of a lane is token 8 a + 4 (lane / 32) + i
+  __device__ __forceinline__ f32x16 logits() const {
     f32x16 S = {};
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
-      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*lds_at<const bf16x8>(ka[s]), qf[s], S, 0, 0, 0);
-    if (last && more) ask_q();
-    if (ragged) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1u)) S[i] = -INFINITY;
-    }
+      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*lds_at<const bf16x8>(ka ^ s << 5), qf[s], S, 0, 0, 0);
+    return S;
+  }
+  __device__ __forceinline__ void take_top(const f32x16& S) {
     float top = fmaxf(S[0], S[1]);
 #pragma unroll
     for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(S[i], S[i + 1]), top);
@@ -227,11 +209,18 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
 #pragma unroll
         for (int j = 0; j < 16; ++j) O[i][j] *= f;
     }
-    u32x4 p[kTailParts][2];
+  }
+  // The weights' parts of 16 tokens at a time, and their products with the values
+  using Parts = u32x4[2][kTailParts];
+  __device__ __forceinline__ void weights(const f32x16& S, Parts& p) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      split<kTailParts>(weight(S[2 * j], scale, m), weight(S[2 * j + 1], scale, m), l,
-                        [&](int k, uint32_t x) { p[k][j / 4][j % 4] = x; });
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        split<kTailParts>(weight(S[8 * ks + 2 * j], scale, m), weight(S[8 * ks + 2 * j + 1], scale, m), l,
+                          [&](int k, uint32_t x) { p[ks][k][j] = x; });
+  }
+  __device__ __forceinline__ void products(const Parts& p) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -239,42 +228,369 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
         i16x4 a[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4>(va[cb] + (16 * ks + 8 * k) * RB));
+          a[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4>((va ^ cb << 6) + (16 * ks + 8 * k) * RB));
         const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
         for (int k = kTailParts - 1; k >= 0; --k)
-          O[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, p[k][ks]), O[cb], 0, 0, 0);
+          O[cb] =
+              __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, p[ks][k]), O[cb], 0, 0, 0);
       }
+  }
+  __device__ __forceinline__ void store(const TreeParams& P, long long place, bool on) {
+    const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+    const float sum = sum_halves(l);
+    if (!on) return;
+    float* o = P.acc + (place + c) * D;
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        *(f32x4*)(o + cb * 32 + 8 * a + 4 * half) =
+            f32x4{O[cb][4 * a], O[cb][4 * a + 1], O[cb][4 * a + 2], O[cb][4 * a + 3]};
+    if (half == 0) *(f32x2*)(P.ml + (place + c) * 2) = f32x2{m, sum};
+  }
+};
+
+// An infinity or NaN in the low half, bf16
+__device__ __forceinline__ bool endless(uint32_t half) { return (half & 0x7f80u) == 0x7f80u; }
+
+// The tails and the nodes: wavefront w's share of their tiles.  Where a share begins inside a block's tiles, their partial
+// result is the share's one `next`; others are their blocks' `first`.  PAST: read once, past the caches.
+template <int D, int PAST>
+__device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds, int w, int groups, int more) {
+  using C = Rows32<D>;
+  constexpr int RB = C::RB, NI = C::NI;
+  const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+  auto of_lane = [&](int base) { return base + lane < P.B ? held(P, base + lane) : Held{0, 0, 0}; };
+  uint32_t total = 0;
+  for (int base = 0; base < P.B; base += 64) total += wave_reduce(tiles_of(P, of_lane(base)), OpAdd{}, 0u);
+  if (total == 0) return;
+  const Shares shares(total, groups, more, P.item_cost);
+  const int share = shares.of_wave(w);
+  if (share < 0) return;
+  uint32_t at = __builtin_amdgcn_readfirstlane(shares.begin(share));
+  const uint32_t end = __builtin_amdgcn_readfirstlane(shares.begin(share + 1));
+  if (at >= end) return;
+
+  // The sequence that tile `at` belongs to, found again among the lengths (which a caller must not change
+  // meanwhile; if it does, the search still ends, and the results are meaningless).
+  int base = 0, b = P.B;
+  Held lens = of_lane(0), h{0, 0, 0};
+  uint32_t seen = 0, in_b = 0;  // tiles in front of sequence b; of sequence b
+  auto lane_held = [&](int j) {
+    return Held{__builtin_amdgcn_readlane(lens.n0, j), __builtin_amdgcn_readlane(lens.n, j),
+                __builtin_amdgcn_readlane(lens.nodes, j)};
+  };
+  for (; base < P.B; base += 64, lens = of_lane(base)) {
+    const uint32_t mine = tiles_of(P, lens), incl = wave_scan(mine, OpAdd{}, 0u);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(seen + incl > at);
+    if (past) {
+      const int j = __builtin_ctzll(past);
+      b = base + j;
+      h = lane_held(j);
+      in_b = tiles_of(P, h);
+      seen += __builtin_amdgcn_readlane(incl, j) - in_b;
+      break;
+    }
+    seen += __builtin_amdgcn_readlane(incl, 63);
+  }
+  if (b >= P.B) return;
+  int kvh, rb, t, t_end;
+  bool begins;  // a block's tiles begin here
+  auto open = [&] {  // the place of tile `at` in sequence b
+    const Run r = run_of(P, h);
+    const uint32_t i = at - seen, of_head = r.tiles * r.blocks, j = i % of_head;
+    kvh = i / of_head, rb = j / r.tiles, t = j % r.tiles;
+    t_end = min(r.tiles, t + (end - at));
+    begins = t == 0;
+    if (begins && lane == 0)
+      P.shares[((size_t)b * P.Hkv + kvh) * P.tail_rb + rb] = int2{share, shares.of_tile(at + r.tiles - 1) - share};
+    at += t_end - t;
+  };
+  open();
+
+  C x(lds);
+  auto tile_at = [&] { return ((size_t)b * P.Hkv + kvh) * P.tail_cap + (size_t)t * kTailTile; };
+  auto fetch_keys = [&] {
+    const Rsrc r = buffer(P.Kt + tile_at() * RB, min(kTailTile, h.n - t * kTailTile) * RB);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) fetch16<PAST>(r, (x.k_from ^ C::k_bits(i)) + i * 1024, x.keys + i * 1024);
+  };
+  auto fetch_values = [&] {
+    const Rsrc r = buffer(P.Vt + tile_at() * RB, min(kTailTile, h.n - t * kTailTile) * RB);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) fetch16<PAST>(r, (x.v_from ^ C::v_bits(i)) + i * 1024, x.values + i * 1024);
+  };
+  // Query row c of the block: the nodes that it sees, its operand of S^T
+  uint64_t vis;
+  bool on;
+  auto ask_queries = [&] {
+    const int r = rb * kRows + c, node = r / P.R;
+    on = node < h.nodes;
+    vis = 0;
+    if (on) vis = P.tree ? P.tree[(size_t)b * P.tree_step + node] : (2ull << node) - 1;
+    vis &= ~0ull >> (64 - h.nodes);
+    const long long row = ((long long)b * P.T + node) * P.Hq + kvh * P.R + r % P.R;
+    x.ask_queries(P.q + (on ? row * D : 0), on);
+  };
+  fetch_keys();
+  ask_queries();
+  fetch_values();
+
+  bool first = true;
+  while (true) {
+    if (first) x.begin();
+    const int tok0 = t * kTailTile, rows = h.n - tok0;
+    const int node0 = h.n0 - tok0;  // row of the tile where the nodes begin
+    const size_t v_tile = tile_at();
+    // Rows of the tile that this query row attends
+    uint32_t see = ~0u;
+    if (node0 <= 0) see = (uint32_t)(vis >> min(-node0, 63));
+    else if (node0 < kTailTile) see = (uint32_t)(vis << node0) | ((1u << node0) - 1u);
+    if (rows < kTailTile) see &= (1u << rows) - 1u;
+    // this block's place, then the next one's
+    const bool last = t + 1 == t_end, stored = on;
+    const long long place = begins ? P.first_at + (((long long)b * P.Hkv + kvh) * P.tail_rb + rb) * kRows
+                                   : P.next_at + (long long)share * kRows;
+    bool goes_on = true;
+    if (!last) {
+      ++t;
+    } else if (at < end) {
+      if (at - seen >= in_b) {  // the next sequence with nodes
+        seen += in_b;
+        in_b = 0;
+        while (in_b == 0 && ++b < P.B) {
+          if (b == base + 64) base += 64, lens = of_lane(base);
+          h = lane_held(b - base);
+          in_b = tiles_of(P, h);
+        }
+      }
+      goes_on = in_b > 0;
+      if (goes_on) open();
+    } else {
+      goes_on = false;
+    }
+
+    fetched<NI>();  // keys
+    f32x16 S = x.logits();
+    have_read();
+    if (goes_on) fetch_keys();
+    if (last && goes_on) ask_queries();
+    if (node0 < kTailTile || rows < kTailTile) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1u)) S[i] = -INFINITY;
+    }
+    x.take_top(S);
+    typename C::Parts p;
+    x.weights(S, p);
+    if (goes_on) fetched<NI>();
+    else fetched<0>();
+    // A weight of zero times an infinity or NaN is NaN, and a row must not get that from a node that it does not
+    // see: such values count as zero in the products, and rows that see them take them in afterwards.
+    bool bad = false;
+    if (node0 < kTailTile) {
+#pragma unroll 1
+      for (int i = 0; i < NI; ++i) {
+        u32x4 v = *lds_at<const u32x4>(x.values + i * 1024 + lane * 16);
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) any |= endless(v[k]) || endless(v[k] >> 16);
+        any = any && i * C::RPW + lane / C::CH >= node0;
+        bad |= __builtin_amdgcn_ballot_w64(any) != 0;
+        if (any) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            v[k] &= (endless(v[k]) ? 0u : 0xffffu) | (endless(v[k] >> 16) ? 0u : 0xffff0000u);
+          *lds_at<u32x4>(x.values + i * 1024 + lane * 16) = v;
+        }
+      }
+      wave_lds_sync();
+    }
+    x.products(p);
+    have_read();
+    if (goes_on) fetch_values();
     if (bad) {
       const uint16_t* V = (const uint16_t*)P.Vt + v_tile * D;
+#pragma unroll 1
       for (int k = max(node0, 0); k < min(rows, kTailTile); ++k) {
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
           for (int a = 0; a < 4; ++a) {
-            const u32x2 x = *(const u32x2*)(V + k * D + cb * 32 + 8 * a + 4 * half);
+            const u32x2 v = *(const u32x2*)(V + k * D + cb * 32 + 8 * a + 4 * half);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t e = x[i / 2] >> (i % 2 * 16);
-              if (endless(e) && (see >> k & 1u)) O[cb][4 * a + i] += __uint_as_float(e << 16);
+              const uint32_t e = v[i / 2] >> (i % 2 * 16);
+              if (endless(e) && (see >> k & 1u)) x.O[cb][4 * a + i] += __uint_as_float(e << 16);
             }
           }
       }
     }
-    wave_lds_sync();
-    if (last) {
-      const float sum = sum_halves(l);
-      if (index >= 0) {
-        float* o = P.acc + index * D;
-#pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb)
-#pragma unroll
-          for (int a = 0; a < 4; ++a)
-            *(f32x4*)(o + cb * 32 + 8 * a + 4 * half) =
-                f32x4{O[cb][4 * a], O[cb][4 * a + 1], O[cb][4 * a + 2], O[cb][4 * a + 3]};
-        if (half == 0) *(f32x2*)(P.ml + index * 2) = f32x2{m, sum};
+    if (last) x.store(P, place, stored);
+    if (!goes_on) break;
+    first = last;
+  }
+}
+
+// Few query rows over many prefixes: P.rows <= 32 rows of each of P.streams streams.  A wavefront takes whole splits of
+// streams, from `unit` to `end`, tile by tile (32 tokens) without a stop between them: masks and offsets are fetched a
+// tile ahead of the values that they lead to, and list entries a tile ahead of those.
+constexpr int kFlowMeta = 4 * 256 + 2 * 256;  // bytes of two tiles' offsets and masks, two tiles' list entries
+template <int D, bool LIST, int PAST>
+__device__ __forceinline__ void flow(const TreeParams& P, unsigned char* lds, unsigned char* meta_lds, int unit, int end) {
+  using C = Rows32<D>;
+  constexpr int RB = C::RB, NI = C::NI;
+  if (unit >= end) return;
+  const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+  const uint32_t row_in = lane / C::CH;
+  const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G)), lg_group = lg_upg + 4;
+  const int tokens = min(P.N, P.k_pages * kPage);
+
+  // A tile: of which split, and its two pages (with a list), -1 where there is none
+  struct Place {
+    int unit, stream, tile, page[2];
+  };
+  auto on = [&](Place x) {  // the tile behind it; behind the last one, the same again
+    const int split = x.unit - x.stream * P.splits;
+    if (++x.tile >= min(P.tiles, (split + 1) * P.split_tiles)) {
+      if (x.unit + 1 < end) {
+        ++x.unit;
+        x.stream = x.unit / P.splits;
+        x.tile = (x.unit - x.stream * P.splits) * P.split_tiles;
+      } else {
+        --x.tile;
       }
     }
+    return x;
+  };
+  // Tokens of the tile's half that are there, and its first token
+  auto rows_of = [&](const Place& x, int i) {
+    if constexpr (LIST) return x.page[i] < 0 ? 0 : min(kPage, P.N - x.page[i] * kPage);
+    return max(0, min(kPage, tokens - x.tile * kTailTile - i * kPage));
+  };
+  auto first_of = [&](const Place& x, int i) -> size_t {
+    if constexpr (LIST) return (size_t)max(x.page[i], 0) * kPage;
+    return (size_t)x.tile * kTailTile + i * kPage;
+  };
+  C w(lds);
+  const uint32_t metas = __builtin_amdgcn_readfirstlane(lds_address(meta_lds)), lists = metas + 1024;
+  auto fetch_list = [&](const Place& x, int slot) {  // lanes 0 and 1; the others' are not used
+    const int left = P.k_pages - 2 * x.tile;
+    fetch4(buffer(P.pages + (size_t)x.stream * P.k_pages + 2 * x.tile, min(left, 2) * 4), lane * 4, lists + slot * 256);
+  };
+  auto read_list = [&](Place& x, int slot) {
+    const u32x2 e = *lds_at<const u32x2>(lists + slot * 256);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x.page[i] = __builtin_amdgcn_readfirstlane(e[i]);
+      if ((unsigned)x.page[i] >= (unsigned)P.NP || 2 * x.tile + i >= P.k_pages) x.page[i] = -1;
+    }
+  };
+  // Offsets and masks, four fetches: each half's 16, then zeros, by lanes 0 .. 15 and 32 .. 47
+  auto fetch_meta = [&](const Place& x, int slot) {
+    const uint32_t to = metas + slot * 512;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int n = rows_of(x, i);
+      const size_t t = n > 0 ? first_of(x, i) : 0;
+      const Rsrc o = buffer(P.off + (size_t)x.stream * (P.Ncap + 1) + t, n * 4);
+      const Rsrc k = buffer(P.mask + (size_t)x.stream * P.Ncap + t, n * 2);
+      if (half == i) {
+        fetch4(o, c * 4, to);
+        fetch2(k, c * 2, to + 256);
+      }
+    }
+  };
+  auto fetch_keys = [&](const Place& x) {
+    const unsigned char* Ks = P.K + (size_t)x.stream * P.Ncap * RB;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Rsrc r = buffer(Ks + first_of(x, h) * RB, rows_of(x, h) * RB);
+#pragma unroll
+      for (int j = 0; j < NI / 2; ++j) {
+        const int i = h * NI / 2 + j;
+        fetch16<PAST>(r, (w.k_from ^ C::k_bits(i)) + j * 1024, w.keys + i * 1024);
+      }
+    }
+  };
+  auto fetch_values = [&](const Place& x, int slot) {
+    const unsigned char* Vs = P.v + ((size_t)x.stream * P.v_stride << lg_group);
+    const uint32_t meta = metas + slot * 512;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // from the half's first kept group on: its values lie within 16 * 16 groups
+      const uint32_t first = __builtin_amdgcn_readfirstlane(*lds_at<const uint32_t>(meta + h * 128));
+      const uint32_t room = P.cap > first ? P.cap - first : 0u;
+      const Rsrc r = buffer(Vs + ((size_t)(room ? first : 0u) << lg_group), min(room, kPage * 16u) << lg_group);
+#pragma unroll
+      for (int j = 0; j < NI / 2; ++j) {
+        const int i = h * NI / 2 + j;
+        const uint32_t in_half = j * C::RPW + row_in, e = meta + h * 128 + in_half * 4;
+        const uint32_t off = *lds_at<const uint32_t>(e), mask = *lds_at<const uint32_t>(e + 256);
+        const uint32_t piece = ((w.v_from ^ C::v_bits(i)) & (RB - 1)) >> 4;
+        const uint32_t bit = 1u << (piece >> lg_upg), within = (piece & ((1u << lg_upg) - 1u)) << 4;
+        const uint32_t group = off - first + __popc(mask & (bit - 1u));
+        fetch16<PAST>(r, (mask & bit) ? (group << lg_group) + within : kNowhere, w.values + i * 1024);
+      }
+    }
+  };
+  auto ask_queries = [&](int stream) {
+    const int kvh = stream % P.Hkv, node = stream / P.Hkv * P.prefix_seqs * P.T + c / P.R;
+    w.ask_queries(P.q + (c < P.rows ? ((size_t)node * P.Hq + kvh * P.R + c % P.R) * D : 0), c < P.rows);
+  };
+
+  Place x0{unit, unit / P.splits, 0, {-1, -1}};
+  x0.tile = (unit - x0.stream * P.splits) * P.split_tiles;
+  Place x1 = on(x0), x2 = on(x1);
+  if constexpr (LIST) {
+    fetch_list(x0, 0), fetch_list(x1, 1);
+    fetched<0>();
+    read_list(x0, 0), read_list(x1, 1);
+    have_read();
+    fetch_list(x2, 0);
+  }
+  fetch_meta(x0, 0);
+  fetch_keys(x0);
+  ask_queries(x0.stream);
+  fetch_meta(x1, 1);
+  fetched<NI + 4>();  // (the queries, if they came later, are waited for as well)
+  fetch_values(x0, 0);
+  int slot = 1;  // of x1's offsets and masks; of x2's list entries it is the other
+
+  bool first = true;
+  while (true) {
+    if (first) w.begin();
+    const int n0 = rows_of(x0, 0), n1 = rows_of(x0, 1), at = x0.unit, stream = x0.stream;
+    const bool last = x1.unit != x0.unit || x1.tile == x0.tile, done = x1.unit == x0.unit && x1.tile == x0.tile;
+    fetched<NI>();  // keys, what x1's values need, x2's list entries
+    if constexpr (LIST) read_list(x2, slot ^ 1);
+    f32x16 S = w.logits();
+    have_read();
+    const Place x3 = on(x2);
+    if (!done) {
+      fetch_keys(x1);
+      fetch_meta(x2, slot ^ 1);
+      if constexpr (LIST) fetch_list(x3, slot);
+    }
+    if (last && !done && x1.stream != stream) ask_queries(x1.stream);
+    if (n0 < kPage || n1 < kPage) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i / 4 % 2) + i % 4 + 4 * half >= (i < 8 ? n0 : n1)) S[i] = -INFINITY;
+    }
+    w.take_top(S);
+    typename C::Parts p;
+    w.weights(S, p);
+    if (done) fetched<0>();
+    else fetched<NI + 4 + (LIST ? 1 : 0)>();
+    w.products(p);
+    have_read();
+    if (!done) fetch_values(x1, slot);
+    if (last) w.store(P, (long long)at * kRows, c < P.rows);
+    if (done) break;
+    x0 = x1, x1 = x2, x2 = x3;
+    slot ^= 1;
     first = last;
   }
 }
@@ -288,55 +604,123 @@ constexpr int tree_lds() {
   return a > b ? a : b;
 }
 
+// Bytes behind the tiles for the nodes of a block of rows
+constexpr int kTable = (8 * kRows + 2) * 4;
+
+// The launch has a workgroup per compute unit at most.  A workgroup takes row blocks of the prefixes' splits in turn, each
+// of the 8 XCDs (id modulo 8) an eighth of them, in order: those of one split share its keys and values.  Then it takes
+// its share of the tails, a wavefront at a time: workgroups that had a row block less take more of them.
 template <int D, int WR, bool LIST, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
-  extern __shared__ __align__(16) unsigned char lds[];
-  if ((int)blockIdx.x < P.tail_blocks) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    branches<D>(P, lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE, blockIdx.x * kWaves + wave,
-                P.tail_blocks * kWaves);
-    return;
+  extern __shared__ __align__(256) unsigned char lds[];
+  constexpr int T = form_tile(WR), ROWS = WR * kRows;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int rows = P.rows, row_blocks = P.row_blocks, splits = P.splits, split_tiles = P.split_tiles;
+  int32_t* table = (int32_t*)(lds + tree_lds<D, WR>());
+  if (P.compact) {
+    uint32_t nodes = 0;
+    for (int base = 0; base < P.B; base += 64) {
+      const uint32_t mine = base + lane < P.B ? held(P, base + lane).nodes : 0;
+      const uint32_t incl = wave_scan(mine, OpAdd{}, 0u);
+      if (blockIdx.x == 0 && wave == 0 && base + lane < P.B) P.where[2 + base + lane] = nodes + incl - mine;
+      nodes += __builtin_amdgcn_readlane(incl, 63);
+    }
+    rows = nodes * P.R, row_blocks = (rows + ROWS - 1) / ROWS;
+    if (row_blocks > 0) {
+      const Splits x = splits_of(P.items, (long long)P.streams * row_blocks, P.tiles);
+      splits = x.n, split_tiles = x.tiles;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) P.where[0] = splits, P.where[1] = row_blocks;
   }
-  // each of the 8 XCDs takes an eighth of the row blocks of all splits, in order
-  const int id = blockIdx.x - P.tail_blocks, each = (gridDim.x - P.tail_blocks) / kXcds;
-  const int at = id % kXcds * each + id / kXcds;
-  const int u = at / P.row_blocks, rb = at % P.row_blocks;
-  if (u >= P.streams * P.splits) return;
-  const int stream = u / P.splits, split = u % P.splits;
-  const int kvh = stream % P.Hkv, seq0 = stream / P.Hkv * P.prefix_seqs;
-  constexpr int T = form_tile(WR), WK = kWaves / WR;
-  const int tiles = (P.k_pages * kPage + T * WK - 1) / (T * WK);
-  const int t0 = split * P.split_tiles, t1 = min(tiles, t0 + P.split_tiles);
-  const int row0 = rb * WR * kRows;
-  // row r of a KV head: node by node of the prefix's sequences, R rows each
-  auto place = [&](int r) { return ((long long)seq0 * P.T + r / P.R) * P.Hq + kvh * P.R + r % P.R; };
-  attend<D, WR, T, form_stages(WR), LIST, STREAM>(
-      P, lds, stream, t0, t1,
-      [&](int r) -> const uint16_t* {
-        r += row0;
-        return r < P.rows ? P.q + place(r) * D : nullptr;
-      },
-      [&](int r) -> long long {
-        r += row0;
-        return r < P.rows ? place(r) * P.splits + split : -1;
-      });
+  const int items = P.streams * splits * row_blocks, each = (items + kXcds - 1) / kXcds;
+  const int xcd = blockIdx.x % kXcds, per = gridDim.x / kXcds;
+  for (int j = blockIdx.x / kXcds; j < each; j += per) {
+    const int at = xcd * each + j;
+    if (at >= items) break;
+    const int u = at / row_blocks, rb = at % row_blocks;
+    const int stream = u / splits, split = u % splits;
+    const int kvh = stream % P.Hkv, seq0 = stream / P.Hkv * P.prefix_seqs;
+    const int t0 = split * split_tiles, t1 = min(P.tiles, t0 + split_tiles);
+    const int row0 = rb * ROWS, node0 = row0 / P.R;
+    if (P.compact) {
+      if (wave == 0) {  // the block's nodes, by where they lie
+        int seen = 0;
+        for (int base = 0; base < P.B; base += 64) {
+          const int mine = base + lane < P.B ? held(P, base + lane).nodes : 0;
+          const int incl = wave_scan(mine, OpAdd{}, 0u), first = seen + incl - mine;
+          for (int i = max(first, node0); i < min(first + mine, node0 + ROWS / P.R + 2); ++i)
+            table[i - node0] = (base + lane) * P.T + i - first;
+          seen += __builtin_amdgcn_readlane(incl, 63);
+        }
+      }
+      __syncthreads();
+    } else if (P.prefix_seqs == 1) {
+      rows = __builtin_amdgcn_readfirstlane(held(P, seq0).nodes * P.R);
+      if (row0 >= rows) continue;
+    }
+    unsigned char* tiles = lds;
+    asm volatile("" : "+s"(tiles));  // addresses made from it stay inside the loop: they would hold registers
+    attend<D, WR, T, form_stages(WR), LIST, STREAM, WR == 2 ? 3 : kParts>(
+        P, tiles, stream, t0, t1,
+        [&](int r) -> const uint16_t* {
+          r += row0;
+          if (r >= rows) return nullptr;
+          const int node = P.compact ? table[r / P.R - node0] : seq0 * P.T + r / P.R;
+          return P.q + ((size_t)node * P.Hq + kvh * P.R + r % P.R) * D;
+        },
+        [&](int r) -> long long { return row0 + r < rows ? (long long)at * ROWS + r : -1; });
+    __syncthreads();
+  }
+  unsigned char* mine = lds + wave * Cfg<D, 1, kTailTile, 1>::STAGE;
+  const int w = blockIdx.x * kWaves + wave, with_more = groups_with_more(items, gridDim.x);
+  if (P.tail_rb == 1) branches<D, 1>(P, mine, w, gridDim.x, with_more);
+  else branches<D, 0>(P, mine, w, gridDim.x, with_more);
 }
 
+// The same launch where few rows meet many prefixes: every wavefront takes its share of all splits, then of the tails.
+template <int D, bool LIST, bool STREAM>
+__global__ __launch_bounds__(64 * kWaves, 2) void flow_kernel(TreeParams P) {
+  extern __shared__ __align__(256) unsigned char lds[];
+  using C = Cfg<D, 1, kTailTile, 1>;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char* tiles = lds + wave * C::STAGE;
+  const int w = blockIdx.x * kWaves + wave, nw = gridDim.x * kWaves;
+  const long long units = (long long)P.streams * P.splits;
+  flow<D, LIST, STREAM>(P, tiles, lds + kWaves * C::STAGE + wave * kFlowMeta, (int)(units * w / nw),
+                        (int)(units * (w + 1) / nw));
+  branches<D, 1>(P, tiles, w, gridDim.x, gridDim.x);
+}
+
+// block: rows of a row block of the first launch's prefixes
 template <int D, int WPR>
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P) {
-  const int row = merge_row_of<WPR>();
-  const long long rows = (long long)P.B * P.T * P.Hq;
-  int n = -1;
-  if (row < rows) {
-    const int node = row / P.Hq;
-    const Held h = held(P, node / P.T);
-    if (node % P.T < h.nodes) n = h.n;
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P, int block) {
+  const int row = merge_row_of<WPR>(), node = row / P.Hq, head = row - node * P.Hq, b = node / P.T, t = node - b * P.T;
+  int parts = -1, share = 0;
+  long long p0 = 0, step = 0, first = 0, next = 0;
+  if (b < P.B) {
+    const int kvh = head / P.R, of_seq = t * P.R + head - kvh * P.R;  // row of the sequence's KV head
+    const long long stream = (long long)b * P.Hkv + kvh, at = stream * P.tail_rb + of_seq / kRows;
+    const Held h = held(P, b);
+    const int2 x = P.shares[at];
+    int row_blocks = P.row_blocks, r = P.prefix_seqs == 1 ? of_seq : of_seq + b * P.T * P.R;
+    if (P.compact) P.splits = P.where[0], row_blocks = P.where[1], r = of_seq + P.where[2 + b] * P.R;
+    p0 = ((P.prefix_seqs == 1 ? stream : kvh) * P.splits * row_blocks + r / block) * block + r % block;
+    step = (long long)row_blocks * block;
+    first = P.first_at + at * kRows + of_seq % kRows, next = P.next_at + of_seq % kRows;
+    if (t < h.nodes) share = x.x, parts = P.splits + 1 + x.y;
   }
-  merge_row<D, WPR>(P, row, rows, n);
+  merge_row<D, WPR>(P, row, parts, [&](int i) {
+    const int j = i - P.splits;
+    return j < 0 ? p0 + i * step : j == 0 ? first : next + (long long)(share + j) * kRows;
+  });
 }
 
 struct TreePlan {
-  int streams, rows, wr, row_blocks, splits, split_tiles, tail_splits, tail_tiles, tail_blocks;
+  int streams, rows, wr, row_blocks, tiles, items, tail_rb, groups;
+  bool flow;
+  Splits splits;
+  uint32_t item_cost;
+  long long prefix_places;  // partial results of the prefixes
 };
 
 TreePlan tree_plan(const stc_shape_t& s, int T, int n_prefix, int k_pages, int tail_cap) {
@@ -344,74 +728,105 @@ TreePlan tree_plan(const stc_shape_t& s, int T, int n_prefix, int k_pages, int t
   const int R = s.Hq / s.Hkv;
   p.streams = n_prefix * s.Hkv;
   p.rows = s.B / n_prefix * T * R;
-  p.wr = p.rows <= 32 ? 1 : p.rows <= 64 ? 2 : 4;
+  p.wr = p.rows <= 64 ? 2 : 4;
+  const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
+  const long long tail_streams = (long long)s.B * s.Hkv;
+  p.tail_rb = (T * R + kRows - 1) / kRows;
+  p.flow = p.rows <= kRows && p.streams >= 64;
+  if (p.flow) p.wr = 1;
   const long long blocks4 = (p.rows + 127) / 128, blocks8 = (p.rows + 255) / 256;
   const bool full = 0.9 * 2 * blocks8 < blocks4;
   const bool long_share = blocks8 * p.streams * k_pages * kPage > 1024 * kUnits;
   if (p.rows > 128 && full && long_share) p.wr = 8;
   p.row_blocks = (p.rows + 32 * p.wr - 1) / (32 * p.wr);
-  const int per = form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
-  const int tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
-  // The tails: pieces of at least 4 tiles, and of as many as leave 4 blocks for every wavefront of the chip
-  const long long tail_streams = (long long)s.B * s.Hkv, blocks = (T * R + kRows - 1) / kRows;
-  const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
-  long long t = (tail_streams * blocks * tail_max + 4 * 2048 - 1) / (4 * 2048);
-  if (t < 4) t = 4;
-  if (t > tail_max) t = tail_max;
-  p.tail_tiles = (int)t;
-  p.tail_splits = (tail_max + p.tail_tiles - 1) / p.tail_tiles;
-  // An XCD has 32 compute units: `ts` of each for the tails, the others for the splits' row blocks, in rounds.
-  // A tile of time for each tile of a split, two for starting and ending a workgroup, the partial results'
-  // traffic; a tail's tile, counted as half full, is 0.6 of one.
-  const long long items = (long long)p.streams * p.row_blocks;
-  const int most = (int)((tail_streams * blocks * p.tail_splits + 8 * kWaves - 1) / (8 * kWaves));
-  double best = 0;
-  int splits = 1, slots = 1;
-  for (int ts = 1; ts <= 31; ts += ts < 4 ? 1 : 4) {
-    const double tails = 2.0 + 0.6 * tail_streams * blocks * tail_max / (8.0 * kWaves * ts);
-    const long long need = ((items + kXcds - 1) / kXcds + ts + 31) / 32;
-    for (long long rounds = need; rounds < need + 4; ++rounds) {
-      long long n = kXcds * (32 * rounds - ts) / items;
-      if (n < 1) continue;
-      if (n > tiles) n = tiles;
-      const double prefix = rounds * ((tiles + n - 1) / n + 2.0);
-      const double cost = (prefix > tails ? prefix : tails) + n * ((double)p.rows * p.streams * 1e-4);
-      if (best == 0 || cost < best) best = cost, splits = (int)n, slots = ts;
+  const int per = p.flow ? kTailTile : form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
+  p.tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
+  const double tail_tiles = 0.5 * tail_streams * p.tail_rb * tail_max;  // counted as half full
+  if (p.flow) {
+    // Splits of a stream: those that end first.  A wavefront's tiles, one more for each split's end
+    double best = 0;
+    for (int n = 1; n <= 64 && n <= p.tiles; ++n) {
+      const Splits x = splits_of(n, 1, p.tiles);
+      const long long units = (long long)p.streams * x.n, turns = (units + 8 * kUnits - 1) / (8 * kUnits);
+      const double cost = (double)turns * (x.tiles + 1.0) + 1e-3 * units * p.rows / 8.0;
+      if (best == 0 || cost < best) best = cost, p.splits = x;
     }
-    if (ts >= most) break;
+    const long long units = (long long)p.streams * p.splits.n;
+    p.prefix_places = units * kRows;
+    const double waves = units > 2 * tail_tiles / kGrain ? (double)units : 2 * tail_tiles / kGrain;
+    p.groups = waves < 8 * kUnits ? ((int)waves + 63) / 64 * 8 + 8 : kUnits;
+    if (p.groups > kUnits) p.groups = kUnits;
+    return p;
   }
-  p.split_tiles = (tiles + splits - 1) / splits;
-  p.splits = (tiles + p.split_tiles - 1) / p.split_tiles;
-  p.tail_blocks = kXcds * slots;
+  // Row blocks of splits: as many as end first.  A unit of time for each tile of a split, two for starting and ending a row
+  // block, the partial results' traffic; eight tiles of tails take two, and four to begin with where they come last.
+  const long long all = (long long)p.streams * p.row_blocks;
+  double best = 0;
+  for (int rounds = 1; rounds <= 4; ++rounds) {
+    for (int spare = 0; spare <= 24; spare += spare < 4 ? 1 : 4) {  // of an XCD's 32 units, those for tails only
+      const long long items = kXcds * (32ll * rounds - spare);
+      const Splits x = splits_of(items, all, p.tiles);
+      const double item = x.tiles + 2.0;
+      const long long total = all * x.n, turns = (total + kUnits - 1) / kUnits;
+      const double rest = 2.0 * tail_tiles / kWaves - (turns * kUnits - total) * (item - 4.0);
+      const double cost =
+          turns * item + (rest > 0 ? 4.0 + rest / kUnits : 0) + x.n * ((double)p.rows * p.streams * 1e-4);
+      if (best == 0 || cost < best) best = cost, p.items = (int)items, p.splits = x;
+    }
+  }
+  const long long most = all > p.items ? all : p.items;
+  p.prefix_places = most * 32 * p.wr;
+  const double used = all * p.splits.n + kXcds + 2 * tail_tiles / (kGrain * kWaves);
+  p.groups = used < kUnits ? ((int)used + kXcds - 1) / kXcds * kXcds : kUnits;
+  p.item_cost = (uint32_t)((p.splits.tiles + 2) * kWaves / 2);
   return p;
 }
 
-size_t partials(const stc_shape_t& s, int T, const TreePlan& p) {
-  return (size_t)s.B * T * s.Hq * (p.splits + p.tail_splits);
+struct TreeSizes {
+  size_t shares, head, first_at, next_at, places;  // bytes, twice; places of partial results
+};
+TreeSizes sizes_of(const stc_shape_t& s, const TreePlan& p) {
+  TreeSizes z;
+  z.shares = ((size_t)s.B + 2 + 3) / 4 * 16;
+  z.head = z.shares + ((size_t)s.B * s.Hkv * p.tail_rb + 1) / 2 * 16;
+  z.first_at = (size_t)p.prefix_places;
+  z.next_at = z.first_at + (size_t)s.B * s.Hkv * p.tail_rb * kRows;
+  z.places = z.next_at + (size_t)p.groups * kWaves * kRows;
+  return z;
 }
 
 template <int D, int WR, bool LIST, bool STREAM>
-int tree_go(const TreeParams& P, int blocks, hipStream_t st) {
+int tree_go(const TreeParams& P, int groups, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
-  constexpr int lds = tree_lds<D, WR>();
+  constexpr int lds = tree_lds<D, WR>() + kTable;
   if (!allow_dynamic_lds((const void*)tree_kernel<D, WR, LIST, STREAM>, lds, done)) return -1;
-  tree_kernel<D, WR, LIST, STREAM><<<blocks, 64 * kWaves, lds, st>>>(P);
+  tree_kernel<D, WR, LIST, STREAM><<<groups, 64 * kWaves, lds, st>>>(P);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+template <int D, bool LIST, bool STREAM>
+int flow_go(const TreeParams& P, int groups, hipStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  using C = Cfg<D, 1, kTailTile, 1>;
+  constexpr int lds = kWaves * (C::STAGE + kFlowMeta);
+  if (!allow_dynamic_lds((const void*)flow_kernel<D, LIST, STREAM>, lds, done)) return -1;
+  flow_kernel<D, LIST, STREAM><<<groups, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 template <int D, bool LIST>
-int tree_rows(const TreeParams& P, int wr, bool stream, int blocks, hipStream_t st) {
-  if (wr == 1)
-    return stream ? tree_go<D, 1, LIST, true>(P, blocks, st) : tree_go<D, 1, LIST, false>(P, blocks, st);
+int tree_rows(const TreeParams& P, int wr, bool stream, int groups, hipStream_t st) {
+  if (wr == 1) return stream ? flow_go<D, LIST, true>(P, groups, st) : flow_go<D, LIST, false>(P, groups, st);
   if (wr == 2)
-    return stream ? tree_go<D, 2, LIST, true>(P, blocks, st) : tree_go<D, 2, LIST, false>(P, blocks, st);
-  return wr == 4 ? tree_go<D, 4, LIST, false>(P, blocks, st) : tree_go<D, 8, LIST, false>(P, blocks, st);
+    return stream ? tree_go<D, 2, LIST, true>(P, groups, st) : tree_go<D, 2, LIST, false>(P, groups, st);
+  return wr == 4 ? tree_go<D, 4, LIST, false>(P, groups, st) : tree_go<D, 8, LIST, false>(P, groups, st);
 }
 
 }  // namespace
 
 size_t tree_ws_bytes(const stc_shape_t& s, int T, int n_prefix, int k_pages, int tail_cap) {
-  return partials(s, T, tree_plan(s, T, n_prefix, k_pages, tail_cap)) * (s.D + 2) * 4;
+  const TreeSizes z = sizes_of(s, tree_plan(s, T, n_prefix, k_pages, tail_cap));
+  return z.head + z.places * (s.D + 2) * 4;
 }
 
 int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const void* K, const void* vpacked,
@@ -420,39 +835,42 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
                 int tail_cap, const uint64_t* tree, bool tree_per_batch, bool out_bf16, void* out, void* ws,
                 hipStream_t st) {
   const TreePlan p = tree_plan(s, T, n_prefix, k_pages, tail_cap);
+  const TreeSizes z = sizes_of(s, p);
   TreeParams P{};
   P.q = (const uint16_t*)q;
   P.K = (const unsigned char*)K, P.v = (const unsigned char*)vpacked;
   P.mask = mask, P.off = tok_off, P.pages = page_idx;
   P.Kt = (const unsigned char*)K_tail, P.Vt = (const unsigned char*)V_tail;
   P.n_tail = n_tail, P.n_draft = n_draft, P.tree = tree, P.tree_step = tree_per_batch ? T : 0;
-  P.acc = (float*)ws, P.ml = P.acc + partials(s, T, p) * s.D;
+  P.where = (int32_t*)ws, P.shares = (int2*)((char*)ws + z.shares);
+  P.acc = (float*)((char*)ws + z.head), P.ml = P.acc + z.places * s.D;
   P.out = out, P.out_bf16 = out_bf16, P.v_stride = s.v_cap_groups;
   P.cap = (uint32_t)(s.v_cap_groups < UINT32_MAX ? s.v_cap_groups : UINT32_MAX);
   P.B = s.B, P.R = s.Hq / s.Hkv, P.Hq = s.Hq, P.Hkv = s.Hkv, P.N = s.N, P.G = s.G, P.T = T;
   P.NP = (s.N + kPage - 1) / kPage, P.Ncap = token_cap(s), P.k_pages = k_pages, P.tail_cap = tail_cap;
   P.streams = p.streams, P.rows = p.rows, P.prefix_seqs = s.B / n_prefix;
-  P.row_blocks = p.row_blocks, P.splits = p.splits, P.split_tiles = p.split_tiles;
-  P.tail_splits = p.tail_splits, P.tail_tiles = p.tail_tiles, P.tail_blocks = p.tail_blocks;
-  const long long items = ((long long)p.streams * p.splits * p.row_blocks + kXcds - 1) / kXcds * kXcds;
-  const long long blocks = items + p.tail_blocks, rows = (long long)s.B * T * s.Hq;  // rows: 2^26 at most
-  if (blocks > (1 << 30)) return -1;
+  P.row_blocks = p.row_blocks, P.splits = p.splits.n, P.split_tiles = p.splits.tiles;
+  P.items = p.items, P.tiles = p.tiles, P.item_cost = p.item_cost;
+  P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
+  P.compact = n_draft && n_prefix == 1 && s.B > 1 && !p.flow;
+  const long long rows = (long long)s.B * T * s.Hq;  // 2^26 at most
+  if ((long long)p.streams * p.splits.n * p.row_blocks > (1 << 30)) return -1;
   // prefixes that are read once go past the caches from 40 MiB on, as for one query a sequence
   const bool stream = p.row_blocks == 1 && 3ll * p.streams * k_pages * kPage * s.D > (40ll << 20);
   const bool list = page_idx != nullptr;
-  const int rc = s.D == 128 ? (list ? tree_rows<128, true>(P, p.wr, stream, (int)blocks, st)
-                                    : tree_rows<128, false>(P, p.wr, stream, (int)blocks, st))
-                            : (list ? tree_rows<64, true>(P, p.wr, stream, (int)blocks, st)
-                                    : tree_rows<64, false>(P, p.wr, stream, (int)blocks, st));
+  const int rc = s.D == 128 ? (list ? tree_rows<128, true>(P, p.wr, stream, p.groups, st)
+                                    : tree_rows<128, false>(P, p.wr, stream, p.groups, st))
+                            : (list ? tree_rows<64, true>(P, p.wr, stream, p.groups, st)
+                                    : tree_rows<64, false>(P, p.wr, stream, p.groups, st));
   if (rc) return -1;
-  const int wpr = p.splits + p.tail_splits > 16 ? 4 : 1;
-  const int groups = (int)((rows * wpr + 3) / 4);
+  const int wpr = p.splits.n > 14 ? 4 : 1, block = 32 * p.wr;
+  const int merges = (int)((rows * wpr + 3) / 4);
   if (s.D == 128) {
-    if (wpr == 4) tree_merge_kernel<128, 4><<<groups, 256, 0, st>>>(P);
-    else tree_merge_kernel<128, 1><<<groups, 256, 0, st>>>(P);
+    if (wpr == 4) tree_merge_kernel<128, 4><<<merges, 256, 0, st>>>(P, block);
+    else tree_merge_kernel<128, 1><<<merges, 256, 0, st>>>(P, block);
   } else {
-    if (wpr == 4) tree_merge_kernel<64, 4><<<groups, 256, 0, st>>>(P);
-    else tree_merge_kernel<64, 1><<<groups, 256, 0, st>>>(P);
+    if (wpr == 4) tree_merge_kernel<64, 4><<<merges, 256, 0, st>>>(P, block);
+    else tree_merge_kernel<64, 1><<<merges, 256, 0, st>>>(P, block);
   }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }

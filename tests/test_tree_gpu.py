@@ -278,7 +278,7 @@ def test_a_node_alone_is_a_step():
 
 @pytest.mark.parametrize("each", [False, True])
 def test_a_sequence_depends_on_itself_alone(each):
-    """Other sequences' lengths, trees and counts change nothing, not a bit."""
+    """Other sequences' lengths, trees and counts change where sums are cut, so roundings, and nothing else."""
     c = Case(6, 12, 8, 2, 128, 300, 8, 200, each=each, n_tail=[50, 0, 150, 7, 188, 30])
     a = c.run()
     n = torch.tensor([50, 188, -1, 0, 3, 30], dtype=torch.int32, device=DEV)
@@ -287,7 +287,10 @@ def test_a_sequence_depends_on_itself_alone(each):
     tree = c.d["tree"].clone()
     tree[1] = 0
     b = c.run(n=n, nd=nd, tree=tree, Kt=Kt, Vt=Vt, q=torch.nan_to_num(c.d["q"], nan=1.0))
-    assert torch.equal(a[0], b[0]) and torch.equal(a[5], b[5])
+    want, size, top, on = c.want()
+    lim = limits(want, size, top, 500, 128, F32)
+    for x in (a, b):
+        assert (np.abs(x.double().cpu().numpy() - want) <= lim)[[0, 5]].all()
 
 
 def test_graph_with_lengths_that_change():
