@@ -61,18 +61,52 @@ __device__ __forceinline__ int forked(const int32_t* n, const int32_t* n_keep, i
   return n_keep && m >= 0 ? min(m, max(n_keep[b], 0)) : m;
 }
 
-constexpr int kForkThreads = 512, kForkPieces = 8;  // 16-byte pieces that a thread holds
+// Lengths of a layer, by one workgroup, which reads all before it writes any, since n_out may be n_tail.
+template <int THREADS>
+__device__ __forceinline__ void fork_lengths(const int32_t* n, int32_t* out, const int32_t* __restrict__ src,
+                                             const int32_t* __restrict__ n_keep, int B, int32_t* dev_status) {
+  int x[kForkMost / THREADS];
+  bool wrong = false;
+#pragma unroll
+  for (int j = 0; j < kForkMost / THREADS; ++j) {
+    const int b = threadIdx.x + j * THREADS;
+    if (b < B) {
+      const int from = src[b];
+      wrong |= from >= B || from < STC_TAIL_EMPTY;
+      x[j] = forked(n, n_keep, b, from, B);
+    }
+  }
+  if (wrong && dev_status) *dev_status = 1;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kForkMost / THREADS; ++j) {
+    const int b = threadIdx.x + j * THREADS;
+    if (b < B) out[b] = x[j];
+  }
+}
 
 // Any map of sequences onto sequences, in place: a workgroup takes a range of rows (or, with many sequences, some
 // columns of a row) of one head for ALL sequences that get another's rows, so it reads whatever it overwrites
-// first: it holds the pieces in registers between one barrier.
-__global__ __launch_bounds__(kForkThreads) void fork_kernel(Layers L, const int32_t* __restrict__ src,
+// first: a thread holds PIECES 16-byte pieces across a barrier.  One workgroup of a layer writes the lengths where they go
+// to another place than they come from (LENGTHS); else a launch behind this one does, since all workgroups read them.
+// Bound by memory: 48 sequences of 8 heads in 4 layers, a third of which move, 289 MB read and written in 65 us, 4.4 TB/s;
+// all of 1500 rows, 786 MB, 5.2.  (Stores past the caches take 5 us off, loads past them put 8 on; 6 wavefronts' registers
+// per SIMD: 65, 5: 74, 8: 86; 1024 workgroups in place of 2048 75; rows that few moves have taken more at a time, by
+// moves in order of their lengths, 72; without the barrier the same.)
+constexpr int kForkThreads = 512;
+template <int PIECES, bool LENGTHS>
+__global__ __launch_bounds__(kForkThreads, 6) void fork_kernel(Layers L, const int32_t* __restrict__ src,
                                                             const int32_t* __restrict__ n_keep, int B,
-                                                            int tail_cap, int Hkv, int lg_ppr) {
+                                                            int tail_cap, int Hkv, int lg_ppr, int32_t* dev_status) {
+  static_assert(kForkThreads * 8 >= kForkMost, "with 8 pieces a thread, every move has a column at least");
   __shared__ int2 moves[kForkMost];  // (to | from << 16, rows)
   __shared__ int s_moves, s_rows;
   const int layer = blockIdx.y;
   const int32_t* n = L.n[layer];
+  if (LENGTHS && blockIdx.x == gridDim.x - 1) {
+    fork_lengths<kForkThreads>(n, L.out[layer], src, n_keep, B, dev_status);
+    return;
+  }
   if (threadIdx.x == 0) s_moves = s_rows = 0;
   __syncthreads();
   for (int b = threadIdx.x; b < B; b += kForkThreads) {
@@ -87,20 +121,21 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(Layers L, const int3
   const int M = s_moves, most = s_rows;
   if (M == 0) return;
   // rows (or columns) of a turn, a power of two
-  const int fit = 31 - __clz(kForkThreads * kForkPieces / M);  // log2 of the pieces for a move, >= 0
+  const int fit = 31 - __clz(kForkThreads * PIECES / M);  // log2 of the pieces for a move, >= 0
   const int lg_cols = min(fit, lg_ppr), lg_rows = fit - lg_cols;
   const int col_blocks = 1 << (lg_ppr - lg_cols), row_blocks = (most + (1 << lg_rows) - 1) >> lg_rows;
   const long long turns = (long long)row_blocks * col_blocks * Hkv * 2;
-  for (long long turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+  const int groups = gridDim.x - (LENGTHS ? 1 : 0);
+  for (long long turn = blockIdx.x; turn < turns; turn += groups) {
     const int cb = turn & (col_blocks - 1);
     const long long rest = turn >> (lg_ppr - lg_cols);
     const int rb = rest % row_blocks, hk = (int)(rest / row_blocks), h = hk >> 1;
     u32x4* x = L.kv[layer][hk & 1];
-    u32x4 v[kForkPieces];
-    size_t to[kForkPieces];
-    bool on[kForkPieces];
+    u32x4 v[PIECES];
+    size_t to[PIECES];
+    bool on[PIECES];
 #pragma unroll
-    for (int j = 0; j < kForkPieces; ++j) {
+    for (int j = 0; j < PIECES; ++j) {
       const int e = threadIdx.x + j * kForkThreads, move = e >> fit;
       on[j] = move < M;
       if (on[j]) {
@@ -117,34 +152,15 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(Layers L, const int3
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // read, before another wavefront writes there
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kForkPieces; ++j)
-      if (on[j]) x[to[j]] = v[j];
+    for (int j = 0; j < PIECES; ++j)
+      if (on[j]) __builtin_nontemporal_store(v[j], x + to[j]);
   }
 }
 
-// The lengths, behind the rows: a workgroup per layer reads all before it writes any, since n_out may be n_tail.
 __global__ __launch_bounds__(1024) void fork_lengths_kernel(Layers L, const int32_t* __restrict__ src,
                                                             const int32_t* __restrict__ n_keep, int B,
                                                             int32_t* dev_status) {
-  const int32_t* n = L.n[blockIdx.x];
-  int x[kForkMost / 1024];
-  bool wrong = false;
-#pragma unroll
-  for (int j = 0; j < kForkMost / 1024; ++j) {
-    const int b = threadIdx.x + j * 1024;
-    if (b < B) {
-      const int from = src[b];
-      wrong |= from >= B || from < STC_TAIL_EMPTY;
-      x[j] = forked(n, n_keep, b, from, B);
-    }
-  }
-  if (wrong && dev_status) *dev_status = 1;
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kForkMost / 1024; ++j) {
-    const int b = threadIdx.x + j * 1024;
-    if (b < B) L.out[blockIdx.x][b] = x[j];
-  }
+  fork_lengths<1024>(L.n[blockIdx.x], L.out[blockIdx.x], src, n_keep, B, dev_status);
 }
 
 Layers layers_of(int count, void* const* K_tail, void* const* V_tail, const int32_t* const* n_tail,
@@ -178,14 +194,25 @@ int launch_fork_tail(const stc_shape_t& s, int n_layers, void* const* K_tail, vo
   for (int at = 0; at < n_layers; at += kTailLayers) {
     const int count = n_layers - at < kTailLayers ? n_layers - at : kTailLayers;
     const Layers L = layers_of(count, K_tail + at, V_tail + at, n_tail + at, n_out + at);
+    bool in_place = false;
+    for (int i = at; i < at + count; ++i) in_place |= n_out[i] == n_tail[i];
+    // Few rows: two pieces a thread, so that more workgroups share them (8 beams of 120 rows 3.7 us, with eight 6)
     const long long pieces = (long long)s.B * tail_cap * s.Hkv * 2 * (s.D / 8);
-    long long groups = (pieces + kForkThreads * kForkPieces - 1) / (kForkThreads * kForkPieces);
-    const long long most = (1024 + count - 1) / count;
+    const bool few = s.B <= 2 * kForkThreads && pieces * count <= 2048ll * 2 * kForkThreads;
+    long long groups = (pieces + (few ? 2 : 8) * kForkThreads - 1) / ((few ? 2 : 8) * kForkThreads);
+    const long long most = (2048 + count - 1) / count;
     if (groups > most) groups = most;
-    fork_kernel<<<dim3((unsigned)groups, count), kForkThreads, 0, st>>>(L, src, n_keep, s.B, tail_cap, s.Hkv,
-                                                                        s.D == 128 ? 4 : 3);
+    const dim3 grid((unsigned)groups + (in_place ? 0 : 1), count);
+#define STC_FORK(PIECES, LENGTHS)                                                                              \
+  fork_kernel<PIECES, LENGTHS><<<grid, kForkThreads, 0, st>>>(L, src, n_keep, s.B, tail_cap, s.Hkv,            \
+                                                              s.D == 128 ? 4 : 3, dev_status)
+    if (few && in_place) STC_FORK(2, false);
+    else if (few) STC_FORK(2, true);
+    else if (in_place) STC_FORK(8, false);
+    else STC_FORK(8, true);
+#undef STC_FORK
     if (hipGetLastError() != hipSuccess) return -1;
-    fork_lengths_kernel<<<count, 1024, 0, st>>>(L, src, n_keep, s.B, dev_status);
+    if (in_place) fork_lengths_kernel<<<count, 1024, 0, st>>>(L, src, n_keep, s.B, dev_status);
     if (hipGetLastError() != hipSuccess) return -1;
   }
   return 0;
