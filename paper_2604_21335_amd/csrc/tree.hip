@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t tiles_of(const TreeParams& P, const Held& h)
 // `more` had a row block of a prefix more than those behind, whose wavefronts take tiles for its time first; where that
 // is (nearly) all of them, only they have shares.  A share has kGrain tiles at least (but the only one), so that few tiles do
 // not become as many partial results.  In whole numbers, since both launches have to find the same.
-constexpr uint32_t kGrain = 2;
+constexpr uint32_t kGrain = 2, kFine = 512;  // up to so many tiles one is enough
 struct Shares {
   uint32_t all, each, odd;         // tiles; tiles of a share, and what is left over all of them
   int from, waves, count, more;    // wavefronts that have shares: from the first on, so many; shares
@@ -81,7 +81,7 @@ struct Shares {
       if (fewer > 0) lead = item_cost;
     }
     const uint32_t rest = all - lead * fewer;
-    count = max(min((int)min(rest / kGrain, 1u << 20), waves), 1);
+    count = max(min((int)min(all <= kFine ? rest : rest / kGrain, 1u << 20), waves), 1);
     each = rest / count, odd = rest % count;
   }
   __device__ __forceinline__ uint32_t begin(int s) const {
@@ -262,8 +262,9 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
   constexpr int RB = C::RB, NI = C::NI;
   const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
   auto of_lane = [&](int base) { return base + lane < P.B ? held(P, base + lane) : Held{0, 0, 0}; };
-  uint32_t total = 0;
-  for (int base = 0; base < P.B; base += 64) total += wave_reduce(tiles_of(P, of_lane(base)), OpAdd{}, 0u);
+  Held lens = of_lane(0), h{0, 0, 0};
+  uint32_t total = wave_reduce(tiles_of(P, lens), OpAdd{}, 0u);
+  for (int base = 64; base < P.B; base += 64) total += wave_reduce(tiles_of(P, of_lane(base)), OpAdd{}, 0u);
   if (total == 0) return;
   const Shares shares(total, groups, more, P.item_cost);
   const int share = shares.of_wave(w);
@@ -275,13 +276,12 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
   // The sequence that tile `at` belongs to, found again among the lengths (which a caller must not change
   // meanwhile; if it does, the search still ends, and the results are meaningless).
   int base = 0, b = P.B;
-  Held lens = of_lane(0), h{0, 0, 0};
   uint32_t seen = 0, in_b = 0;  // tiles in front of sequence b; of sequence b
   auto lane_held = [&](int j) {
     return Held{__builtin_amdgcn_readlane(lens.n0, j), __builtin_amdgcn_readlane(lens.n, j),
                 __builtin_amdgcn_readlane(lens.nodes, j)};
   };
-  for (; base < P.B; base += 64, lens = of_lane(base)) {
+  while (true) {
     const uint32_t mine = tiles_of(P, lens), incl = wave_scan(mine, OpAdd{}, 0u);
     const uint64_t past = __builtin_amdgcn_ballot_w64(seen + incl > at);
     if (past) {
@@ -293,8 +293,10 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
       break;
     }
     seen += __builtin_amdgcn_readlane(incl, 63);
+    base += 64;
+    if (base >= P.B) return;
+    lens = of_lane(base);
   }
-  if (b >= P.B) return;
   int kvh, rb, t, t_end;
   bool begins;  // a block's tiles begin here
   auto open = [&] {  // the place of tile `at` in sequence b
@@ -433,15 +435,66 @@ __device__ __forceinline__ void branches(const TreeParams& P, unsigned char* lds
   }
 }
 
+constexpr int kFlowMeta = 4 * 256 + 2 * 256;  // bytes of two tiles' offsets and masks, two tiles' list entries
+
+// The sums of a workgroup's wavefronts, of the same P.rows query rows, become the partial result of split `unit`.  Shared
+// memory holds them all at once, in place of the tiles; its rows are padded by a quad.
+template <int D>
+__device__ __forceinline__ void merge_team(const TreeParams& P, unsigned char* lds, const Rows32<D>& x, int unit) {
+  constexpr int MROW = D + 4, BUF = kRows * MROW * 4, Q = D / 4;
+  static_assert(kWaves * (BUF + kRows * 8) <= kWaves * (2 * Rows32<D>::TILE + kFlowMeta), "fits where the tiles were");
+  const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  f32x2* mls = (f32x2*)(lds + kWaves * BUF);
+  const float sum = sum_halves(x.l);
+  __syncthreads();
+  if (c < P.rows) {
+    float* own = (float*)(lds + wave * BUF) + c * MROW;
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        *(f32x4*)(own + cb * 32 + 8 * a + 4 * half) =
+            f32x4{x.O[cb][4 * a], x.O[cb][4 * a + 1], x.O[cb][4 * a + 2], x.O[cb][4 * a + 3]};
+    if (half == 0) mls[wave * kRows + c] = f32x2{x.m, sum};
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < P.rows * Q; i += 64 * kWaves) {
+    const int r = i / Q, quad = i % Q;
+    float top = kNone;
+#pragma unroll
+    for (int g = 0; g < kWaves; ++g) top = fmaxf(top, mls[g * kRows + r][0]);
+    f32x4 o = {0, 0, 0, 0};
+    float l = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kWaves; ++g) {
+      const f32x2 e = mls[g * kRows + r];
+      const float f = __builtin_amdgcn_exp2f(e[0] - top);
+      const f32x4 v = *(const f32x4*)((float*)(lds + g * BUF) + r * MROW + quad * 4);
+      l += f * e[1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += f * v[k];
+    }
+    const size_t place = (size_t)unit * kRows + r;
+    *(f32x4*)(P.acc + place * D + quad * 4) = o;
+    if (quad == 0) *(f32x2*)(P.ml + place * 2) = f32x2{top, l};
+  }
+  __syncthreads();
+}
+
 // Few query rows over many prefixes: P.rows <= 32 rows of each of P.streams streams.  A wavefront takes whole splits of
 // streams, from `unit` to `end`, tile by tile (32 tokens) without a stop between them: masks and offsets are fetched a
 // tile ahead of the values that they lead to, and list entries a tile ahead of those.
-constexpr int kFlowMeta = 4 * 256 + 2 * 256;  // bytes of two tiles' offsets and masks, two tiles' list entries
-template <int D, bool LIST, int PAST>
-__device__ __forceinline__ void flow(const TreeParams& P, unsigned char* lds, unsigned char* meta_lds, int unit, int end) {
+// TEAM: the workgroup's wavefronts take the tiles of one split in turn, and merge what they have.
+template <int D, bool LIST, int PAST, bool TEAM>
+__device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds, int unit, int end) {
   using C = Rows32<D>;
-  constexpr int RB = C::RB, NI = C::NI;
+  constexpr int RB = C::RB, NI = C::NI, STEP = TEAM ? kWaves : 1;
   if (unit >= end) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char* lds = all_lds + wave * 2 * C::TILE;
+  unsigned char* meta_lds = all_lds + kWaves * 2 * C::TILE + wave * kFlowMeta;
+  const int split_tiles = P.split_tiles * STEP, tiles = (P.k_pages + 1) / 2;
   const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
   const uint32_t row_in = lane / C::CH;
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G)), lg_group = lg_upg + 4;
@@ -453,13 +506,14 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* lds, un
   };
   auto on = [&](Place x) {  // the tile behind it; behind the last one, the same again
     const int split = x.unit - x.stream * P.splits;
-    if (++x.tile >= min(P.tiles, (split + 1) * P.split_tiles)) {
-      if (x.unit + 1 < end) {
+    x.tile += STEP;
+    if (x.tile >= min(tiles, (split + 1) * split_tiles)) {
+      if (!TEAM && x.unit + 1 < end) {
         ++x.unit;
         x.stream = x.unit / P.splits;
-        x.tile = (x.unit - x.stream * P.splits) * P.split_tiles;
+        x.tile = (x.unit - x.stream * P.splits) * split_tiles;
       } else {
-        --x.tile;
+        x.tile -= STEP;
       }
     }
     return x;
@@ -541,7 +595,13 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* lds, un
   };
 
   Place x0{unit, unit / P.splits, 0, {-1, -1}};
-  x0.tile = (unit - x0.stream * P.splits) * P.split_tiles;
+  x0.tile = (unit - x0.stream * P.splits) * split_tiles + (TEAM ? wave : 0);
+  const bool some = !TEAM || x0.tile < min(tiles, (unit - x0.stream * P.splits + 1) * split_tiles);
+  if (!some) {
+    w.begin();
+    merge_team<D>(P, all_lds, w, unit);
+    return;
+  }
   Place x1 = on(x0), x2 = on(x1);
   if constexpr (LIST) {
     fetch_list(x0, 0), fetch_list(x1, 1);
@@ -587,12 +647,13 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* lds, un
     w.products(p);
     have_read();
     if (!done) fetch_values(x1, slot);
-    if (last) w.store(P, (long long)at * kRows, c < P.rows);
+    if (!TEAM && last) w.store(P, (long long)at * kRows, c < P.rows);
     if (done) break;
     x0 = x1, x1 = x2, x2 = x3;
     slot ^= 1;
     first = last;
   }
+  if constexpr (TEAM) merge_team<D>(P, all_lds, w, unit);
 }
 
 constexpr int form_tile(int wr) { return wr == 8 ? 64 : 32; }
@@ -677,18 +738,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
   else branches<D, 0>(P, mine, w, gridDim.x, with_more);
 }
 
-// The same launch where few rows meet many prefixes: every wavefront takes its share of all splits, then of the tails.
-template <int D, bool LIST, bool STREAM>
+// The same launch for up to 32 rows.  With many prefixes every wavefront takes its share of all splits, else (TEAM) every
+// workgroup a split, then they take their shares of the tails.
+template <int D, bool LIST, bool STREAM, bool TEAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void flow_kernel(TreeParams P) {
   extern __shared__ __align__(256) unsigned char lds[];
-  using C = Cfg<D, 1, kTailTile, 1>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned char* tiles = lds + wave * C::STAGE;
   const int w = blockIdx.x * kWaves + wave, nw = gridDim.x * kWaves;
-  const long long units = (long long)P.streams * P.splits;
-  flow<D, LIST, STREAM>(P, tiles, lds + kWaves * C::STAGE + wave * kFlowMeta, (int)(units * w / nw),
-                        (int)(units * (w + 1) / nw));
-  branches<D, 1>(P, tiles, w, gridDim.x, gridDim.x);
+  unsigned char* mine = lds + wave * 2 * Rows32<D>::TILE;
+  if constexpr (TEAM) {
+    const int items = P.streams * P.splits, each = (items + kXcds - 1) / kXcds, per = gridDim.x / kXcds;
+    for (int j = blockIdx.x / kXcds; j < each; j += per) {
+      const int at = blockIdx.x % kXcds * each + j;
+      flow<D, LIST, STREAM, true>(P, lds, at, items);
+    }
+    branches<D, 1>(P, mine, w, gridDim.x, groups_with_more(items, gridDim.x));
+  } else {
+    const long long units = (long long)P.streams * P.splits;
+    flow<D, LIST, STREAM, false>(P, lds, (int)(units * w / nw), (int)(units * (w + 1) / nw));
+    branches<D, 1>(P, mine, w, gridDim.x, gridDim.x);
+  }
 }
 
 // block: rows of a row block of the first launch's prefixes
@@ -728,12 +797,11 @@ TreePlan tree_plan(const stc_shape_t& s, int T, int n_prefix, int k_pages, int t
   const int R = s.Hq / s.Hkv;
   p.streams = n_prefix * s.Hkv;
   p.rows = s.B / n_prefix * T * R;
-  p.wr = p.rows <= 64 ? 2 : 4;
+  p.wr = p.rows <= kRows ? 1 : p.rows <= 64 ? 2 : 4;
   const int tail_max = (tail_cap + kTailTile - 1) / kTailTile;
   const long long tail_streams = (long long)s.B * s.Hkv;
   p.tail_rb = (T * R + kRows - 1) / kRows;
   p.flow = p.rows <= kRows && p.streams >= 64;
-  if (p.flow) p.wr = 1;
   const long long blocks4 = (p.rows + 127) / 128, blocks8 = (p.rows + 255) / 256;
   const bool full = 0.9 * 2 * blocks8 < blocks4;
   const bool long_share = blocks8 * p.streams * k_pages * kPage > 1024 * kUnits;
@@ -804,22 +872,24 @@ int tree_go(const TreeParams& P, int groups, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-template <int D, bool LIST, bool STREAM>
+template <int D, bool LIST, bool STREAM, bool TEAM>
 int flow_go(const TreeParams& P, int groups, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
-  using C = Cfg<D, 1, kTailTile, 1>;
-  constexpr int lds = kWaves * (C::STAGE + kFlowMeta);
-  if (!allow_dynamic_lds((const void*)flow_kernel<D, LIST, STREAM>, lds, done)) return -1;
-  flow_kernel<D, LIST, STREAM><<<groups, 64 * kWaves, lds, st>>>(P);
+  constexpr int lds = kWaves * (2 * Rows32<D>::TILE + kFlowMeta);
+  if (!allow_dynamic_lds((const void*)flow_kernel<D, LIST, STREAM, TEAM>, lds, done)) return -1;
+  flow_kernel<D, LIST, STREAM, TEAM><<<groups, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 template <int D, bool LIST>
-int tree_rows(const TreeParams& P, int wr, bool stream, int groups, hipStream_t st) {
-  if (wr == 1) return stream ? flow_go<D, LIST, true>(P, groups, st) : flow_go<D, LIST, false>(P, groups, st);
-  if (wr == 2)
-    return stream ? tree_go<D, 2, LIST, true>(P, groups, st) : tree_go<D, 2, LIST, false>(P, groups, st);
-  return wr == 4 ? tree_go<D, 4, LIST, false>(P, groups, st) : tree_go<D, 8, LIST, false>(P, groups, st);
+int tree_rows(const TreeParams& P, const TreePlan& p, bool stream, hipStream_t st) {
+  if (p.wr == 1 && p.flow)
+    return stream ? flow_go<D, LIST, true, false>(P, p.groups, st) : flow_go<D, LIST, false, false>(P, p.groups, st);
+  if (p.wr == 1)
+    return stream ? flow_go<D, LIST, true, true>(P, p.groups, st) : flow_go<D, LIST, false, true>(P, p.groups, st);
+  if (p.wr == 2)
+    return stream ? tree_go<D, 2, LIST, true>(P, p.groups, st) : tree_go<D, 2, LIST, false>(P, p.groups, st);
+  return p.wr == 4 ? tree_go<D, 4, LIST, false>(P, p.groups, st) : tree_go<D, 8, LIST, false>(P, p.groups, st);
 }
 
 }  // namespace
@@ -852,16 +922,16 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
   P.row_blocks = p.row_blocks, P.splits = p.splits.n, P.split_tiles = p.splits.tiles;
   P.items = p.items, P.tiles = p.tiles, P.item_cost = p.item_cost;
   P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
-  P.compact = n_draft && n_prefix == 1 && s.B > 1 && !p.flow;
+  P.compact = n_draft && n_prefix == 1 && s.B > 1 && p.wr > 1;
   const long long rows = (long long)s.B * T * s.Hq;  // 2^26 at most
   if ((long long)p.streams * p.splits.n * p.row_blocks > (1 << 30)) return -1;
   // prefixes that are read once go past the caches from 40 MiB on, as for one query a sequence
   const bool stream = p.row_blocks == 1 && 3ll * p.streams * k_pages * kPage * s.D > (40ll << 20);
   const bool list = page_idx != nullptr;
-  const int rc = s.D == 128 ? (list ? tree_rows<128, true>(P, p.wr, stream, p.groups, st)
-                                    : tree_rows<128, false>(P, p.wr, stream, p.groups, st))
-                            : (list ? tree_rows<64, true>(P, p.wr, stream, p.groups, st)
-                                    : tree_rows<64, false>(P, p.wr, stream, p.groups, st));
+  const int rc = s.D == 128 ? (list ? tree_rows<128, true>(P, p, stream, st)
+                                    : tree_rows<128, false>(P, p, stream, st))
+                            : (list ? tree_rows<64, true>(P, p, stream, st)
+                                    : tree_rows<64, false>(P, p, stream, st));
   if (rc) return -1;
   const int wpr = p.splits.n > 14 ? 4 : 1, block = 32 * p.wr;
   const int merges = (int)((rows * wpr + 3) / 4);
