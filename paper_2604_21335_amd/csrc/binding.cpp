@@ -117,11 +117,13 @@ class Args {
   }
 
   // The next argument stands for the number of layers' tensors: a list or tuple of them, of at least one.
+  // (They stay where this object is, which outlives the call.)
   struct Many {
     static constexpr int kMost = 1024;
     void* p[kMost];
     int n;
   };
+  Many tails[4];
   template <class... T>
   void many(Many& m, const char* name, int64_t numel, T... types) {
     PyObject* o = next();
@@ -436,29 +438,34 @@ STC_PY(decode_attention_tree, 18,
   auto ws = a.ws(); auto nws = a.bytes(); auto st = a.stream();
   return [=] { return stc_decode_attention_tree(&s, T, P, q, K, v, mask, off, idx, k, Kt, Vt, n, nd, cap, tree.p, tree.per_batch, type, out, ws, nws, st); };)
 
-// The tails of all layers: K_tails, V_tails, n_tails, n_outs (None: the lengths advance in place)
+// The tails of all layers: K_tails, V_tails, n_tails, n_outs
 struct LayerTails {
-  Args::Many K, V, n, out;
+  int n;
+  void **K, **V;
+  const int32_t* const* len;
+  int32_t* const* out;
 };
-static void layer_tails(Args& a, LayerTails& t, const stc_shape_t& s, int cap) {
+static LayerTails layer_tails(Args& a, const stc_shape_t& s, int cap) {
   const int64_t rows = (int64_t)s.B * s.Hkv * cap * s.D;
-  a.many(t.K, "K_tails", rows, kBf16); a.many(t.V, "V_tails", rows, kBf16);
-  a.many(t.n, "n_tails", s.B, at::kInt); a.many(t.out, "n_outs", s.B, at::kInt);
-  a.need(t.V.n == t.K.n && t.n.n == t.K.n && t.out.n == t.K.n, "K_tails, V_tails, n_tails, n_outs", "must be as many");
+  auto& t = a.tails;
+  a.many(t[0], "K_tails", rows, kBf16); a.many(t[1], "V_tails", rows, kBf16);
+  a.many(t[2], "n_tails", s.B, at::kInt); a.many(t[3], "n_outs", s.B, at::kInt);
+  a.need(t[1].n == t[0].n && t[2].n == t[0].n && t[3].n == t[0].n, "K_tails, V_tails, n_tails, n_outs", "must be as many");
+  return {t[0].n, t[0].p, t[1].p, (const int32_t* const*)t[2].p, (int32_t* const*)t[3].p};
 }
 
 STC_PY(accept_tail, 8,
   auto s = *a.shape(); a.one_device(); auto T = a.integer(); auto cap = a.integer();
-  LayerTails t; layer_tails(a, t, s, cap);
+  auto t = layer_tails(a, s, cap);
   auto keep = (const uint64_t*)a.sized("keep", s.B, at::kLong, at::kUInt64); auto st = a.stream();
-  return [=] { return stc_accept_tail(&s, T, t.K.n, t.K.p, t.V.p, (const int32_t* const*)t.n.p, (int32_t* const*)t.out.p, cap, keep, st); };)
+  return [=] { return stc_accept_tail(&s, T, t.n, t.K, t.V, t.len, t.out, cap, keep, st); };)
 
 STC_PY(fork_tail, 9,
   auto s = *a.shape(); a.one_device(); auto cap = a.integer();
-  LayerTails t; layer_tails(a, t, s, cap);
+  auto t = layer_tails(a, s, cap);
   auto src = (const int32_t*)a.sized("src", s.B, at::kInt); auto keep = (const int32_t*)a.sized("n_keep", s.B, at::kInt);
   auto status = (int32_t*)a.sized("dev_status", 1, at::kInt); auto st = a.stream();
-  return [=] { return stc_fork_tail(&s, t.K.n, t.K.p, t.V.p, (const int32_t* const*)t.n.p, (int32_t* const*)t.out.p, cap, src, keep, status, st); };)
+  return [=] { return stc_fork_tail(&s, t.n, t.K, t.V, t.len, t.out, cap, src, keep, status, st); };)
 
 PyMethodDef methods[] = {
 #define STC_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
