@@ -64,8 +64,8 @@ __device__ __forceinline__ uint32_t tiles_of(const TreeParams& P, const Held& h)
 
 // How the tiles are shared out: share s, of one wavefront, begins at begin(s), and none is empty.  Workgroups in front of
 // `more` had a row block of a prefix more than those behind, whose wavefronts take tiles for its time first; where that
-// is (nearly) all of them, only they have shares.  A share has kGrain tiles at least (but the only one), so that few tiles do
-// not become as many partial results.  In whole numbers, since both launches have to find the same.
+// is (nearly) all of them, only they have shares.  Else a share has kGrain tiles at least, or is the only one, so that few
+// tiles do not become as many partial results.  In whole numbers, since both launches have to find the same.
 constexpr uint32_t kGrain = 2, kFine = 512;  // up to so many tiles one is enough
 struct Shares {
   uint32_t all, each, odd;         // tiles; tiles of a share, and what is left over all of them
@@ -74,14 +74,14 @@ struct Shares {
   __device__ __forceinline__ Shares(uint32_t all, int groups, int more, uint32_t item_cost)
       : all(all), more(more), lead(0) {
     const uint32_t total = groups * kWaves, fewer = groups - more;
-    if (fewer > 0 && all / fewer < item_cost + kGrain * total / fewer) {
+    if (fewer > 0 && all < (uint64_t)item_cost * fewer + total) {
       from = more * kWaves, waves = fewer * kWaves;
     } else {
       from = 0, waves = total;
       if (fewer > 0) lead = item_cost;
     }
     const uint32_t rest = all - lead * fewer;
-    count = max(min((int)min(all <= kFine ? rest : rest / kGrain, 1u << 20), waves), 1);
+    count = max(min((int)min(lead || all <= kFine ? rest : rest / kGrain, 1u << 20), waves), 1);
     each = rest / count, odd = rest % count;
   }
   __device__ __forceinline__ uint32_t begin(int s) const {
