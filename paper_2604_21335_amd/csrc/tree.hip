@@ -23,6 +23,7 @@ struct TreeParams : SharedParams {
   int items, tiles;       // row blocks of all splits that the launch has room for; tiles of a prefix
   int compact;            // only nodes that are there are rows
   uint32_t item_cost;     // time of a row block of a split, in tiles of the tails
+  int flow_shares;        // wavefronts that share the tiles of all prefixes, 0 where splits do
   int tail_rb;            // row blocks of a sequence and KV head, at most
   long long first_at, next_at;  // places of the tails' partial results: of fragments that begin a tail, of others
 };
@@ -63,9 +64,9 @@ __device__ __forceinline__ uint32_t tiles_of(const TreeParams& P, const Held& h)
 }
 
 // How the tiles are shared out: share s, of one wavefront, begins at begin(s), and none is empty.  Workgroups in front of
-// `more` had a row block of a prefix more than those behind, whose wavefronts take tiles for its time first; where that
-// is (nearly) all of them, only they have shares.  Else a share has kGrain tiles at least, or is the only one, so that few
-// tiles do not become as many partial results.  In whole numbers, since both launches have to find the same.
+// `more` had a row block of a prefix more than those behind, whose wavefronts take tiles for its time first; where those
+// end all of them sooner than everyone would, only they have shares.  Else a share has kGrain tiles at least, or is the only
+// one, so that few tiles do not become as many partial results.  In whole numbers, since both launches have to find the same.
 constexpr uint32_t kGrain = 2, kFine = 512;  // up to so many tiles one is enough
 struct Shares {
   uint32_t all, each, odd;         // tiles; tiles of a share, and what is left over all of them
@@ -74,11 +75,10 @@ struct Shares {
   __device__ __forceinline__ Shares(uint32_t all, int groups, int more, uint32_t item_cost)
       : all(all), more(more), lead(0) {
     const uint32_t total = groups * kWaves, fewer = groups - more;
-    if (fewer > 0 && all < (uint64_t)item_cost * fewer + total) {
-      from = more * kWaves, waves = fewer * kWaves;
-    } else {
-      from = 0, waves = total;
-      if (fewer > 0) lead = item_cost;
+    from = 0, waves = total;
+    if (fewer > 0) {
+      if (all / fewer <= item_cost + all / groups) from = more * kWaves, waves = fewer * kWaves;
+      else if (all >= (uint64_t)item_cost * fewer + total) lead = item_cost;
     }
     const uint32_t rest = all - lead * fewer;
     count = max(min((int)min(lead || all <= kFine ? rest : rest / kGrain, 1u << 20), waves), 1);
@@ -106,6 +106,12 @@ struct Shares {
     while (begin(s + 1) <= tile) ++s;
     return s;
   }
+};
+// The tiles of all streams, shared out evenly: share s begins at begin(s), tile `at` is of share of(at).
+struct FlowShares {
+  int tiles, count;
+  __device__ __forceinline__ int begin(int s) const { return (int)((int64_t)tiles * s / count); }
+  __device__ __forceinline__ int of(int at) const { return (int)((((int64_t)at + 1) * count - 1) / tiles); }
 };
 __device__ __forceinline__ int groups_with_more(int items, int groups) {
   const int each = (items + kXcds - 1) / kXcds, per = groups / kXcds, turns = (each + per - 1) / per;
@@ -482,39 +488,39 @@ __device__ __forceinline__ void merge_team(const TreeParams& P, unsigned char* l
   __syncthreads();
 }
 
-// Few query rows over many prefixes: P.rows <= 32 rows of each of P.streams streams.  A wavefront takes whole splits of
-// streams, from `unit` to `end`, tile by tile (32 tokens) without a stop between them: masks and offsets are fetched a
-// tile ahead of the values that they lead to, and list entries a tile ahead of those.
-// TEAM: the workgroup's wavefronts take the tiles of one split in turn, and merge what they have.
+// Few query rows, P.rows <= 32 of each of P.streams streams, tile by tile (32 tokens): masks and offsets are fetched a tile
+// ahead of the values that they lead to, and list entries a tile ahead of those.  TEAM: the wavefronts of a workgroup take
+// the tiles of a split (number `from`) in turn, and merge what they have.  Else the wavefront takes the tiles from `from` to
+// `end` of all streams, as they follow each other: where its first one is not a stream's first, the stream's partial
+// result is the wavefront's one `next` (number `share`), others are the streams' `first`.
 template <int D, bool LIST, int PAST, bool TEAM>
-__device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds, int unit, int end) {
+__device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds, int from, int end, int share) {
   using C = Rows32<D>;
   constexpr int RB = C::RB, NI = C::NI, STEP = TEAM ? kWaves : 1;
-  if (unit >= end) return;
+  if (from >= end) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char* lds = all_lds + wave * 2 * C::TILE;
   unsigned char* meta_lds = all_lds + kWaves * 2 * C::TILE + wave * kFlowMeta;
-  const int split_tiles = P.split_tiles * STEP, tiles = (P.k_pages + 1) / 2;
+  const int tiles = (P.k_pages + 1) / 2;  // of a stream
   const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
   const uint32_t row_in = lane / C::CH;
   const int lg_upg = 31 - __clz(C::CH) - (31 - __clz(P.G)), lg_group = lg_upg + 4;
   const int tokens = min(P.N, P.k_pages * kPage);
 
-  // A tile: of which split, and its two pages (with a list), -1 where there is none
+  // A tile, and its two pages (with a list), -1 where there is none
   struct Place {
-    int unit, stream, tile, page[2];
+    int stream, tile, page[2];
   };
+  const int stream0 = TEAM ? from / P.splits : from / tiles;
+  const int tile0 = TEAM ? (from - stream0 * P.splits) * P.split_tiles * STEP : from - stream0 * tiles;
+  const int stream1 = TEAM ? stream0 : (end - 1) / tiles;  // the last stream, and where its tiles end
+  const int tile1 = TEAM ? min(tiles, tile0 + P.split_tiles * STEP) : end - stream1 * tiles;
   auto on = [&](Place x) {  // the tile behind it; behind the last one, the same again
-    const int split = x.unit - x.stream * P.splits;
     x.tile += STEP;
-    if (x.tile >= min(tiles, (split + 1) * split_tiles)) {
-      if (!TEAM && x.unit + 1 < end) {
-        ++x.unit;
-        x.stream = x.unit / P.splits;
-        x.tile = (x.unit - x.stream * P.splits) * split_tiles;
-      } else {
-        x.tile -= STEP;
-      }
+    if (x.stream == stream1) {
+      if (x.tile >= tile1) x.tile -= STEP;
+    } else if (x.tile == tiles) {
+      ++x.stream, x.tile = 0;
     }
     return x;
   };
@@ -594,12 +600,10 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds
     w.ask_queries(P.q + (c < P.rows ? ((size_t)node * P.Hq + kvh * P.R + c % P.R) * D : 0), c < P.rows);
   };
 
-  Place x0{unit, unit / P.splits, 0, {-1, -1}};
-  x0.tile = (unit - x0.stream * P.splits) * split_tiles + (TEAM ? wave : 0);
-  const bool some = !TEAM || x0.tile < min(tiles, (unit - x0.stream * P.splits + 1) * split_tiles);
-  if (!some) {
+  Place x0{stream0, tile0 + (TEAM ? wave : 0), {-1, -1}};
+  if (TEAM && x0.tile >= tile1) {
     w.begin();
-    merge_team<D>(P, all_lds, w, unit);
+    merge_team<D>(P, all_lds, w, from);
     return;
   }
   Place x1 = on(x0), x2 = on(x1);
@@ -618,11 +622,11 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds
   fetch_values(x0, 0);
   int slot = 1;  // of x1's offsets and masks; of x2's list entries it is the other
 
-  bool first = true;
+  bool first = true, whole = tile0 == 0;  // the stream's first tile was the wavefront's
   while (true) {
     if (first) w.begin();
-    const int n0 = rows_of(x0, 0), n1 = rows_of(x0, 1), at = x0.unit, stream = x0.stream;
-    const bool last = x1.unit != x0.unit || x1.tile == x0.tile, done = x1.unit == x0.unit && x1.tile == x0.tile;
+    const int n0 = rows_of(x0, 0), n1 = rows_of(x0, 1), stream = x0.stream;
+    const bool done = x1.stream == stream && x1.tile == x0.tile, last = done || x1.stream != stream;
     fetched<NI>();  // keys, what x1's values need, x2's list entries
     if constexpr (LIST) read_list(x2, slot ^ 1);
     f32x16 S = w.logits();
@@ -647,13 +651,16 @@ __device__ __forceinline__ void flow(const TreeParams& P, unsigned char* all_lds
     w.products(p);
     have_read();
     if (!done) fetch_values(x1, slot);
-    if (!TEAM && last) w.store(P, (long long)at * kRows, c < P.rows);
+    if (!TEAM && last) {
+      w.store(P, (long long)(whole ? stream : P.streams + share) * kRows, c < P.rows);
+      whole = true;
+    }
     if (done) break;
     x0 = x1, x1 = x2, x2 = x3;
     slot ^= 1;
     first = last;
   }
-  if constexpr (TEAM) merge_team<D>(P, all_lds, w, unit);
+  if constexpr (TEAM) merge_team<D>(P, all_lds, w, from);
 }
 
 constexpr int form_tile(int wr) { return wr == 8 ? 64 : 32; }
@@ -671,7 +678,7 @@ constexpr int kTable = (8 * kRows + 2) * 4;
 // The launch has a workgroup per compute unit at most.  A workgroup takes row blocks of the prefixes' splits in turn, each
 // of the 8 XCDs (id modulo 8) an eighth of them, in order: those of one split share its keys and values.  Then it takes
 // its share of the tails, a wavefront at a time: workgroups that had a row block less take more of them.
-template <int D, int WR, bool LIST, bool STREAM>
+template <int D, int WR, bool LIST, bool STREAM, int PARTS>
 __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
   extern __shared__ __align__(256) unsigned char lds[];
   constexpr int T = form_tile(WR), ROWS = WR * kRows;
@@ -721,7 +728,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
     }
     unsigned char* tiles = lds;
     asm volatile("" : "+s"(tiles));  // addresses made from it stay inside the loop: they would hold registers
-    attend<D, WR, T, form_stages(WR), LIST, STREAM, WR == 2 ? 3 : kParts>(
+    attend<D, WR, T, form_stages(WR), LIST, STREAM, PARTS>(
         P, tiles, stream, t0, t1,
         [&](int r) -> const uint16_t* {
           r += row0;
@@ -738,33 +745,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
   else branches<D, 0>(P, mine, w, gridDim.x, with_more);
 }
 
-// The same launch for up to 32 rows.  With many prefixes every wavefront takes its share of all splits, else (TEAM) every
-// workgroup a split, then they take their shares of the tails.
+// The same launch for up to 32 rows.  With few prefixes (TEAM) every workgroup takes splits in turn; with many the first
+// P.flow_shares wavefronts share all their tiles.  Then come the tails.
 template <int D, bool LIST, bool STREAM, bool TEAM>
 __global__ __launch_bounds__(64 * kWaves, 2) void flow_kernel(TreeParams P) {
   extern __shared__ __align__(256) unsigned char lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = blockIdx.x * kWaves + wave, nw = gridDim.x * kWaves;
-  unsigned char* mine = lds + wave * 2 * Rows32<D>::TILE;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x * kWaves + wave;
+  int more;
   if constexpr (TEAM) {
     const int items = P.streams * P.splits, each = (items + kXcds - 1) / kXcds, per = gridDim.x / kXcds;
-    for (int j = blockIdx.x / kXcds; j < each; j += per) {
-      const int at = blockIdx.x % kXcds * each + j;
-      flow<D, LIST, STREAM, true>(P, lds, at, items);
-    }
-    branches<D, 1>(P, mine, w, gridDim.x, groups_with_more(items, gridDim.x));
+    for (int j = blockIdx.x / kXcds; j < each; j += per)
+      flow<D, LIST, STREAM, true>(P, lds, blockIdx.x % kXcds * each + j, items, 0);
+    more = groups_with_more(items, gridDim.x);
   } else {
-    const long long units = (long long)P.streams * P.splits;
-    flow<D, LIST, STREAM, false>(P, lds, (int)(units * w / nw), (int)(units * (w + 1) / nw));
-    branches<D, 1>(P, mine, w, gridDim.x, gridDim.x);
+    const int tiles = P.streams * ((P.k_pages + 1) / 2);
+    if (w < P.flow_shares) {
+      const FlowShares f{tiles, P.flow_shares};
+      flow<D, LIST, STREAM, false>(P, lds, f.begin(w), f.begin(w + 1), w);
+    }
+    more = (P.flow_shares + kWaves - 1) / kWaves;
   }
+  branches<D, 1>(P, lds + wave * 2 * Rows32<D>::TILE, w, gridDim.x, more);
 }
 
 // block: rows of a row block of the first launch's prefixes
-template <int D, int WPR>
+template <int D, int WPR, bool FLOW>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P, int block) {
   const int row = merge_row_of<WPR>(), node = row / P.Hq, head = row - node * P.Hq, b = node / P.T, t = node - b * P.T;
-  int parts = -1, share = 0;
+  int parts = -1, share = 0, flow_share = 0;
   long long p0 = 0, step = 0, first = 0, next = 0;
   if (b < P.B) {
     const int kvh = head / P.R, of_seq = t * P.R + head - kvh * P.R;  // row of the sequence's KV head
@@ -776,17 +784,26 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P, int block
     p0 = ((P.prefix_seqs == 1 ? stream : kvh) * P.splits * row_blocks + r / block) * block + r % block;
     step = (long long)row_blocks * block;
     first = P.first_at + at * kRows + of_seq % kRows, next = P.next_at + of_seq % kRows;
+    if constexpr (FLOW) {  // the prefix's parts lie like the tail's
+      const int tiles = (P.k_pages + 1) / 2, s = (int)(P.prefix_seqs == 1 ? stream : kvh);
+      const FlowShares f{P.streams * tiles, P.flow_shares};
+      flow_share = f.of(s * tiles), P.splits = f.of(s * tiles + tiles - 1) - flow_share + 1;
+      p0 = (long long)s * kRows + r, step = kRows;
+    }
     if (t < h.nodes) share = x.x, parts = P.splits + 1 + x.y;
   }
   merge_row<D, WPR>(P, row, parts, [&](int i) {
     const int j = i - P.splits;
-    return j < 0 ? p0 + i * step : j == 0 ? first : next + (long long)(share + j) * kRows;
+    if (j >= 0) return j == 0 ? first : next + (long long)(share + j) * kRows;
+    if (FLOW && i > 0) return p0 % kRows + (long long)(P.streams + flow_share + i) * kRows;
+    return p0 + i * step;
   });
 }
 
 struct TreePlan {
   int streams, rows, wr, row_blocks, tiles, items, tail_rb, groups;
   bool flow;
+  int flow_shares;
   Splits splits;
   uint32_t item_cost;
   long long prefix_places;  // partial results of the prefixes
@@ -809,21 +826,21 @@ TreePlan tree_plan(const stc_shape_t& s, int T, int n_prefix, int k_pages, int t
   p.row_blocks = (p.rows + 32 * p.wr - 1) / (32 * p.wr);
   const int per = p.flow ? kTailTile : form_tile(p.wr) * (kWaves / p.wr);  // tokens of a tile of all groups
   p.tiles = (int)(((long long)k_pages * kPage + per - 1) / per);
-  const double tail_tiles = 0.5 * tail_streams * p.tail_rb * tail_max;  // counted as half full
+  const double tail_tiles = tail_streams * p.tail_rb * (0.5 * tail_cap / kTailTile + 0.75);  // counted as half full
   if (p.flow) {
-    // Splits of a stream: those that end first.  A wavefront's tiles, one more for each split's end
-    double best = 0;
-    for (int n = 1; n <= 64 && n <= p.tiles; ++n) {
-      const Splits x = splits_of(n, 1, p.tiles);
-      const long long units = (long long)p.streams * x.n, turns = (units + 8 * kUnits - 1) / (8 * kUnits);
-      const double cost = (double)turns * (x.tiles + 1.0) + 1e-3 * units * p.rows / 8.0;
-      if (best == 0 || cost < best) best = cost, p.splits = x;
-    }
-    const long long units = (long long)p.streams * p.splits.n;
-    p.prefix_places = units * kRows;
-    const double waves = units > 2 * tail_tiles / kGrain ? (double)units : 2 * tail_tiles / kGrain;
-    p.groups = waves < 8 * kUnits ? ((int)waves + 63) / 64 * 8 + 8 : kUnits;
-    if (p.groups > kUnits) p.groups = kUnits;
+    // Workgroups for prefixes and for tails by the number of tiles, two of them a wavefront at least.  A tail's tile counts
+    // twice: its values are whole, and a block has few.  (8 x 32 heads, 64 pages, tails of 200: 34 us with 1632
+    // wavefronts for the prefixes, 39 with 1808, 37 with all, tails behind; 4096 tokens 95, 83, 85, and 79 with 1920.)
+    const double prefix_tiles = (double)p.streams * p.tiles, all = prefix_tiles + 2.0 * tail_tiles;
+    const double groups = all / (2.0 * kWaves);
+    p.groups = groups < kUnits ? ((int)groups + kXcds) / kXcds * kXcds : kUnits;
+    const int most = p.groups * kWaves;
+    double shares = most * prefix_tiles / all;
+    if (shares > prefix_tiles / 2) shares = prefix_tiles / 2;
+    p.flow_shares = shares < kWaves ? kWaves : (int)shares / kWaves * kWaves;
+    p.prefix_places = (long long)(p.streams + p.flow_shares) * kRows;
+    p.splits = {1, p.tiles};
+    p.item_cost = (uint32_t)(prefix_tiles / p.flow_shares + 2.0) * kWaves;
     return p;
   }
   // Row blocks of splits: as many as end first.  A unit of time for each tile of a split, two for starting and ending a row
@@ -863,12 +880,12 @@ TreeSizes sizes_of(const stc_shape_t& s, const TreePlan& p) {
   return z;
 }
 
-template <int D, int WR, bool LIST, bool STREAM>
+template <int D, int WR, bool LIST, bool STREAM, int PARTS>
 int tree_go(const TreeParams& P, int groups, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
   constexpr int lds = tree_lds<D, WR>() + kTable;
-  if (!allow_dynamic_lds((const void*)tree_kernel<D, WR, LIST, STREAM>, lds, done)) return -1;
-  tree_kernel<D, WR, LIST, STREAM><<<groups, 64 * kWaves, lds, st>>>(P);
+  if (!allow_dynamic_lds((const void*)tree_kernel<D, WR, LIST, STREAM, PARTS>, lds, done)) return -1;
+  tree_kernel<D, WR, LIST, STREAM, PARTS><<<groups, 64 * kWaves, lds, st>>>(P);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -888,8 +905,14 @@ int tree_rows(const TreeParams& P, const TreePlan& p, bool stream, hipStream_t s
   if (p.wr == 1)
     return stream ? flow_go<D, LIST, true, true>(P, p.groups, st) : flow_go<D, LIST, false, true>(P, p.groups, st);
   if (p.wr == 2)
-    return stream ? tree_go<D, 2, LIST, true>(P, p.groups, st) : tree_go<D, 2, LIST, false>(P, p.groups, st);
-  return p.wr == 4 ? tree_go<D, 4, LIST, false>(P, p.groups, st) : tree_go<D, 8, LIST, false>(P, p.groups, st);
+    return stream ? tree_go<D, 2, LIST, true, 3>(P, p.groups, st) : tree_go<D, 2, LIST, false, 3>(P, p.groups, st);
+  // Two parts of a weight leave 2^-16 of it, and a float output off by 1.5 .. 2 10^-6 of its norm; that is what sums of
+  // 32768 floats leave anyway, but twice what those of some thousand do.  Three cost 5 .. 14 % here (448 rows over 32768
+  // tokens 69 -> 79 us), so they are for float outputs of fewer tokens.
+  const bool three = !P.out_bf16 && P.k_pages * kPage <= 16384;
+  if (p.wr == 4)
+    return three ? tree_go<D, 4, LIST, false, 3>(P, p.groups, st) : tree_go<D, 4, LIST, false, 2>(P, p.groups, st);
+  return three ? tree_go<D, 8, LIST, false, 3>(P, p.groups, st) : tree_go<D, 8, LIST, false, 2>(P, p.groups, st);
 }
 
 }  // namespace
@@ -921,7 +944,7 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
   P.streams = p.streams, P.rows = p.rows, P.prefix_seqs = s.B / n_prefix;
   P.row_blocks = p.row_blocks, P.splits = p.splits.n, P.split_tiles = p.splits.tiles;
   P.items = p.items, P.tiles = p.tiles, P.item_cost = p.item_cost;
-  P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
+  P.flow_shares = p.flow_shares, P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
   P.compact = n_draft && n_prefix == 1 && s.B > 1 && p.wr > 1;
   const long long rows = (long long)s.B * T * s.Hq;  // 2^26 at most
   if ((long long)p.streams * p.splits.n * p.row_blocks > (1 << 30)) return -1;
@@ -935,13 +958,16 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
   if (rc) return -1;
   const int wpr = p.splits.n > 14 ? 4 : 1, block = 32 * p.wr;
   const int merges = (int)((rows * wpr + 3) / 4);
+#define STC_MERGE(DD)                                                                  \
+  if (p.flow) tree_merge_kernel<DD, 1, true><<<merges, 256, 0, st>>>(P, block);        \
+  else if (wpr == 4) tree_merge_kernel<DD, 4, false><<<merges, 256, 0, st>>>(P, block); \
+  else tree_merge_kernel<DD, 1, false><<<merges, 256, 0, st>>>(P, block)
   if (s.D == 128) {
-    if (wpr == 4) tree_merge_kernel<128, 4><<<merges, 256, 0, st>>>(P, block);
-    else tree_merge_kernel<128, 1><<<merges, 256, 0, st>>>(P, block);
+    STC_MERGE(128);
   } else {
-    if (wpr == 4) tree_merge_kernel<64, 4><<<merges, 256, 0, st>>>(P, block);
-    else tree_merge_kernel<64, 1><<<merges, 256, 0, st>>>(P, block);
+    STC_MERGE(64);
   }
+#undef STC_MERGE
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
