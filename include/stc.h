@@ -478,12 +478,15 @@ int stc_rotary_append_tree(const stc_shape_t *shape, int T, const void *q, const
  *            sizes are not limited to 4 GiB
  *   page_idx [n_prefix, Hkv, k_pages] int32, in, or NULL, as for stc_decode_attention_shared
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16, in;  tail_cap >= 1
- *   n_tail   [B] int32, in (counted as tail_cap if larger);  n_draft  [B] int32, in, may be NULL
+ *   n_tail   [B] int32, in (counted as tail_cap if larger);  n_draft  [B] int32, in, may be NULL.  Neither may change
+ *            while the call works
  *   tree     [B, T] (tree_per_batch 1) or [T] (0) uint64, in, may be NULL
  *   out      [B, T, Hq, D], out, float or bf16; rows of padding and of nodes that a sequence does not have are left
  *            as they are; a query without any token gets zeros
  *   ws       stc_tree_workspace_bytes(...) bytes; calls whose work overlaps in time need one each
- * Magnitudes count as for stc_decode_attention_shared.  Keys and values of a node that are infinite or NaN reach the
+ * Magnitudes count as for stc_decode_attention_shared.  Weights are carried as bf16 parts: two (2^-16) for the prefix
+ * where a KV head has more than 64 query rows of one prefix, three (2^-24) where it has fewer, where the output is float and
+ * up to 16384 tokens are listed, and for the tails.  Keys and values of a node that are infinite or NaN reach the
  * queries that see it and no others.  Where the sums of a query are cut depends on the lengths and nodes of the whole
  * batch: other sequences change its results by roundings, and by nothing else.
  */

@@ -2,9 +2,20 @@
 // compressed prefix (one for the batch, or one for each sequence) and the sequence's own tail, and of the
 // nodes, whose keys and values stand behind the tail, those that their bits name.
 //
-// In the prefix there is nothing to mask: the T * R rows of a KV head (those of all sequences, where they
-// share the prefix) are columns of dense products with its tokens, by shared_block.hpp.  The tails have
-// workgroups of their own in the same launch, and a second launch merges a row's partial results.
+// In the prefix there is nothing to mask: the T * R rows of a KV head (those of all sequences, where they share the
+// prefix) are columns of dense products with its tokens.  Beyond 32 rows shared_block.hpp takes them, by 2, 4 or 8
+// wavefronts to a tile; up to 32 a wavefront fetches tiles of its own (flow).  Where sequences share the prefix, only
+// nodes that are there are rows, and splits are cut for as many as there are.  The tails and the nodes (branches) are
+// 32 rows and 32 tokens at a time; a node's bits hide logits in the tiles that hold nodes.  All of it is one launch of a
+// workgroup per compute unit, whose wavefronts take their shares of the tails, cut evenly by tiles, behind their shares of
+// the prefix.  A second launch merges a row's partial results.
+//
+// What bounds it (D = 128, half of the value groups kept; both launches):
+//   448 rows of one sequence over 32768 tokens, 4 KV heads: 69 us; matrix products with weights in two parts, 730 TFLOP/s of
+//     executed ones, in 35 turns of 1.8 us; the merge of 15 splits takes 6.
+//   16 sequences of 16 nodes, half of them there, over the same: 114 us, 900 TFLOP/s (all there: 180); the chip's power.
+//   8 x 32 heads over 64 listed pages each and tails of up to 200: 34 us, memory, 118 MB; first loads and the merge.
+//   64 x 32 heads over 208 tokens, tails of up to 1000: 116 us; the tails at 6.2 TB/s, then units that end late, merge 8.
 #include "shared_block.hpp"
 
 namespace stc {
@@ -23,6 +34,7 @@ struct TreeParams : SharedParams {
   int items, tiles;       // row blocks of all splits that the launch has room for; tiles of a prefix
   int compact;            // only nodes that are there are rows
   uint32_t item_cost;     // time of a row block of a split, in tiles of the tails
+  int waves;              // of the first launch
   int flow_shares;        // wavefronts that share the tiles of all prefixes, 0 where splits do
   int tail_rb;            // row blocks of a sequence and KV head, at most
   long long first_at, next_at;  // places of the tails' partial results: of fragments that begin a tail, of others
@@ -733,7 +745,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
         [&](int r) -> const uint16_t* {
           r += row0;
           if (r >= rows) return nullptr;
-          const int node = P.compact ? table[r / P.R - node0] : seq0 * P.T + r / P.R;
+          // (clamped: where a caller changes lengths meanwhile, the table need not have been written)
+          const int node = P.compact ? min(max(table[r / P.R - node0], 0), P.B * P.T - 1) : seq0 * P.T + r / P.R;
           return P.q + ((size_t)node * P.Hq + kvh * P.R + r % P.R) * D;
         },
         [&](int r) -> long long { return row0 + r < rows ? (long long)at * ROWS + r : -1; });
@@ -790,7 +803,11 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P, int block
       flow_share = f.of(s * tiles), P.splits = f.of(s * tiles + tiles - 1) - flow_share + 1;
       p0 = (long long)s * kRows + r, step = kRows;
     }
-    if (t < h.nodes) share = x.x, parts = P.splits + 1 + x.y;
+    // (clamped: where a caller changes lengths meanwhile, what stands there need not have been written)
+    if (t < h.nodes) {
+      share = min(max(x.x, 0), P.waves - 1);
+      parts = P.splits + 1 + min(max(x.y, 0), P.waves - 1 - share);
+    }
   }
   merge_row<D, WPR>(P, row, parts, [&](int i) {
     const int j = i - P.splits;
@@ -944,7 +961,7 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
   P.streams = p.streams, P.rows = p.rows, P.prefix_seqs = s.B / n_prefix;
   P.row_blocks = p.row_blocks, P.splits = p.splits.n, P.split_tiles = p.splits.tiles;
   P.items = p.items, P.tiles = p.tiles, P.item_cost = p.item_cost;
-  P.flow_shares = p.flow_shares, P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
+  P.waves = p.groups * kWaves, P.flow_shares = p.flow_shares, P.tail_rb = p.tail_rb, P.first_at = z.first_at, P.next_at = z.next_at;
   P.compact = n_draft && n_prefix == 1 && s.B > 1 && p.wr > 1;
   const long long rows = (long long)s.B * T * s.Hq;  // 2^26 at most
   if ((long long)p.streams * p.splits.n * p.row_blocks > (1 << 30)) return -1;

@@ -146,6 +146,44 @@ def test_many_prefixes():
         Case(B, T, 16, 8, 64, 40, 4, 30, seed=B, each=True, n_tail=[0, 3, -1, 28, 9]).check()
 
 
+# more sequences than a wavefront has lanes, some of them padding or without nodes; tails that are more than the prefix,
+# so that workgroups with and without a share of the prefix take different shares of them
+@pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,N,cap", [(70, 5, 4, 2, 64, 90, 40), (130, 3, 6, 1, 128, 33, 70), (300, 2, 8, 8, 64, 40, 120),
+                                                (65, 17, 3, 3, 64, 300, 200), (200, 1, 16, 1, 128, 600, 9)])
+def test_many_sequences(B, T, Hq, Hkv, D, N, cap, each):
+    n = [cap - T, 0, 5, -1, cap // 2, 31, 1, 33]
+    Case(B, T, Hq, Hkv, D, N, 8, cap, seed=B, each=each, n_tail=np.minimum(n, cap - T),
+         n_draft=[T, 0, max(T - 1, 1), 1, T]).check(BF16 if each else F32)
+    Case(B, T, Hq, Hkv, D, N, 8, cap, seed=B + 1, each=each).check()
+
+
+# up to 32 rows of 64 and more streams: their tiles in one row, cut anywhere
+@pytest.mark.parametrize("D,G", [(128, 8), (64, 4)])
+@pytest.mark.parametrize("N", [1, 17, 31, 33, 100, 500, 1300])
+def test_few_rows_of_many_prefixes(N, D, G):
+    c = Case(16, 4, 32, 4, D, N, G, 90, seed=N, each=True, n_cap=N + 7)
+    c.check()
+    NP = (N + 15) // 16
+    rng = np.random.default_rng(N)
+    for k in {1, min(2, NP), min(5, NP), NP}:
+        pages = np.stack([[rng.permutation(NP)[:k] for _ in range(4)] for _ in range(16)])
+        pages[3, 1, -1], pages[7, 0, 0] = NP, -1
+        c.check(BF16, pages=pages)
+    c.check(k=(NP + 1) // 2)
+
+
+@pytest.mark.parametrize("N,T,R,Hkv,D", [(9000, 64, 16, 8, 64), (17000, 40, 4, 1, 64), (17000, 64, 16, 4, 64)])
+def test_float_outputs_of_many_rows(N, T, R, Hkv, D):
+    """Two and three parts of a weight, 4 and 8 wavefronts to a tile."""
+    Case(1, T, R * Hkv, Hkv, D, N, 8, T + 9, seed=N + R).check()
+
+
+@pytest.mark.parametrize("Hkv,T,R", [(64, 2, 4), (70, 5, 1)])
+def test_few_rows_of_one_prefix_with_many_heads(Hkv, T, R):
+    Case(3, T, R * Hkv, Hkv, 64, 400, 4, 50, seed=Hkv, n_draft=[T, 1, T]).check()
+
+
 # lengths of the prefix that end inside a page, a tile, a group's turn, a split
 @pytest.mark.parametrize("B,T,Hq,Hkv,D,each", [(2, 3, 4, 2, 128, True), (3, 6, 10, 2, 64, False), (4, 20, 5, 1, 128, False)])
 @pytest.mark.parametrize("N", [1, 15, 16, 17, 31, 32, 33, 63, 65, 127, 129, 255, 257, 1000, 4001])
