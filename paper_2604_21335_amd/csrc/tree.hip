@@ -740,7 +740,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeParams P) {
     }
     unsigned char* tiles = lds;
     asm volatile("" : "+s"(tiles));  // addresses made from it stay inside the loop: they would hold registers
-    attend<D, WR, T, form_stages(WR), LIST, STREAM, PARTS>(
+    attend<D, WR, T, form_stages(WR), LIST, STREAM, PARTS, true>(
         P, tiles, stream, t0, t1,
         [&](int r) -> const uint16_t* {
           r += row0;
