@@ -645,8 +645,9 @@ __device__ __forceinline__ void merge_row(const SharedParams& P, int row, int to
     join(__shfl_xor(top, s), __shfl_xor(sum, s), o1);
   }
   if constexpr (WPR > 1) {
-    __shared__ f32x4 s_o[4][L];
-    __shared__ f32x2 s_e[4];
+    constexpr int WAVES = WPR > 4 ? WPR : 4;  // of the workgroup
+    __shared__ f32x4 s_o[WAVES][L];
+    __shared__ f32x2 s_e[WAVES];
     if (lane < L) s_o[wave][lane] = o;
     if (lane == 0) s_e[wave] = f32x2{top, sum};
     __syncthreads();
@@ -664,10 +665,10 @@ __device__ __forceinline__ void merge_row(const SharedParams& P, int row, int to
   }
 }
 
-// The row of the output that a wavefront of a workgroup of 4 merges.
-template <int WPR>
+// The row of the output that a wavefront of a workgroup merges.
+template <int WPR, int WAVES = 4>
 __device__ __forceinline__ int merge_row_of() {
-  return blockIdx.x * (4 / WPR) + (threadIdx.x >> 6) / WPR;
+  return blockIdx.x * (WAVES / WPR) + (threadIdx.x >> 6) / WPR;
 }
 
 }  // namespace shared

@@ -16,6 +16,8 @@
 //   16 sequences of 16 nodes, half of them there, over the same: 114 us, 900 TFLOP/s (all there: 180); the chip's power.
 //   8 x 32 heads over 64 listed pages each and tails of up to 200: 34 us, memory, 118 MB; first loads and the merge.
 //   64 x 32 heads over 208 tokens, tails of up to 1000: 116 us; the tails at 6.2 TB/s, then units that end late, merge 8.
+#include <algorithm>
+
 #include "shared_block.hpp"
 
 namespace stc {
@@ -783,8 +785,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void flow_kernel(TreeParams P) {
 
 // block: rows of a row block of the first launch's prefixes
 template <int D, int WPR, bool FLOW>
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeParams P, int block) {
-  const int row = merge_row_of<WPR>(), node = row / P.Hq, head = row - node * P.Hq, b = node / P.T, t = node - b * P.T;
+__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void tree_merge_kernel(TreeParams P, int block) {
+  const int row = merge_row_of<WPR, WPR == 1 ? 4 : WPR>(), node = row / P.Hq, head = row - node * P.Hq;
+  const int b = node / P.T, t = node - b * P.T;
   int parts = -1, share = 0, flow_share = 0;
   long long p0 = 0, step = 0, first = 0, next = 0;
   if (b < P.B) {
@@ -973,16 +976,25 @@ int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const 
                             : (list ? tree_rows<64, true>(P, p, stream, st)
                                     : tree_rows<64, false>(P, p, stream, st));
   if (rc) return -1;
-  const int wpr = p.splits.n > 14 ? 4 : 1, block = 32 * p.wr;
-  const int merges = (int)((rows * wpr + 3) / 4);
-#define STC_MERGE(DD)                                                                  \
-  if (p.flow) tree_merge_kernel<DD, 1, true><<<merges, 256, 0, st>>>(P, block);        \
-  else if (wpr == 4) tree_merge_kernel<DD, 4, false><<<merges, 256, 0, st>>>(P, block); \
-  else tree_merge_kernel<DD, 1, false><<<merges, 256, 0, st>>>(P, block)
-  if (s.D == 128) {
-    STC_MERGE(128);
+  // 4 wavefronts for a row of many partial results, 16 where long tails of few sequences may be cut into hundreds: one row
+  // with a tail of 200000 tokens takes 46 us, 171 with one wavefront.  With up to 64 pieces (1024 rows, 40000 tokens) four
+  // wavefronts take 77 us, as one does.
+  const long long tails = (long long)s.B * s.Hkv * p.tail_rb;
+  const long long cuts = std::min<long long>(P.waves / tails, tail_cap / kTailTile / (int)kGrain);
+  const int wpr = cuts > 256 ? 16 : p.splits.n > 14 || cuts > 32 ? 4 : 1, block = 32 * p.wr;
+  const int merges = wpr == 1 ? (int)((rows + 3) / 4) : (int)rows;
+#define STC_MERGE(DD, FLOW)                                                                       \
+  if (wpr == 16) tree_merge_kernel<DD, 16, FLOW><<<merges, 1024, 0, st>>>(P, block);              \
+  else if (wpr == 4) tree_merge_kernel<DD, 4, FLOW><<<merges, 256, 0, st>>>(P, block);            \
+  else tree_merge_kernel<DD, 1, FLOW><<<merges, 256, 0, st>>>(P, block)
+  if (s.D == 128 && p.flow) {
+    STC_MERGE(128, true);
+  } else if (s.D == 128) {
+    STC_MERGE(128, false);
+  } else if (p.flow) {
+    STC_MERGE(64, true);
   } else {
-    STC_MERGE(64);
+    STC_MERGE(64, false);
   }
 #undef STC_MERGE
   return hipGetLastError() == hipSuccess ? 0 : -1;

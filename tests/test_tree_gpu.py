@@ -206,6 +206,16 @@ def test_long_tails(each):
     Case(1, 64, 16, 1, 64, 33, 8, 9000, seed=2, each=each, n_tail=[8930]).check()
 
 
+# tails in hundreds of pieces, of which few or none hold tokens in some of the calls
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,T,Hq,Hkv,n", [(1, 1, 1, 1, [39000]), (2, 3, 4, 2, [39990, 33]), (3, 2, 5, 1, [-1, 0, 20001]),
+                                          (1, 9, 16, 2, [64]), (4, 1, 2, 1, [39999, 39998, 40000, 7])])
+def test_tails_in_hundreds_of_pieces(B, T, Hq, Hkv, n, D):
+    cap = 40000
+    Case(B, T, Hq, Hkv, D, 33, 8, cap, seed=B + T, n_tail=n, n_draft=[T, max(T - 1, 0), 1, T]).check()
+    Case(B, T, Hq, Hkv, D, 70, 4, cap, seed=B + T + 1, each=True, n_tail=n).check(BF16)
+
+
 @pytest.mark.parametrize("T", [1, 5, 64])
 def test_a_chain_and_one_tree_for_all(T):
     c = Case(4, T, 6, 2, 128, 90, 8, 150, tree=None, seed=T)
