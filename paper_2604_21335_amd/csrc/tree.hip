@@ -136,29 +136,28 @@ __device__ __forceinline__ int groups_with_more(int items, int groups) {
 // What lies behind the buffer's end comes as zeros.  Written out, and waited for by number (they end in order, and with
 // them whatever else was asked for), since the compiler would wait for all of them in front of any read of shared memory.
 // (The buffer's base is the wavefront's, whatever the compiler made of it.)
+// A memory instruction must stand five wait states behind a vector instruction that writes a scalar register which it
+// reads, and nothing in the hardware sees to that.  Bases come out of vector instructions (the first lane's value, or a
+// register put aside in a lane), and the compiler does not look at what is written out: the move to m0 is one of the five,
+// the other four follow it.  (m0 itself needs one.)
 __device__ __forceinline__ Rsrc buffer(const void* base, uint32_t bytes) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
   return rsrc((const void*)(uintptr_t)u, bytes);
 }
+#define STC_FETCH(WHAT, HOW)                                                                              \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\t" WHAT " %1, %2, 0 offen" HOW " lds" ::"s"(to), "v"(at), "s"(r) \
+               : "memory", "m0")
 template <int PAST>
 __device__ __forceinline__ void fetch16(Rsrc r, uint32_t at, uint32_t to) {
-  if constexpr (PAST)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(at), "s"(r)
-                 : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
-                 : "memory");
+  if constexpr (PAST) STC_FETCH("buffer_load_dwordx4", " nt");
+  else STC_FETCH("buffer_load_dwordx4", "");
 }
-__device__ __forceinline__ void fetch4(Rsrc r, uint32_t at, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
-               : "memory");
-}
-__device__ __forceinline__ void fetch2(Rsrc r, uint32_t at, uint32_t to) {  // (four bytes there, the upper two zero)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ushort %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(r)
-               : "memory");
-}
+__device__ __forceinline__ void fetch4(Rsrc r, uint32_t at, uint32_t to) { STC_FETCH("buffer_load_dword", ""); }
+// (four bytes there, the upper two zero)
+__device__ __forceinline__ void fetch2(Rsrc r, uint32_t at, uint32_t to) { STC_FETCH("buffer_load_ushort", ""); }
+#undef STC_FETCH
 template <int N>
 __device__ __forceinline__ void fetched() {  // all but the last N
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
