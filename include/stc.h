@@ -509,7 +509,7 @@ int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, con
  *   n_tail    [B] int32 each, in (negative: padding, left alone); layers may share one where n_out is another
  *   n_out     [B] int32 each, out: the new lengths; n_out[i] may be n_tail[i] itself, but must not overlap another
  *             layer's n_tail or n_out
- *   keep      [B] uint64, in, the same for all layers
+ *   keep      [B] uint64, in, the same for all layers; must not overlap an n_out
  */
 int stc_accept_tail(const stc_shape_t *shape, int T, int n_layers, void *const *K_tail, void *const *V_tail,
                     const int32_t *const *n_tail, int32_t *const *n_out, int tail_cap, const uint64_t *keep,

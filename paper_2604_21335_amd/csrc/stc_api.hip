@@ -590,19 +590,20 @@ bool apart(uintptr_t* at, int n, size_t bytes) {
   return true;
 }
 
-// Whether an array of so many bytes overlaps one of the n sorted ones, other than `own`, which it may be itself.
-bool overlaps(const void* p, size_t bytes, const uintptr_t* at, int n, const void* own = nullptr) {
+// Whether an array of so many bytes overlaps one of the n sorted ones, of `each` bytes, other than `own`, which it may be
+// itself.
+bool overlaps(const void* p, size_t bytes, const uintptr_t* at, int n, size_t each, const void* own = nullptr) {
   const uintptr_t x = (uintptr_t)p;
-  for (const uintptr_t* w = std::lower_bound(at, at + n, x < bytes ? 0 : x - bytes + 1);
+  for (const uintptr_t* w = std::lower_bound(at, at + n, x < each ? 0 : x - each + 1);
        w != at + n && *w < x + bytes; ++w)
     if (*w != (uintptr_t)own || *w != x) return true;
   return false;
 }
 
 // The tails of all layers and their lengths: all there and aligned, and what is written apart from what else is
-// read or written.  `also`: two more arrays of B numbers that are read, or NULL.
+// read or written.  `also`, `also2`: two more arrays that are read, of B numbers of so many bytes, or NULL.
 int layers_status(const stc_shape_t* s, int n_layers, void* const* K, void* const* V, const int32_t* const* n,
-                  int32_t* const* out, int tail_cap, const int32_t* also, const int32_t* also2) {
+                  int32_t* const* out, int tail_cap, const void* also, size_t also_bytes, const void* also2) {
   uintptr_t tails[2 * kMostLayers], written[kMostLayers];
   for (int i = 0; i < n_layers; ++i) {
     if (!K[i] || !V[i] || !n[i] || !out[i]) return STC_ERR_NULL;
@@ -615,8 +616,9 @@ int layers_status(const stc_shape_t* s, int n_layers, void* const* K, void* cons
       !apart(written, n_layers, lengths))
     return STC_ERR_SHAPE;
   for (int i = 0; i < n_layers; ++i)
-    if (overlaps(n[i], lengths, written, n_layers, out[i])) return STC_ERR_SHAPE;
-  if ((also && overlaps(also, lengths, written, n_layers)) || (also2 && overlaps(also2, lengths, written, n_layers)))
+    if (overlaps(n[i], lengths, written, n_layers, lengths, out[i])) return STC_ERR_SHAPE;
+  if ((also && overlaps(also, s->B * also_bytes, written, n_layers, lengths)) ||
+      (also2 && overlaps(also2, lengths, written, n_layers, lengths)))
     return STC_ERR_SHAPE;
   return STC_OK;
 }
@@ -691,7 +693,7 @@ int stc_accept_tail(const stc_shape_t* shape, int T, int n_layers, void* const* 
       tail_cap > (1 << 30))
     return STC_ERR_SHAPE;
   if ((uintptr_t)keep & 7) return STC_ERR_ALIGN;
-  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, nullptr, nullptr);
+  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep, 8, nullptr);
   if (status != STC_OK) return status;
   return stc::launch_accept_tail(*shape, T, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep,
                                  (hipStream_t)stream)
@@ -707,7 +709,7 @@ int stc_fork_tail(const stc_shape_t* shape, int n_layers, void* const* K_tail, v
       tail_cap > (1 << 30))
     return STC_ERR_SHAPE;
   if (((uintptr_t)src & 3) || ((uintptr_t)n_keep & 3) || ((uintptr_t)dev_status & 3)) return STC_ERR_ALIGN;
-  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, src, n_keep);
+  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, src, 4, n_keep);
   if (status != STC_OK) return status;
   return stc::launch_fork_tail(*shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, src, n_keep, dev_status,
                                (hipStream_t)stream)

@@ -129,6 +129,20 @@ def test_accept_and_fork_refuse(call, kw, status):
     assert _tails(call, **kw) == getattr(stc, "STC_ERR_" + status)
 
 
+# the sets of kept nodes are read, of all sequences by every layer, while lengths are written
+@pytest.mark.parametrize("keep", [0x1000, 0x1010, 0x1020, 0x1030, 0xfe0, 0x1000 - 8])
+def test_accept_refuses_kept_sets_where_lengths_are_written(keep):
+    assert _tails("accept", keep=ctypes.c_void_p(keep)) == stc.STC_ERR_SHAPE
+
+
+def test_accept_refuses_kept_sets_where_lengths_of_a_far_layer_are_written():
+    n = [0x1000 + 32 * i for i in range(100)]
+    at = [0x100000 + 0x10000 * i for i in range(200)]
+    for keep in (0x1000 + 32 * 99 + 16, 0x1000 + 32 * 40 - 16):
+        assert _tails("accept", layers=100, K=at[:100], V=at[100:], n=[0x10000] * 100, out=n,
+                      keep=ctypes.c_void_p(keep)) == stc.STC_ERR_SHAPE
+
+
 def test_null_shape():
     lib = stc.load_library()
     assert lib.stc_accept_tail(None, 1, 1, None, None, None, None, 1, None, None) == stc.STC_ERR_NULL
