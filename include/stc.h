@@ -31,7 +31,8 @@
  *   drafted tokens       stc_rotary_append_tree (up to 64 tokens of every sequence, a tree, behind
  *                        its tail), stc_decode_attention_tree (their attention, over one prefix or
  *                        one for each sequence), stc_tree_workspace_bytes, stc_accept_tail (the
- *                        accepted ones stay)
+ *                        accepted ones stay); stc_rotary_append_drafts, stc_accept_drafts (the same,
+ *                        with counts of the nodes that sequences have room for)
  *   tails of a batch     stc_fork_tail (sequences that continue others' tails, or end)
  *   per-query-head form  stc_select_pages_per_head, stc_decode_attention_per_head,
  *                        stc_union_pages + stc_decode_attention_union (shared K/V reads)
@@ -451,7 +452,8 @@ int stc_decode_attention_shared(const stc_shape_t *shape, const void *q, const v
  *   q_out     [B, T, Hq, D] bf16, out: rows of nodes that a sequence has; may be q where q's strides are T*Hq*D and
  *             Hq*D
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16: rows n_tail[b] .. n_tail[b] + n_draft[b] - 1 of b are written.
- *             Where they would pass tail_cap nothing of b is written, and *dev_status becomes 1
+ *             Where they would pass tail_cap nothing of b is written, and *dev_status becomes 1: who goes on with the
+ *             sequence takes stc_rotary_append_drafts, which says so to the calls behind
  *   n_tail    [B] int32, in;  n_draft  [B] int32, in, may be NULL
  *   tree      [B, T] (tree_per_batch 1) or [T] (0) uint64, in, may be NULL; used where pos is NULL
  *   rot_dim   0 (no rotation; turns may be NULL), 16, 32, .. D;  layout without STC_ROTARY_INVERSE
@@ -465,6 +467,20 @@ int stc_rotary_append_tree(const stc_shape_t *shape, int T, const void *q, const
                            const int32_t *n_tail, const int32_t *n_draft, int tail_cap, const uint64_t *tree,
                            int tree_per_batch, int rot_dim, int layout, const double *turns, float amplitude,
                            const int32_t *pos, int32_t pos0, int32_t *dev_status, void *stream);
+
+/*
+ * The same, and what became of it: the attention and the accepted rows behind it do not see which sequences had no room,
+ * and rows behind a tail that this call did not write hold whatever was there.
+ *   n_have    [B] int32, out, may be NULL: the nodes that a sequence has now, n_draft[b] (clamped to 0 .. T; NULL: T), and 0
+ *             of padding and where nothing was written for want of room.  It is the n_draft of stc_decode_attention_tree
+ *             and stc_accept_drafts, which then leave such a sequence as it is.  Must not overlap n_tail or n_draft
+ */
+int stc_rotary_append_drafts(const stc_shape_t *shape, int T, const void *q, const int64_t *q_stride,
+                             const void *k_new, const int64_t *k_stride, const void *v_new,
+                             const int64_t *v_stride, void *q_out, void *K_tail, void *V_tail,
+                             const int32_t *n_tail, const int32_t *n_draft, int tail_cap, const uint64_t *tree,
+                             int tree_per_batch, int rot_dim, int layout, const double *turns, float amplitude,
+                             const int32_t *pos, int32_t pos0, int32_t *n_have, int32_t *dev_status, void *stream);
 
 /*
  * Decode attention of the nodes: every node's query heads attend the tokens of the listed pages of the prefix, rows
@@ -502,7 +518,8 @@ int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, con
  * Accepted nodes stay: of the T rows behind the tail those whose bits are set in keep[b] move together, in order,
  * in place, and the tail grows by their number, in all layers at once.  (An accepted path is the set of its last
  * node: tree[b][last].)  Bits at and above T, and of rows at and above tail_cap, do not count.  The other rows are
- * left as they are, and as what they are: behind the tail.
+ * left as they are, and as what they are: behind the tail.  Which nodes a sequence has, this call is not told: keep must
+ * name none of a sequence that had no room for its nodes (stc_accept_drafts takes the counts).
  *   shape     B, Hkv, D are used (the rest must be valid)
  *   n_layers  1 .. 1024; the arrays below are HOST arrays of n_layers device pointers
  *   K_tail, V_tail  [B, Hkv, tail_cap, D] bf16 each, in/out; no two may overlap
@@ -514,6 +531,14 @@ int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, con
 int stc_accept_tail(const stc_shape_t *shape, int T, int n_layers, void *const *K_tail, void *const *V_tail,
                     const int32_t *const *n_tail, int32_t *const *n_out, int tail_cap, const uint64_t *keep,
                     void *stream);
+
+/*
+ * The same, of the nodes that a sequence has: bits at and above n_draft[b] do not count either.
+ *   n_draft   [B] int32, in, may be NULL: all T.  The n_have of stc_rotary_append_drafts.  Must not overlap an n_out
+ */
+int stc_accept_drafts(const stc_shape_t *shape, int T, int n_layers, void *const *K_tail, void *const *V_tail,
+                      const int32_t *const *n_tail, int32_t *const *n_out, int tail_cap, const uint64_t *keep,
+                      const int32_t *n_draft, void *stream);
 
 /*
  * Sequences that go on with others' tails (beams, samples of one answer, another try from an earlier token), in place

@@ -37,7 +37,7 @@ EXPORTS = ["stc_version", "stc_status_string", "stc_workspace_bytes", "stc_bound
            "stc_decode_step_static", "stc_rotary_turns", "stc_rotary", "stc_rotary_append",
            "stc_shared_workspace_bytes", "stc_decode_attention_shared",
            "stc_rotary_append_tree", "stc_tree_workspace_bytes", "stc_decode_attention_tree",
-           "stc_accept_tail", "stc_fork_tail"]
+           "stc_accept_tail", "stc_fork_tail", "stc_rotary_append_drafts", "stc_accept_drafts"]
 
 
 class StcError(RuntimeError):
@@ -147,6 +147,9 @@ def load_library():
     lib.stc_rotary_append_tree.restype = ci
     lib.stc_rotary_append_tree.argtypes = [shp, ci, vp, strides, vp, strides, vp, strides, vp, vp, vp, vp,
                                            vp, ci, vp, ci, ci, ci, vp, f32, vp, i32, vp, vp]
+    lib.stc_rotary_append_drafts.restype = ci
+    lib.stc_rotary_append_drafts.argtypes = [shp, ci, vp, strides, vp, strides, vp, strides, vp, vp, vp, vp,
+                                             vp, ci, vp, ci, ci, ci, vp, f32, vp, i32, vp, vp, vp]
     lib.stc_tree_workspace_bytes.restype = sz
     lib.stc_tree_workspace_bytes.argtypes = [shp, ci, ci, ci, ci]
     lib.stc_decode_attention_tree.restype = ci
@@ -154,6 +157,8 @@ def load_library():
                                               vp, ci, ci, vp, vp, sz, vp]
     lib.stc_accept_tail.restype = ci
     lib.stc_accept_tail.argtypes = [shp, ci, ci, ptrs, ptrs, ptrs, ptrs, ci, vp, vp]
+    lib.stc_accept_drafts.restype = ci
+    lib.stc_accept_drafts.argtypes = [shp, ci, ci, ptrs, ptrs, ptrs, ptrs, ci, vp, vp, vp]
     lib.stc_fork_tail.restype = ci
     lib.stc_fork_tail.argtypes = [shp, ci, ptrs, ptrs, ptrs, ptrs, ci, vp, vp, vp, vp]
     lib.stc_compact_tokens.restype = ctypes.c_int
@@ -354,14 +359,15 @@ def stc_decode_attention_shared(shape, q, K, vpacked, mask, tok_off, page_idx, k
 
 def stc_rotary_append_tree(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail, tail_cap, turns, rot_dim,
                            layout, tree=None, n_draft=None, amplitude=1.0, pos=None, pos0=0,
-                           dev_status=None):
+                           dev_status=None, n_have=None):
     """T drafted tokens of every sequence, q [B, T, Hq, D], k_new, v_new [B, T, Hkv, D] (slices of one
     projection's output will do): rotated q to q_out, rotated k_new and v_new to rows n_tail[b] .. of sequence
     b's tails, whose lengths stay.  tree [T] or [B, T] int64: the nodes that a node sees, as bits; None: a chain.
-    n_draft [B] int32: nodes that a sequence has; None: T."""
+    n_draft [B] int32: nodes that a sequence has; None: T.  n_have [B] int32, out: nodes that it has now, none where there
+    was no room for all (stc_rotary_append_drafts); the n_draft of the calls below."""
     (_native or _load_native()).rotary_append_tree(shape, q, k_new, v_new, q_out, K_tail, V_tail, n_tail,
                                                    tail_cap, turns, rot_dim, layout, tree, n_draft, amplitude,
-                                                   pos, pos0, dev_status)
+                                                   pos, pos0, n_have, dev_status)
 
 
 def stc_tree_workspace_bytes(shape, T, k_pages, tail_cap, n_prefix=1):
@@ -377,12 +383,12 @@ def stc_decode_attention_tree(shape, q, K, vpacked, mask, tok_off, page_idx, k_p
                                                       n_draft, out, ws)
 
 
-def stc_accept_tail(shape, T, K_tails, V_tails, n_tails, tail_cap, keep, n_outs=None):
+def stc_accept_tail(shape, T, K_tails, V_tails, n_tails, tail_cap, keep, n_outs=None, n_draft=None):
     """Of the T nodes behind sequence b's tail, those whose bits keep[b] (int64) has move together, and the tail
     grows by them, in all layers: K_tails, V_tails, n_tails are lists of the layers' tensors.  n_outs: where the new
-    lengths go; None: n_tails."""
+    lengths go; None: n_tails.  n_draft [B] int32: nodes that a sequence has (stc_accept_drafts); None: T."""
     (_native or _load_native()).accept_tail(shape, T, tail_cap, K_tails, V_tails, n_tails,
-                                            n_tails if n_outs is None else n_outs, keep)
+                                            n_tails if n_outs is None else n_outs, keep, n_draft)
 
 
 def stc_fork_tail(shape, K_tails, V_tails, n_tails, tail_cap, src, n_keep=None, n_outs=None, dev_status=None):
@@ -620,6 +626,8 @@ class SharedPrefix:
         most = max(self.nodes, default=0)
         self._q_tree = torch.zeros(B * most * p.Hq * p.D, dtype=torch.bfloat16, device=dev)
         self._out_tree = torch.zeros(B * most * p.Hq * p.D, dtype=out_dtype, device=dev)
+        # nodes that sequences have, of the last draft; before it, as many as a call says
+        self.n_nodes = torch.full((B,), 64, dtype=torch.int32, device=dev)
         self._same = torch.arange(B, dtype=torch.int32, device=dev)
         # the workspace covers every choice of pages
         need = max(self._need(k) for k in range(1, p.NP + 1))
@@ -678,18 +686,25 @@ class SharedPrefix:
     def draft(self, q, k_new, v_new, tree=None, n_draft=None, pos=None):
         """The nodes of every sequence: q [B, T, Hq, D], k_new, v_new [B, T, Hkv, D].  Keys and values go behind
         the tails, whose lengths stay; returns the queries for attend_tree().  Where a sequence has no room for
-        its nodes, nothing of it is written and dev_status becomes 1."""
+        all of its nodes, it has none: nothing of it is written, attend_tree() leaves its rows as they are, accept()
+        its tail and length, and dev_status becomes 1."""
         pos0, r, out = self._first(pos), self.rotary, self._tree_rows(self._q_tree, q.shape[1])
         stc_rotary_append_tree(self.shape, q, k_new, v_new, out, self.K_tail, self.V_tail, self.n_tail,
                                self.tail_cap, r.turns if r else None, r.rot_dim if r else 0,
                                r.layout if r else STC_ROTARY_HALVES, tree=tree, n_draft=n_draft,
                                amplitude=r.amplitude if r else 1.0, pos=pos, pos0=pos0,
-                               dev_status=self.dev_status)
+                               dev_status=self.dev_status, n_have=self.n_nodes)
         return out
 
     def attend_tree(self, q, tree=None, n_draft=None, page_idx=None):
-        """page_idx as in attend().  Returns [B, T, Hq, D]; rows of nodes that are not there are what they were."""
-        return self._attend_tree(q, self._tree_rows(self._out_tree, q.shape[1]), tree, n_draft, page_idx)
+        """The nodes that draft() wrote, or the first n_draft [B] of them.  page_idx as in attend().  Returns
+        [B, T, Hq, D]; rows of nodes that are not there are what they were."""
+        nodes = self.n_nodes
+        if n_draft is not None:
+            if n_draft.numel() != self.B:
+                raise ValueError("n_draft has a number for each sequence")
+            nodes = torch.minimum(n_draft.view(-1), nodes)
+        return self._attend_tree(q, self._tree_rows(self._out_tree, q.shape[1]), tree, nodes, page_idx)
 
     def _attend_tree(self, q, out, tree, n_draft, page_idx):
         self._whole()
@@ -701,14 +716,14 @@ class SharedPrefix:
         return out
 
     def step_tree(self, q, k_new, v_new, tree=None, n_draft=None, page_idx=None, pos=None):
-        return self.attend_tree(self.draft(q, k_new, v_new, tree, n_draft, pos), tree, n_draft, page_idx)
+        return self.attend_tree(self.draft(q, k_new, v_new, tree, n_draft, pos), tree, None, page_idx)
 
     def accept(self, keep, T, layers=()):
-        """keep [B] int64: bits of the nodes (of T) that stay, in order, behind the tails, which grow by them.
-        layers: the objects of the model's other layers, for the same in all of them."""
+        """keep [B] int64: bits of the nodes (of T, and of those that draft() wrote) that stay, in order, behind the
+        tails, which grow by them.  layers: the objects of the model's other layers, for the same in all of them."""
         every = (self,) + tuple(layers)
         stc_accept_tail(self.shape, T, [x.K_tail for x in every], [x.V_tail for x in every],
-                        [x.n_tail for x in every], self.tail_cap, keep)
+                        [x.n_tail for x in every], self.tail_cap, keep, n_draft=self.n_nodes)
 
     def fork(self, src=None, n_keep=None, layers=()):
         """src [B] int32: sequence b goes on with the tail of src[b] (STC_TAIL_FREED: it ends, STC_TAIL_EMPTY: it

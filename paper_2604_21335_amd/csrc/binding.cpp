@@ -392,7 +392,7 @@ static Tree tree_of(Args& a, int32_t B, int64_t T) {
   return {p, p && n != T};
 }
 
-STC_PY(rotary_append_tree, 18,
+STC_PY(rotary_append_tree, 19,
   auto s = *a.shape(); a.one_device();
   auto q = a.rows("q", 4); auto k = a.rows("k_new", 4); auto v = a.rows("v_new", 4);
   const int64_t T = q.size[1];
@@ -411,11 +411,12 @@ STC_PY(rotary_append_tree, 18,
   auto layout = a.integer(); auto tree = tree_of(a, s.B, T);
   auto nd = (int32_t*)a.sized("n_draft", s.B, at::kInt); auto amp = a.real();
   auto pos = (int32_t*)a.sized("pos", s.B * T, at::kInt); auto pos0 = a.integer();
+  auto have = (int32_t*)a.sized("n_have", s.B, at::kInt);
   auto status = (int32_t*)a.sized("dev_status", 1, at::kInt); auto st = a.stream();
   // strides of dimensions of one element: as if rows followed each other
   if (T == 1) q.stride[1] = (int64_t)s.Hq * s.D;
   if (s.B == 1) q.stride[0] = T * s.Hq * s.D;
-  return [=] { return stc_rotary_append_tree(&s, (int)T, q.p, q.stride, k.p, k.stride, v.p, v.stride, qo, Kt, Vt, n, nd, cap, tree.p, tree.per_batch, rot, layout, turns, amp, pos, pos0, status, st); };)
+  return [=] { return stc_rotary_append_drafts(&s, (int)T, q.p, q.stride, k.p, k.stride, v.p, v.stride, qo, Kt, Vt, n, nd, cap, tree.p, tree.per_batch, rot, layout, turns, amp, pos, pos0, have, status, st); };)
 
 STC_PY(decode_attention_tree, 18,
   auto s = *a.shape(); a.one_device(); auto P = a.integer(); auto T = a.integer();
@@ -454,11 +455,12 @@ static LayerTails layer_tails(Args& a, const stc_shape_t& s, int cap) {
   return {t[0].n, t[0].p, t[1].p, (const int32_t* const*)t[2].p, (int32_t* const*)t[3].p};
 }
 
-STC_PY(accept_tail, 8,
+STC_PY(accept_tail, 9,
   auto s = *a.shape(); a.one_device(); auto T = a.integer(); auto cap = a.integer();
   auto t = layer_tails(a, s, cap);
-  auto keep = (const uint64_t*)a.sized("keep", s.B, at::kLong, at::kUInt64); auto st = a.stream();
-  return [=] { return stc_accept_tail(&s, T, t.n, t.K, t.V, t.len, t.out, cap, keep, st); };)
+  auto keep = (const uint64_t*)a.sized("keep", s.B, at::kLong, at::kUInt64);
+  auto nd = (const int32_t*)a.sized("n_draft", s.B, at::kInt); auto st = a.stream();
+  return [=] { return stc_accept_drafts(&s, T, t.n, t.K, t.V, t.len, t.out, cap, keep, nd, st); };)
 
 STC_PY(fork_tail, 9,
   auto s = *a.shape(); a.one_device(); auto cap = a.integer();

@@ -174,14 +174,16 @@ __global__ __launch_bounds__(256) void rotary_append_tree_kernel(
     const int32_t* __restrict__ n_tail, const int32_t* __restrict__ n_draft, const uint64_t* __restrict__ tree,
     u32x4* q_out, u32x4* __restrict__ K_tail, u32x4* __restrict__ V_tail, const double* __restrict__ turns,
     const int32_t* __restrict__ pos, int pos0, int T, int tree_step, int tail_cap, int Hq, int Hkv, int rot_dim,
-    float amplitude, int interleaved, NodeStrides qs, NodeStrides ks, NodeStrides vs, int32_t* dev_status) {
+    float amplitude, int interleaved, NodeStrides qs, NodeStrides ks, NodeStrides vs, int32_t* n_have,
+    int32_t* dev_status) {
   constexpr int SLOTS = D / 16, PPR = D / 8;
   const int b = blockIdx.y, n = n_tail[b], nodes = n_draft ? max(0, min(n_draft[b], T)) : T;
-  if (n < 0) return;
-  if (nodes > tail_cap - n) {  // no room for all of them: none is written
-    if (nodes > 0 && dev_status && blockIdx.x == 0 && threadIdx.x == 0) *dev_status = 1;
-    return;
+  const bool fits = n >= 0 && nodes <= tail_cap - n;  // no room for all of them: none is written
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (n_have) n_have[b] = fits ? nodes : 0;
+    if (!fits && n >= 0 && nodes > 0 && dev_status) *dev_status = 1;
   }
+  if (!fits) return;
   const int slots = (Hq + 2 * Hkv) * SLOTS, i = blockIdx.x * 256 + threadIdx.x;
   const int t = i / slots, slot = i % SLOTS, row = i % slots / SLOTS;
   if (t >= nodes) return;
@@ -280,7 +282,7 @@ int launch_rotary_append_tree(const stc_shape_t& s, int T, const void* q, const 
                               const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
                               const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
                               bool tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
-                              const int32_t* pos, int pos0, int32_t* dev_status, hipStream_t st) {
+                              const int32_t* pos, int pos0, int32_t* n_have, int32_t* dev_status, hipStream_t st) {
   const auto strides = [](const int64_t* x) { return NodeStrides{x[0] / 8, x[1] / 8}; };
   const long long slots = (long long)T * (s.Hq + 2 * s.Hkv) * (s.D / 16);
   const dim3 grid((unsigned)((slots + 255) / 256), s.B);
@@ -289,7 +291,7 @@ int launch_rotary_append_tree(const stc_shape_t& s, int T, const void* q, const 
       (const u32x4*)q, (const u32x4*)k_new, (const u32x4*)v_new, n_tail, n_draft, tree, (u32x4*)q_out,   \
       (u32x4*)K_tail, (u32x4*)V_tail, turns, pos, pos0, T, tree_per_batch ? T : 0, tail_cap, s.Hq, s.Hkv, \
       rot_dim, amplitude, layout == STC_ROTARY_INTERLEAVED, strides(q_stride), strides(k_stride),        \
-      strides(v_stride), dev_status)
+      strides(v_stride), n_have, dev_status)
   if (s.D == 128) STC_APPEND(128);
   else STC_APPEND(64);
 #undef STC_APPEND

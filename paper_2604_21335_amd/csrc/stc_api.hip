@@ -624,12 +624,13 @@ int layers_status(const stc_shape_t* s, int n_layers, void* const* K, void* cons
 }
 }  // namespace
 
-int stc_rotary_append_tree(const stc_shape_t* shape, int T, const void* q, const int64_t* q_stride,
-                           const void* k_new, const int64_t* k_stride, const void* v_new,
-                           const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
-                           const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
-                           int tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
-                           const int32_t* pos, int32_t pos0, int32_t* dev_status, void* stream) {
+int stc_rotary_append_drafts(const stc_shape_t* shape, int T, const void* q, const int64_t* q_stride,
+                             const void* k_new, const int64_t* k_stride, const void* v_new,
+                             const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
+                             const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
+                             int tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
+                             const int32_t* pos, int32_t pos0, int32_t* n_have, int32_t* dev_status,
+                             void* stream) {
   if (!shape || !q || !q_stride || !k_new || !k_stride || !v_new || !v_stride || !q_out || !K_tail || !V_tail ||
       !n_tail)
     return STC_ERR_NULL;
@@ -645,15 +646,32 @@ int stc_rotary_append_tree(const stc_shape_t* shape, int T, const void* q, const
   if (q_out == q && ((shape->B > 1 && q_stride[0] != T * row) || (T > 1 && q_stride[1] != row))) return STC_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(K_tail) ||
       !aligned16(V_tail) || (turns && !aligned16(turns)) || ((uintptr_t)n_tail & 3) || ((uintptr_t)n_draft & 3) ||
-      ((uintptr_t)pos & 3) || ((uintptr_t)tree & 7) || ((uintptr_t)dev_status & 3))
+      ((uintptr_t)pos & 3) || ((uintptr_t)tree & 7) || ((uintptr_t)n_have & 3) ||
+      ((uintptr_t)dev_status & 3))
     return STC_ERR_ALIGN;
+  const uintptr_t have = (uintptr_t)n_have;  // read by others while it is written
+  const size_t counts = (size_t)shape->B * 4;
+  if (n_have && (overlaps(n_tail, counts, &have, 1, counts) || (n_draft && overlaps(n_draft, counts, &have, 1, counts))))
+    return STC_ERR_SHAPE;
   for (int i = 0; i < 2; ++i)
     if (!stride_ok(q_stride[i]) || !stride_ok(k_stride[i]) || !stride_ok(v_stride[i])) return STC_ERR_ALIGN;
   return stc::launch_rotary_append_tree(*shape, T, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, K_tail,
                                         V_tail, n_tail, n_draft, tail_cap, tree, tree_per_batch != 0, rot_dim,
-                                        layout, turns, amplitude, pos, pos0, dev_status, (hipStream_t)stream)
+                                        layout, turns, amplitude, pos, pos0, n_have, dev_status,
+                                        (hipStream_t)stream)
              ? STC_ERR_LAUNCH
              : STC_OK;
+}
+
+int stc_rotary_append_tree(const stc_shape_t* shape, int T, const void* q, const int64_t* q_stride,
+                           const void* k_new, const int64_t* k_stride, const void* v_new,
+                           const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
+                           const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
+                           int tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
+                           const int32_t* pos, int32_t pos0, int32_t* dev_status, void* stream) {
+  return stc_rotary_append_drafts(shape, T, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, K_tail, V_tail, n_tail,
+                                  n_draft, tail_cap, tree, tree_per_batch, rot_dim, layout, turns, amplitude, pos, pos0,
+                                  nullptr, dev_status, stream);
 }
 
 size_t stc_tree_workspace_bytes(const stc_shape_t* shape, int T, int n_prefix, int k_pages, int tail_cap) {
@@ -685,20 +703,26 @@ int stc_decode_attention_tree(const stc_shape_t* shape, int T, int n_prefix, con
              : STC_OK;
 }
 
-int stc_accept_tail(const stc_shape_t* shape, int T, int n_layers, void* const* K_tail, void* const* V_tail,
-                    const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
-                    void* stream) {
+int stc_accept_drafts(const stc_shape_t* shape, int T, int n_layers, void* const* K_tail, void* const* V_tail,
+                      const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
+                      const int32_t* n_draft, void* stream) {
   if (!shape || !K_tail || !V_tail || !n_tail || !n_out || !keep) return STC_ERR_NULL;
   if (!shape_ok(shape) || T < 1 || T > kMostNodes || n_layers < 1 || n_layers > kMostLayers || tail_cap < 1 ||
       tail_cap > (1 << 30))
     return STC_ERR_SHAPE;
-  if ((uintptr_t)keep & 7) return STC_ERR_ALIGN;
-  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep, 8, nullptr);
+  if (((uintptr_t)keep & 7) || ((uintptr_t)n_draft & 3)) return STC_ERR_ALIGN;
+  const int status = layers_status(shape, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep, 8, n_draft);
   if (status != STC_OK) return status;
-  return stc::launch_accept_tail(*shape, T, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep,
+  return stc::launch_accept_tail(*shape, T, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep, n_draft,
                                  (hipStream_t)stream)
              ? STC_ERR_LAUNCH
              : STC_OK;
+}
+
+int stc_accept_tail(const stc_shape_t* shape, int T, int n_layers, void* const* K_tail, void* const* V_tail,
+                    const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
+                    void* stream) {
+  return stc_accept_drafts(shape, T, n_layers, K_tail, V_tail, n_tail, n_out, tail_cap, keep, nullptr, stream);
 }
 
 int stc_fork_tail(const stc_shape_t* shape, int n_layers, void* const* K_tail, void* const* V_tail,

@@ -115,7 +115,7 @@ int launch_rotary_append_tree(const stc_shape_t& s, int T, const void* q, const 
                               const int64_t* v_stride, void* q_out, void* K_tail, void* V_tail,
                               const int32_t* n_tail, const int32_t* n_draft, int tail_cap, const uint64_t* tree,
                               bool tree_per_batch, int rot_dim, int layout, const double* turns, float amplitude,
-                              const int32_t* pos, int pos0, int32_t* dev_status, hipStream_t st);
+                              const int32_t* pos, int pos0, int32_t* n_have, int32_t* dev_status, hipStream_t st);
 
 size_t tree_ws_bytes(const stc_shape_t& s, int T, int n_prefix, int k_pages, int tail_cap);
 int launch_tree(const stc_shape_t& s, int T, int n_prefix, const void* q, const void* K, const void* vpacked,
@@ -128,7 +128,7 @@ constexpr int kTailLayers = 64;  // layers of a launch
 constexpr int kForkMost = 4096;  // sequences of a fork
 int launch_accept_tail(const stc_shape_t& s, int T, int n_layers, void* const* K_tail, void* const* V_tail,
                        const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
-                       hipStream_t st);
+                       const int32_t* n_draft, hipStream_t st);
 int launch_fork_tail(const stc_shape_t& s, int n_layers, void* const* K_tail, void* const* V_tail,
                      const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const int32_t* src,
                      const int32_t* n_keep, int32_t* dev_status, hipStream_t st);

@@ -20,11 +20,12 @@ struct Layers {
 // moves to place i behind the tail.  A kept row never stands in front of its place, so a thread that reads rows in
 // order, eight at a time before it writes them, reads each before it is overwritten.  The length is read by all
 // before it may be advanced in place.
-__global__ __launch_bounds__(1024) void accept_kernel(Layers L, const uint64_t* __restrict__ keep, int T,
-                                                      int tail_cap, int Hkv, int PPR) {
+__global__ __launch_bounds__(1024) void accept_kernel(Layers L, const uint64_t* __restrict__ keep,
+                                                      const int32_t* __restrict__ n_draft, int T, int tail_cap, int Hkv,
+                                                      int PPR) {
   const int b = blockIdx.x, layer = blockIdx.y;
-  const int n = L.n[layer][b];
-  uint64_t k = keep[b] & (~0ull >> (64 - T));
+  const int n = L.n[layer][b], nodes = n_draft ? max(0, min(n_draft[b], T)) : T;
+  uint64_t k = nodes ? keep[b] & (~0ull >> (64 - nodes)) : 0;
   const int room = n < 0 ? 0 : max(tail_cap - n, 0);  // rows behind the tail
   if (room < 64) k &= (1ull << room) - 1;
   const int count = __builtin_popcountll(k);
@@ -177,12 +178,12 @@ Layers layers_of(int count, void* const* K_tail, void* const* V_tail, const int3
 
 int launch_accept_tail(const stc_shape_t& s, int T, int n_layers, void* const* K_tail, void* const* V_tail,
                        const int32_t* const* n_tail, int32_t* const* n_out, int tail_cap, const uint64_t* keep,
-                       hipStream_t st) {
+                       const int32_t* n_draft, hipStream_t st) {
   const int ppr = s.D / 8, cols = 2 * s.Hkv * ppr, threads = cols >= 1024 ? 1024 : (cols + 63) / 64 * 64;
   for (int at = 0; at < n_layers; at += kTailLayers) {
     const int count = n_layers - at < kTailLayers ? n_layers - at : kTailLayers;
     const Layers L = layers_of(count, K_tail + at, V_tail + at, n_tail + at, n_out + at);
-    accept_kernel<<<dim3(s.B, count), threads, 0, st>>>(L, keep, T, tail_cap, s.Hkv, ppr);
+    accept_kernel<<<dim3(s.B, count), threads, 0, st>>>(L, keep, n_draft, T, tail_cap, s.Hkv, ppr);
     if (hipGetLastError() != hipSuccess) return -1;
   }
   return 0;

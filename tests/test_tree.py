@@ -143,6 +143,32 @@ def test_accept_refuses_kept_sets_where_lengths_of_a_far_layer_are_written():
                       keep=ctypes.c_void_p(keep)) == stc.STC_ERR_SHAPE
 
 
+# counts of nodes: written by the one call, where others are read; read by the other, where lengths are written
+@pytest.mark.parametrize("have,kw,status", [
+    (0x20002, {}, "ALIGN"), (0x30000, dict(n=ctypes.c_void_p(0x30000)), "SHAPE"), (0x30010, dict(n=ctypes.c_void_p(0x30000)), "SHAPE"),
+    (0x2fff0, dict(n=ctypes.c_void_p(0x30000)), "SHAPE"), (0x40000, dict(nd=ctypes.c_void_p(0x40000)), "SHAPE"),
+    (0x40004, dict(nd=ctypes.c_void_p(0x40000)), "SHAPE"), (0x3fffc, dict(nd=ctypes.c_void_p(0x40000)), "SHAPE"),
+    (0x50000, dict(T=65), "SHAPE"), (0x50000, dict(q=None), "NULL")])
+def test_append_with_counts_refuses(have, kw, status):
+    a = dict(T=3, q=FAKE, n=FAKE, nd=None)
+    a.update(kw)
+    row = (I64 * 2)(3 * 1024, 1024)
+    assert stc.load_library().stc_rotary_append_drafts(
+        ctypes.byref(_shape(None)), a["T"], a["q"], row, FAKE, row, FAKE, row, ctypes.c_void_p(0x90000), FAKE, FAKE,
+        a["n"], a["nd"], 16, None, 0, 64, 0, FAKE, 1.0, None, 0, ctypes.c_void_p(have), None,
+        None) == getattr(stc, "STC_ERR_" + status)
+
+
+@pytest.mark.parametrize("counts,status", [(0x20002, "ALIGN"), (0x1000, "SHAPE"), (0x1010, "SHAPE"), (0x1030, "SHAPE"),
+                                           (0xff0, "SHAPE")])
+def test_accept_with_counts_refuses(counts, status):
+    size = 5 * 2 * 16 * 128 * 2
+    n = _ptrs([0x1000, 0x1020])
+    assert stc.load_library().stc_accept_drafts(
+        ctypes.byref(_shape(None)), 8, 2, _ptrs([0x100000, 0x100000 + size]), _ptrs([0x900000, 0x900000 + size]), n, n, 16,
+        FAKE, ctypes.c_void_p(counts), None) == getattr(stc, "STC_ERR_" + status)
+
+
 def test_null_shape():
     lib = stc.load_library()
     assert lib.stc_accept_tail(None, 1, 1, None, None, None, None, 1, None, None) == stc.STC_ERR_NULL
