@@ -500,11 +500,10 @@ int stc_rotary_append_drafts(const stc_shape_t *shape, int T, const void *q, con
  *   out      [B, T, Hq, D], out, float or bf16; rows of padding and of nodes that a sequence does not have are left
  *            as they are; a query without any token gets zeros
  *   ws       stc_tree_workspace_bytes(...) bytes; calls whose work overlaps in time need one each
- * Magnitudes count as for stc_decode_attention_shared.  Weights are carried as bf16 parts: two (2^-16) for the prefix
- * where a KV head has more than 64 query rows of one prefix, three (2^-24) where it has fewer, where the output is float and
- * up to 16384 tokens are listed, and for the tails.  Keys and values of a node that are infinite or NaN reach the
- * queries that see it and no others.  Where the sums of a query are cut depends on the lengths and nodes of the whole
- * batch: other sequences change its results by roundings, and by nothing else.
+ * Magnitudes count as for stc_decode_attention_shared.  Weights are carried as three bf16 parts (2^-24), but where the output
+ * is bf16 and a KV head has more than 64 query rows of one prefix: there as two (2^-16) for the prefix.  Keys and values
+ * of a node that are infinite or NaN reach the queries that see it and no others.  Where the sums of a query are cut
+ * depends on the lengths and nodes of the whole batch: other sequences change its results by roundings, and by nothing else.
  */
 size_t stc_tree_workspace_bytes(const stc_shape_t *shape, int T, int n_prefix, int k_pages, int tail_cap);
 int stc_decode_attention_tree(const stc_shape_t *shape, int T, int n_prefix, const void *q, const void *K,

@@ -925,10 +925,12 @@ int tree_rows(const TreeParams& P, const TreePlan& p, bool stream, hipStream_t s
     return stream ? flow_go<D, LIST, true, true>(P, p.groups, st) : flow_go<D, LIST, false, true>(P, p.groups, st);
   if (p.wr == 2)
     return stream ? tree_go<D, 2, LIST, true, 3>(P, p.groups, st) : tree_go<D, 2, LIST, false, 3>(P, p.groups, st);
-  // Two parts of a weight leave 2^-16 of it, and a float output off by 1.5 .. 2 10^-6 of its norm; that is what sums of
-  // 32768 floats leave anyway, but twice what those of some thousand do.  Three cost 5 .. 14 % here (448 rows over 32768
-  // tokens 69 -> 79 us), so they are for float outputs of fewer tokens.
-  const bool three = !P.out_bf16 && P.k_pages * kPage <= 16384;
+  // Three parts are a float's 24 bits, for float outputs.  Two leave 2^-16 of a weight, and 1.3 .. 2 10^-6 of the output's
+  // norm whatever the number of tokens, where three leave 0.4 .. 0.8 10^-6 (9000 .. 131072 tokens).  Beside a bf16 output's
+  // own rounding, 1.7 10^-3 of its norm, neither is seen (it changes by less than 10^-6), and a third part would cost 22 %
+  // of 16 sequences of 16 nodes, half of them there, over 32768 tokens (127 -> 155 us); 448 rows over as many take 79 us
+  // with three, 69 with two.
+  const bool three = !P.out_bf16;
   if (p.wr == 4)
     return three ? tree_go<D, 4, LIST, false, 3>(P, p.groups, st) : tree_go<D, 4, LIST, false, 2>(P, p.groups, st);
   return three ? tree_go<D, 8, LIST, false, 3>(P, p.groups, st) : tree_go<D, 8, LIST, false, 2>(P, p.groups, st);
