@@ -90,7 +90,7 @@ __device__ __forceinline__ void fork_lengths(const int32_t* n, int32_t* out, con
 // columns of a row) of one head for ALL sequences that get another's rows, so it reads whatever it overwrites
 // first: a thread holds PIECES 16-byte pieces across a barrier.  One workgroup of a layer writes the lengths where they go
 // to another place than they come from (LENGTHS); else a launch behind this one does, since all workgroups read them.
-// Bound by memory: 48 sequences of 8 heads in 4 layers, a third of which move, 289 MB read and written in 65 us, 4.4 TB/s;
+// Bound by memory: 48 sequences of 8 heads in 4 layers, a third of which move, 318 MB read and written in 56 .. 68 us, 4.7 .. 5.7 TB/s;
 // all of 1500 rows, 786 MB, 5.2.  (Stores past the caches take 5 us off, loads past them put 8 on; 6 wavefronts' registers
 // per SIMD: 65, 5: 74, 8: 86; 1024 workgroups in place of 2048 75; rows that few moves have taken more at a time, by
 // moves in order of their lengths, 72; without the barrier the same.)

@@ -11,11 +11,11 @@
 // the prefix.  A second launch merges a row's partial results.
 //
 // What bounds it (D = 128, half of the value groups kept; both launches):
-//   448 rows of one sequence over 32768 tokens, 4 KV heads: 69 us; matrix products with weights in two parts, 730 TFLOP/s of
-//     executed ones, in 35 turns of 1.8 us; the merge of 15 splits takes 6.
-//   16 sequences of 16 nodes, half of them there, over the same: 114 us, 900 TFLOP/s (all there: 180); the chip's power.
-//   8 x 32 heads over 64 listed pages each and tails of up to 200: 34 us, memory, 118 MB; first loads and the merge.
-//   64 x 32 heads over 208 tokens, tails of up to 1000: 116 us; the tails at 6.2 TB/s, then units that end late, merge 8.
+//   448 rows of one sequence over 32768 tokens, 4 KV heads: 78 us; matrix products with weights in three parts, 730 TFLOP/s of
+//     executed ones, in 35 turns of 2.1 us; the merge of 15 splits takes 7.
+//   16 sequences of 16 nodes, half of them there, over the same: 123 .. 127 us, 850 TFLOP/s (all there: 181); the chip's power.
+//   8 x 32 heads over 64 listed pages each and tails of up to 200: 34 us, memory, 120 MB; first loads and the merge.
+//   64 x 32 heads over 208 tokens, tails of up to 1000: 117 us; the tails at 6.2 TB/s, then units that end late, merge 8.
 #include <algorithm>
 
 #include "shared_block.hpp"
@@ -139,7 +139,7 @@ __device__ __forceinline__ int groups_with_more(int items, int groups) {
 // A memory instruction must stand five wait states behind a vector instruction that writes a scalar register which it
 // reads, and nothing in the hardware sees to that.  Bases come out of vector instructions (the first lane's value, or a
 // register put aside in a lane), and the compiler does not look at what is written out: the move to m0 is one of the five,
-// the other four follow it.  (m0 itself needs one.)
+// the other four follow it.  (m0 itself needs one.  Ten more states cost 0 .. 2 %: small tiles of many prefixes 34.7 -> 35.4 us.)
 __device__ __forceinline__ Rsrc buffer(const void* base, uint32_t bytes) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
